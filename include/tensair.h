@@ -452,6 +452,7 @@ TENSAIR_API int tensair_tune(const char* name, int value);
 TENSAIR_API int tensair_profile_read(tensair_ctx* ctx, uint32_t max_kinds, tensair_kernel_time* out, uint32_t* n_kinds);
 
 TENSAIR_API const char* tensair_strerror(int code);
+/* ctx NULL: what the calling thread's last refused or failed operator call (lookup, gradient, AdamW) said. */
 TENSAIR_API const char* tensair_last_error(const tensair_ctx* ctx);
 
 /* The device-side error word.  Kernels never trap: one that meets bad input or gives up a bounded wait sets a bit
@@ -471,6 +472,115 @@ TENSAIR_API const char* tensair_last_error(const tensair_ctx* ctx);
 TENSAIR_API int tensair_checked_build(void);
 TENSAIR_API int tensair_error_of_flags(uint32_t flags);
 TENSAIR_API int tensair_raise_error_flags(tensair_ctx* ctx, uint32_t flags);
+
+/*
+ * ---- operators of language models over the caller's tensors ----
+ *
+ * What a model that is trained on from these tables needs next to them: rows looked up for a batch of tokens, the
+ * gradient of the table, an AdamW step over many tensors, and the AdamW step of the rows that a batch touched.
+ * They need no context.  Each call enqueues its work on `stream` (a cudaStream_t of the calling thread's current
+ * device; NULL = the legacy default stream), allocates no device memory, does not synchronise and can be
+ * captured into a CUDA graph.  All pointers inside the argument blocks are device pointers that must stay valid until
+ * the stream has passed the call; the argument blocks themselves are read during the call.  Arguments are checked
+ * before anything is enqueued; tensair_last_error(NULL) says what the calling thread's last refused call was refused for.
+ * Everything is computed in fp32 whatever the tensors' types are, and rounded to nearest once, when it is stored.
+ * No sum depends on timing: the same inputs give the same bits.
+ */
+enum { TENSAIR_FLOAT32 = 0, TENSAIR_BFLOAT16 = 1, TENSAIR_FLOAT16 = 2, TENSAIR_INT32 = 3, TENSAIR_INT64 = 4 };
+
+/* The token ids of a batch. */
+typedef struct tensair_tokens {
+    const void* ids;          /* [n], of `type` */
+    uint64_t n;               /* 0 .. 2^30 */
+    uint64_t V;               /* rows of the table, 1 .. 2^30 */
+    int64_t padding_id;       /* an id that stands for "no token": its position reads as a zero row and has no gradient */
+    uint32_t* error;          /* nullable: a sticky error word of the caller's; bit 0 is set when an id is neither in [0,V)
+                                 nor padding_id (tensair_error_of_flags decodes it); such a position is treated as
+                                 one without a token */
+    uint32_t type;            /* TENSAIR_INT32 or TENSAIR_INT64 */
+    uint32_t reserved;
+} tensair_tokens;
+
+/* Rows of d elements, `stride` elements (>= d) apart. */
+typedef struct tensair_rows {
+    void* data;
+    uint64_t stride;
+    uint32_t d;               /* 1 .. 2^20 */
+    uint32_t type;            /* TENSAIR_FLOAT32, TENSAIR_BFLOAT16 or TENSAIR_FLOAT16 */
+} tensair_rows;
+
+/* out[i] = scale * table[ids[i]], a row of zeros where there is no token.  table: V rows; out: n rows. */
+TENSAIR_API int tensair_embedding_lookup(const tensair_tokens* tokens, const tensair_rows* table, const tensair_rows* out,
+                                         float scale, void* stream);
+
+/*
+ * The gradient of the lookup with respect to the table, by sorted tokens: with S(v) = the positions that hold token v,
+ *     G[v] = scale * sum over i in S(v), ascending, of grad[i].
+ * The batch is sorted by token on the device and every token's rows are added up in fp32 in an order that n and the
+ * token's place in the sorted batch fix.  grad rows of positions without a token are not read.
+ *   tensair_embedding_gradient       the whole table: out[v] = G[v] for all V rows (zeros for tokens that do not occur), or,
+ *                                    with accumulate != 0, out[v] += G[v] for the tokens that occur (no other row is
+ *                                    read or written).
+ *   tensair_embedding_gradient_rows  the touched rows alone, as a sparse gradient message has them: *count = the distinct
+ *                                    tokens, row_ids[0 .. count) ascending, rows[m] = G[row_ids[m]] (fp32).  Both
+ *                                    arrays need room for min(n, V) rows; entries from count on are left alone.
+ * workspace: device memory of tensair_embedding_workspace_bytes(n, V, d) bytes, 256-byte aligned; a workspace that
+ * serves n tokens serves every smaller batch of the same V and d.  It holds nothing between calls; calls that share
+ * one must be ordered by their streams.
+ */
+TENSAIR_API int tensair_embedding_workspace_bytes(uint64_t n, uint64_t V, uint32_t d, uint64_t* bytes);
+TENSAIR_API int tensair_embedding_gradient(const tensair_tokens* tokens, const tensair_rows* grad, const tensair_rows* out,
+                                           float scale, int accumulate, void* workspace, uint64_t workspace_bytes,
+                                           void* stream);
+TENSAIR_API int tensair_embedding_gradient_rows(const tensair_tokens* tokens, const tensair_rows* grad, float scale,
+                                                uint32_t* row_ids, const tensair_rows* rows, uint32_t* count,
+                                                void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * AdamW (Loshchilov & Hutter): with g = *grad_scale * gradient and t = step,
+ *     m <- beta1 m + (1 - beta1) g            v <- beta2 v + (1 - beta2) g^2
+ *     p <- p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ */
+typedef struct tensair_adamw {
+    double lr, beta1, beta2, eps, weight_decay;
+    uint64_t step;            /* t, from 1 */
+    uint64_t seed;            /* of the stochastic rounding of 8-bit moments */
+    const float* grad_scale;  /* device, nullable = 1: a factor on every gradient (clipping, loss scaling).  If it is not
+                                 finite when the stream reaches the call, the step changes nothing. */
+} tensair_adamw;
+
+/* The AdamW step of the rows of a table that a batch touched, straight from the batch's gradient rows: for every token v
+ * that occurs, row v of table (any type), m and v (TENSAIR_FLOAT32) is updated with the gradient G[v] above; all other
+ * rows, weight decay included, stay as they are.  Workspace as above. */
+TENSAIR_API int tensair_embedding_adamw(const tensair_tokens* tokens, const tensair_rows* grad, float scale,
+                                        const tensair_rows* table, const tensair_rows* m, const tensair_rows* v,
+                                        const tensair_adamw* adamw, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* One tensor of an AdamW step: n elements, contiguous. */
+typedef struct tensair_adamw_tensor {
+    void* param;
+    const void* grad;
+    void* m;                  /* state_bits 32: float[n]; 8: e4m3[n], m = value * m_scale of its block */
+    void* v;                  /* state_bits 32: float[n]; 8: e4m3[n], sqrt(v) = value * v_scale of its block */
+    float* m_scale;           /* state_bits 8: float[ceil(n / 256)], one for each block of 256 elements; else ignored */
+    float* v_scale;
+    void* copy;               /* nullable: receives the updated parameter rounded to copy_type */
+    uint64_t n;               /* below 2^40; 0 = nothing to do */
+    double lr_factor;         /* on lr, for this tensor */
+    double decay_factor;      /* on weight_decay, for this tensor */
+    uint32_t param_type, grad_type, copy_type;
+    uint32_t reserved;
+} tensair_adamw_tensor;
+
+/*
+ * One AdamW step of `count` tensors, at once: one launch for each combination of parameter and gradient type (and
+ * for every 340 tensors).  tensors: host.  Moments in 8 bits start as zeros (codes and scales); a block whose largest
+ * first moment is below 2^-110 is stored as zeros.  They are rounded stochastically to a neighbouring e4m3 value with random
+ * bits that depend on (seed, step, the element's place in the list of tensors) alone; a positive v is never
+ * stored as zero; a non-finite moment is stored as NaN and leaves the other elements of its block alone.
+ */
+TENSAIR_API int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint32_t state_bits,
+                                   const tensair_adamw* adamw, void* stream);
 
 /* ---- host-only pieces, usable without a GPU ---- */
 

@@ -60,6 +60,30 @@ class KernelTime(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("launches", C.c_uint64), ("total_ms", C.c_double)]
 
 
+FLOAT32, BFLOAT16, FLOAT16, INT32, INT64 = 0, 1, 2, 3, 4
+
+
+class Tokens(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("n", C.c_uint64), ("V", C.c_uint64), ("padding_id", C.c_int64), ("error", C.c_void_p),
+                ("type", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_uint64), ("d", C.c_uint32), ("type", C.c_uint32)]
+
+
+class Adamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_uint64), ("seed", C.c_uint64), ("grad_scale", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_uint64), ("lr_factor", C.c_double),
+                ("decay_factor", C.c_double), ("param_type", C.c_uint32), ("grad_type", C.c_uint32),
+                ("copy_type", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 class TensairError(RuntimeError):
     def __init__(self, code: int, what: str, detail: str = ""):
         self.code = code
@@ -123,8 +147,16 @@ SYMBOLS = {
     "tensair_schedule_load": (_int, [_vp, C.c_char_p, _u64]),
     "tensair_save_state": (_int, [_vp, _vp, _u64, _P(_u64)]),
     "tensair_load_state": (_int, [_vp, C.c_char_p, _u64]),
+    "tensair_embedding_lookup": (_int, [_P(Tokens), _P(Rows), _P(Rows), C.c_float, _vp]),
+    "tensair_embedding_workspace_bytes": (_int, [_u64, _u64, _u32, _P(_u64)]),
+    "tensair_embedding_gradient": (_int, [_P(Tokens), _P(Rows), _P(Rows), C.c_float, _int, _vp, _u64, _vp]),
+    "tensair_embedding_gradient_rows": (_int, [_P(Tokens), _P(Rows), C.c_float, _vp, _P(Rows), _vp, _vp, _u64, _vp]),
+    "tensair_embedding_adamw": (_int, [_P(Tokens), _P(Rows), C.c_float, _P(Rows), _P(Rows), _P(Rows), _P(Adamw), _vp, _u64, _vp]),
+    "tensair_adamw_step": (_int, [_P(AdamwTensor), _u64, _u32, _P(Adamw), _vp]),
 }
 
+_OPERATORS = {"tensair_embedding_lookup", "tensair_embedding_workspace_bytes", "tensair_embedding_gradient",
+              "tensair_embedding_gradient_rows", "tensair_embedding_adamw", "tensair_adamw_step"}
 _lib = None
 
 
@@ -158,7 +190,8 @@ def strerror(code: int) -> str:
 
 def _check(rc: int, what: str, ctx=None):
     if rc != OK:
-        detail = lib().tensair_last_error(ctx).decode() if ctx else ""
+        # without a context: what the calling thread's last operator call said, kept by the operator calls alone
+        detail = lib().tensair_last_error(ctx).decode() if ctx or what in _OPERATORS else ""
         raise TensairError(rc, what, detail)
 
 

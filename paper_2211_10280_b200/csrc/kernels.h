@@ -188,4 +188,7 @@ cudaError_t launch_index_received(const Launcher& L, MsgHeader* hdr, const uint3
 cudaError_t launch_apply_rows(const Launcher& L, const MsgHeader* hdr, const uint32_t* ids, const float* delta,
                               float* table, const Shape& s, int input_rows_only);
 
+// operators.cu: what the last refused or failed operator call of this thread said
+const char* operator_error();
+
 }  // namespace tensair

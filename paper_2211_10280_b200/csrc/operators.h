@@ -1,0 +1,142 @@
+// Shared pieces of the language-model operators (embedding lookup, its gradient, AdamW): argument blocks, element
+// types, and the host-side launchers.  These calls have no context: they work on caller-owned tensors, on the
+// caller's stream, and count no launches of a context.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace tensair {
+
+// How the token ids of a batch are read.
+struct TokenIds {
+    const void* ids;
+    int64_t padding;      // an id equal to this stands for "no token"
+    uint32_t* err;        // nullable: receives kErrBadToken
+    uint32_t n, V;
+    bool wide;            // 64-bit ids
+};
+
+// ---- element types: everything is computed in fp32 and rounded to nearest once, when it is stored
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// E consecutive elements, aligned for one access of up to 16 bytes (wider packs are two of them).
+template <typename T, int E>
+struct alignas(sizeof(T) * E > 16 ? 16 : sizeof(T) * E) Pack {
+    T v[E];
+};
+template <typename T, int E>
+__device__ __forceinline__ Pack<T, E> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, E>*>(p); }
+template <typename T, int E>
+__device__ __forceinline__ void store_pack(T* p, const float (&x)[E]) {
+    Pack<T, E> out;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out.v[e] = from_float<T>(x[e]);
+    *reinterpret_cast<Pack<T, E>*>(p) = out;
+}
+
+// x / divisor for 32-bit x by one multiplication with a reciprocal rounded up (Granlund & Montgomery 1994):
+// exact for x < 2^31 and any divisor >= 1.
+struct FastDiv {
+    uint32_t divisor, mul, shift;
+    explicit FastDiv(uint32_t d = 1) : divisor(d) {
+        shift = 0;
+        while (shift < 31 && (1ull << shift) < d) ++shift;
+        mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t div(uint32_t x) const { return (__umulhi(x, mul) + x) >> shift; }
+};
+
+// The constants of one AdamW step (see adamw.cuh for the formulas).
+struct AdamwConsts {
+    float beta1, rest1;        // beta1, 1 - beta1
+    float beta2, rest2;
+    float eps;
+    float inv_root2;           // 1 / sqrt(1 - beta2^t)
+    float step_size;           // lr / (1 - beta1^t)
+    float keep;                // 1 - lr * weight_decay
+    const float* grad_scale;   // device, nullable
+};
+
+// ---- token_sort.cu
+// A batch's positions sorted by token, stable, with the tokens' segments.
+struct SortedTokens {
+    uint32_t* key;         // [n] token of each sorted position; V from n_valid on
+    uint32_t* pos;         // [n] the batch position it came from
+    uint32_t* seg_start;   // [min(n, V) + 1] first sorted position of each distinct token, then n_valid
+    uint32_t* span_rank;   // [spans] distinct tokens that begin before the span
+    uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2] short, [3] long crossing segments
+    uint32_t span;         // sorted positions per span (a power of two)
+};
+struct SortScratch {
+    item_t* a;
+    item_t* b;
+    uint32_t* hist;
+    uint32_t* tile_counts;
+};
+bool sorts_in_one_launch(uint32_t n);
+cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w);
+
+// ---- embedding.cu
+struct RowsView {          // rows of d elements, `stride` elements apart
+    void* data;
+    uint64_t stride;
+    uint32_t type;
+};
+enum SumKind { kSumTable, kSumRows, kSumAdamw };
+struct SumArgs {
+    SortedTokens s;
+    RowsView grad;         // [n] gradient rows
+    uint32_t n, V, d;
+    float scale;
+    float* partials;       // [spans][2][partial_stride]
+    uint32_t partial_stride;
+    uint2* crossing;       // [2][spans] (span, rank) of the segments that leave the span they begin in: short, then long
+    // where a finished row goes
+    RowsView out;          // kSumTable: row `token`; kSumRows: row `rank`; kSumAdamw: the table of parameters
+    int accumulate;
+    uint32_t clear_rows;   // kSumTable: rows of `out` to set to zero first
+    uint32_t* out_ids;     // kSumRows
+    uint32_t* out_count;   // kSumRows
+    float* m;
+    float* v;
+    uint64_t m_stride, v_stride;
+    AdamwConsts adamw;
+};
+uint32_t span_length(uint32_t n, uint32_t d);
+// The longest batch below n tokens whose spans are shorter than those of n; 0 if there is none.
+uint32_t longest_with_shorter_spans(uint32_t n, uint32_t d);
+cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView& table, const RowsView& out, uint32_t d,
+                          float scale);
+cudaError_t launch_clear_rows(cudaStream_t stream, const RowsView& rows, uint64_t count, uint32_t d);
+cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs& a);
+
+// ---- adamw.cu
+struct AdamwTensor {
+    void* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;        // 8-bit moments
+    float* v_scale;
+    void* copy;            // nullable
+    uint64_t n;
+    uint64_t block0;       // 8-bit moments: blocks of the tensors before it
+    float step_size, keep;
+    uint32_t param_type, grad_type, copy_type;
+};
+cudaError_t launch_adamw(cudaStream_t stream, const AdamwTensor* tensors, uint32_t count, int bits, const AdamwConsts& c,
+                         uint64_t step, uint64_t seed, int sms);
+
+inline uint32_t type_bytes(uint32_t type) { return type == 0 ? 4 : 2; }
+
+}  // namespace tensair

@@ -5,6 +5,8 @@
 //              output words 0,1 feed draw 2*(j/2), words 2,3 feed draw 2*(j/2)+1
 //   delays     counter = (step, sender, receiver, 2<<24); word 0 is used
 //   init       counter = (e/4 low, e/4 high, 0, 3<<24) for table element e = row*d + col; word e%4
+//   rounding   counter = (group of 8 elements low, high, step low, 5<<24 | step high); element e of the group takes the
+//              low (e even) or high (e odd) half of word e/2
 #pragma once
 #include <stdint.h>
 
@@ -19,6 +21,7 @@ constexpr uint32_t kTagNegative = 1u << 24;
 constexpr uint32_t kTagDelay = 2u << 24;
 constexpr uint32_t kTagInit = 3u << 24;
 constexpr uint32_t kTagRoute = 4u << 24;
+constexpr uint32_t kTagRounding = 5u << 24;
 
 struct Philox4 {
     uint32_t x, y, z, w;

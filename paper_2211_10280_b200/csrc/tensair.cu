@@ -1005,7 +1005,7 @@ const char* tensair_strerror(int code) {
     }
 }
 
-const char* tensair_last_error(const tensair_ctx* ctx) { return ctx ? ctx->last_error.c_str() : ""; }
+const char* tensair_last_error(const tensair_ctx* ctx) { return ctx ? ctx->last_error.c_str() : operator_error(); }
 
 int tensair_error_of_flags(uint32_t flags) { return error_of_flags(flags, nullptr); }
 
