@@ -116,117 +116,125 @@ cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView
     return cudaSuccess;
 }
 
-cudaError_t launch_clear_rows(cudaStream_t stream, const RowsView& rows, uint64_t count, uint32_t d) {
-    const size_t b = type_bytes(rows.type);
-    if (rows.stride == d) return cudaMemsetAsync(rows.data, 0, count * d * b, stream);
-    return cudaMemset2DAsync(rows.data, rows.stride * b, 0, d * b, count, stream);
-}
-
 namespace {
 
 // ------------------------------------------------------------------ sums by token
 constexpr int kSumThreads = 256;
-constexpr int kSumBatch = 8;           // gradient vectors a thread has in flight
 constexpr int kCrossThreads = 512;
 constexpr int kCrossWarps = kCrossThreads / 32;
 constexpr uint32_t kLongCrossing = 16; // a segment over more spans than this is added up by a whole block
 
-// What is done with the finished sum of a token: E columns from `col` on.
+// What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
+// several tokens' reads are in flight before the first is needed; put() joins and stores.
 template <SumKind kKind, typename TO, int E>
 struct Finish {
-    static __device__ __forceinline__ void put(const SumArgs& a, float grad_scale, uint32_t key, uint32_t rank, uint32_t col,
-                                               const float (&sum)[E]) {
+    Pack<TO, E> old;
+    Pack<float, E> m0, v0;
+
+    __device__ __forceinline__ void fetch(const SumArgs& a, uint32_t key, uint32_t col) {
+        if (kKind == kSumRows || (kKind == kSumTable && !a.accumulate)) return;
+        old = load_pack<TO, E>((const TO*)a.out.data + (uint64_t)key * a.out.stride + col);
+        if (kKind == kSumAdamw) {
+            m0 = load_pack<float, E>(a.m + (uint64_t)key * a.m_stride + col);
+            v0 = load_pack<float, E>(a.v + (uint64_t)key * a.v_stride + col);
+        }
+    }
+    __device__ __forceinline__ void put(const SumArgs& a, float grad_scale, uint32_t key, uint32_t rank, uint32_t col,
+                                        const float (&sum)[E]) {
         float y[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = sum[e] * a.scale;
         TO* out = (TO*)a.out.data + (uint64_t)(kKind == kSumRows ? rank : key) * a.out.stride + col;
         if (kKind == kSumTable) {
-            if (a.accumulate) {
-                const Pack<TO, E> old = load_pack<TO, E>(out);
+            if (a.accumulate)
 #pragma unroll
                 for (int e = 0; e < E; ++e) y[e] += to_float(old.v[e]);
-            }
-            store_pack<TO, E>(out, y);
         } else if (kKind == kSumRows) {
-            store_pack<TO, E>(out, y);
             if (col == 0) a.out_ids[rank] = key;
         } else {
-            float* mp = a.m + (uint64_t)key * a.m_stride + col;
-            float* vp = a.v + (uint64_t)key * a.v_stride + col;
-            const Pack<TO, E> p = load_pack<TO, E>(out);
-            const Pack<float, E> m0 = load_pack<float, E>(mp), v0 = load_pack<float, E>(vp);
             float m[E], v[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 m[e] = m0.v[e];
                 v[e] = v0.v[e];
-                y[e] = adamw_update(to_float(p.v[e]), y[e] * grad_scale, m[e], v[e], a.adamw, a.adamw.step_size, a.adamw.keep);
+                y[e] = adamw_update(to_float(old.v[e]), y[e] * grad_scale, m[e], v[e], a.adamw, a.adamw.step_size, a.adamw.keep);
             }
-            store_pack<TO, E>(out, y);
-            store_pack<float, E>(mp, m);
-            store_pack<float, E>(vp, v);
+            store_pack<float, E>(a.m + (uint64_t)key * a.m_stride + col, m);
+            store_pack<float, E>(a.v + (uint64_t)key * a.v_stride + col, v);
         }
+        store_pack<TO, E>(out, y);
     }
 };
+
 
 template <SumKind kKind, typename TG, typename TO, int E>
 __global__ void __launch_bounds__(kSumThreads)
 k_segment_sums(const __grid_constant__ SumArgs a, uint32_t span0, uint32_t total, FastDiv vecs) {
+    constexpr int kBatch = kKind == kSumRows ? 8 : 4;   // gradient vectors in flight; fewer where finished rows bring reads of their own
+    let_next_launch_begin();
     const uint32_t w = blockIdx.x * kSumThreads + threadIdx.x;
+    const uint32_t q = vecs.div(w);
+    const uint32_t span = span0 + q, col = (w - q * vecs.divisor) * E;
+    const uint32_t begin = span * a.s.span;
+    const TG* grad = (const TG*)a.grad.data + col;
+    after_previous_launch();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
     const uint32_t n_valid = a.s.info[0];
     if (kKind == kSumRows && span0 == 0 && w == 0) *a.out_count = a.s.info[1];
-    if (w >= total) return;
-    const uint32_t q = vecs.div(w);
-    const uint32_t span = span0 + q, col = (w - q * vecs.divisor) * E;
-    const uint32_t begin = span * a.s.span;
-    if (begin >= n_valid) return;
+    if (w >= total || begin >= n_valid) return;
     const uint32_t end = begin + a.s.span < n_valid ? begin + a.s.span : n_valid;
-    const TG* grad = (const TG*)a.grad.data + col;
-    uint32_t key = a.s.key[begin];
-    bool whole = begin == 0 || a.s.key[begin - 1] != key;        // the current token begins in this span
+    uint32_t k[kBatch + 1];
+    k[0] = a.s.key[begin];
+    bool whole = begin == 0 || a.s.key[begin - 1] != k[0];       // the current token begins in this span
     uint32_t rank = a.s.span_rank[span] - (whole ? 0u : 1u);
     float* partial = a.partials + (uint64_t)span * 2 * a.partial_stride + col;
     float sum[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-    for (uint32_t i = begin; i < end; i += kSumBatch) {
-        uint32_t k[kSumBatch];
-        Pack<TG, E> x[kSumBatch];
+    bool ended = true;
+    for (uint32_t i = begin; i < end; i += kBatch) {
+        Pack<TG, E> x[kBatch];
+        Finish<kKind, TO, E> row[kBatch];
+        bool ends[kBatch];
 #pragma unroll
-        for (int j = 0; j < kSumBatch; ++j)
+        for (int j = 0; j < kBatch; ++j)
             if (i + j < end) {
-                k[j] = a.s.key[i + j];
+                k[j + 1] = i + j + 1 < n_valid ? a.s.key[i + j + 1] : 0xFFFFFFFFu;
                 x[j] = load_pack<TG, E>(grad + (uint64_t)a.s.pos[i + j] * a.grad.stride);
             }
+        bool here = whole;
 #pragma unroll
-        for (int j = 0; j < kSumBatch; ++j)
+        for (int j = 0; j < kBatch; ++j) {
+            ends[j] = i + j < end && k[j + 1] != k[j];
+            if (ends[j] && here) row[j].fetch(a, k[j], col);
+            here |= ends[j];
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
             if (i + j < end) {
-                if (k[j] != key) {
-                    if (whole) Finish<kKind, TO, E>::put(a, grad_scale, key, rank, col, sum);
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
+                if (ends[j]) {
+                    if (whole) row[j].put(a, grad_scale, k[j], rank, col, sum);
                     else store_pack<float, E>(partial, sum);     // the end of a token from an earlier span
-                    key = k[j];
                     ++rank;
                     whole = true;
 #pragma unroll
                     for (int e = 0; e < E; ++e) sum[e] = 0.0f;
                 }
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
+                ended = ends[j];
+                k[0] = k[j + 1];
             }
     }
-    const bool ends = end == n_valid || a.s.key[end] != key;
-    if (whole && ends) Finish<kKind, TO, E>::put(a, grad_scale, key, rank, col, sum);
-    else if (!whole) store_pack<float, E>(partial, sum);
-    else {
-        store_pack<float, E>(partial + a.partial_stride, sum);   // it goes on in the next span
-        if (col == 0) {
-            const uint32_t spans = (a.s.seg_start[rank + 1] - 1) / a.s.span - span;
-            const bool large = spans > kLongCrossing;
-            const uint32_t at = atomicAdd(a.s.info + (large ? 3 : 2), 1u);   // the list's order changes no sum
-            a.crossing[(large ? (a.n + a.s.span - 1) / a.s.span : 0u) + at] = make_uint2(span, rank);
-        }
+    if (ended) return;
+    // the token goes on in the next span; k[0] is its id
+    store_pack<float, E>(partial + (whole ? a.partial_stride : 0u), sum);
+    if (whole && col == 0) {
+        const uint32_t last = (a.s.seg_start[rank + 1] - 1) / a.s.span;
+        const bool large = last - span > kLongCrossing;
+        const uint32_t at = atomicAdd(a.s.info + (large ? 3 : 2), 1u);   // the list's order changes no sum
+        a.crossing[(large ? (a.n + a.s.span - 1) / a.s.span : 0u) + at] = make_uint4(span, rank, last, k[0]);
     }
 }
 
@@ -237,49 +245,49 @@ template <SumKind kKind, typename TO, int E>
 __global__ void __launch_bounds__(kCrossThreads)
 k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs) {
     __shared__ float join[kCrossWarps][32 * E + 1];
+    after_previous_launch();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
-    const uint32_t spans = (a.n + a.s.span - 1) / a.s.span;
     const uint64_t n_short = a.s.info[2], n_long = a.s.info[3];
     const uint64_t step = (uint64_t)2 * a.partial_stride;
     for (uint64_t w = (uint64_t)blockIdx.x * kCrossThreads + threadIdx.x; w < n_short * vecs.divisor;
          w += (uint64_t)gridDim.x * kCrossThreads) {
         const uint32_t q = (uint32_t)(w / vecs.divisor);
-        const uint2 c = a.crossing[q];
+        const uint4 c = a.crossing[q];
         const uint32_t col = (uint32_t)(w - (uint64_t)q * vecs.divisor) * E;
-        const uint32_t first = a.s.seg_start[c.y];
-        const uint32_t last = (a.s.seg_start[c.y + 1] - 1) / a.s.span;
-        const uint32_t key = a.s.key[first];
+        Finish<kKind, TO, E> row;
+        row.fetch(a, c.w, col);
         const float* at = a.partials + (uint64_t)c.x * step + col;
         const Pack<float, E> tail = load_pack<float, E>(at + a.partial_stride);
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = tail.v[e];
 #pragma unroll 4
-        for (uint32_t s = c.x + 1; s <= last; ++s) {
+        for (uint32_t s = c.x + 1; s <= c.z; ++s) {
             at += step;
             const Pack<float, E> x = load_pack<float, E>(at);
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] += x.v[e];
         }
-        Finish<kKind, TO, E>::put(a, grad_scale, key, c.y, col, sum);
+        row.put(a, grad_scale, c.w, c.y, col, sum);
     }
+    const uint32_t spans = (a.n + a.s.span - 1) / a.s.span;
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     for (uint64_t w = blockIdx.x; w < n_long * slabs; w += gridDim.x) {
         const uint32_t q = (uint32_t)(w / slabs);
-        const uint2 c = a.crossing[spans + q];
+        const uint4 c = a.crossing[spans + q];
         const uint32_t col = ((uint32_t)(w - (uint64_t)q * slabs) * 32 + lane) * E;
-        const uint32_t first = a.s.seg_start[c.y];
-        const uint32_t heads = (a.s.seg_start[c.y + 1] - 1) / a.s.span - c.x;   // partial rows after the first
-        const uint32_t key = a.s.key[first];
+        const uint32_t heads = c.z - c.x;              // partial rows after the first
         const uint32_t share = (heads + kCrossWarps - 1) / kCrossWarps;
         const uint32_t from = wid * share, to = from + share < heads ? from + share : heads;
+        Finish<kKind, TO, E> row;
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
         if (col < a.d) {
             const float* at = a.partials + (uint64_t)c.x * step + col;
             if (wid == 0) {
+                row.fetch(a, c.w, col);
                 const Pack<float, E> tail = load_pack<float, E>(at + a.partial_stride);
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] = tail.v[e];
@@ -299,7 +307,7 @@ k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs)
             for (int x = 1; x < kCrossWarps; ++x)
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] += join[x][lane * E + e];
-            Finish<kKind, TO, E>::put(a, grad_scale, key, c.y, col, sum);
+            row.put(a, grad_scale, c.w, c.y, col, sum);
         }
         __syncthreads();
     }
@@ -319,15 +327,17 @@ static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a) {
     const uint32_t most = kMaxItems / vecs.divisor;
     for (uint32_t span0 = 0; span0 < spans; span0 += most) {
         const uint32_t total = (spans - span0 < most ? spans - span0 : most) * vecs.divisor;
-        k_segment_sums<kKind, TG, TO, E><<<(total + kSumThreads - 1) / kSumThreads, kSumThreads, 0, stream>>>(a, span0, total, vecs);
+        const cudaError_t e = launch_early(k_segment_sums<kKind, TG, TO, E>, (total + kSumThreads - 1) / kSumThreads, kSumThreads,
+                                           stream, a, span0, total, vecs);
+        if (e != cudaSuccess) return e;
     }
     if (spans > 1) {
         const uint32_t slabs = (vecs.divisor + 31) / 32;
         uint64_t blocks = ((uint64_t)spans * vecs.divisor + kCrossThreads - 1) / kCrossThreads;
         if (blocks > 592) blocks = 592;
-        k_crossing_sums<kKind, TO, E><<<(uint32_t)blocks, kCrossThreads, 0, stream>>>(a, vecs, slabs);
+        return launch_early(k_crossing_sums<kKind, TO, E>, (uint32_t)blocks, kCrossThreads, stream, a, vecs, slabs);
     }
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs& a) {

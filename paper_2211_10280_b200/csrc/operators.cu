@@ -72,7 +72,7 @@ Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     l.pos = take((uint64_t)n * 4);
     l.seg_start = take(((uint64_t)(n < V ? n : V) + 1) * 4);
     l.span_rank = take((uint64_t)l.spans * 4);
-    l.crossing = take((uint64_t)l.spans * 2 * sizeof(uint2));
+    l.crossing = take((uint64_t)l.spans * 2 * sizeof(uint4));
     l.partials = take((uint64_t)l.spans * 2 * l.partial_stride * 4);
     const bool large = !sorts_in_one_launch(n);
     l.items_a = take(large ? (uint64_t)n * 8 : 0);
@@ -95,9 +95,21 @@ uint64_t workspace_bytes(uint32_t n, uint32_t V, uint32_t d) {
     }
 }
 
+int multiprocessors() {
+    static std::atomic<int> known[kMaxDevices];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return 0;
+    int sms = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (!sms) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+        if (device < kMaxDevices) known[device].store(sms, std::memory_order_relaxed);
+    }
+    return sms;
+}
+
 // The part all gradient calls share: checks, workspace, sort, sums.
 int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float scale, void* workspace, uint64_t bytes,
-                  void* stream, SumKind kind, SumArgs& a, uint32_t d) {
+                  void* stream, SumKind kind, SumArgs& a, uint32_t d, const ClearRows& clear = ClearRows{}) {
     TENSAIR_REQUIRE(std::isfinite(scale), "scale is not finite");
     const int rc = check_rows(grad, d, tokens->n == 0, "grad: NULL", "grad: type, width, stride or alignment");
     if (rc != TENSAIR_OK) return rc;
@@ -107,11 +119,9 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
         TENSAIR_REQUIRE(workspace && (uintptr_t)workspace % 256 == 0, "workspace: NULL or not aligned to 256 bytes");
         if (bytes < l.total) return refuse(TENSAIR_ENOMEM, "workspace: smaller than tensair_embedding_workspace_bytes says");
     }
-    if (a.clear_rows) {
-        const cudaError_t e = launch_clear_rows((cudaStream_t)stream, a.out, a.clear_rows, d);
-        if (e != cudaSuccess) return launched(e);
-    }
-    if (!n) return TENSAIR_OK;
+    const int sms = multiprocessors();
+    if (!sms) return refuse(TENSAIR_ECUDA, "no CUDA device is current");
+    if (!n) return clear.rows ? launched(launch_clear((cudaStream_t)stream, clear, sms)) : TENSAIR_OK;
     uint8_t* w = (uint8_t*)workspace;
     a.s = SortedTokens{(uint32_t*)(w + l.key), (uint32_t*)(w + l.pos), (uint32_t*)(w + l.seg_start),
                        (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info), l.span};
@@ -122,10 +132,10 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
     a.scale = scale;
     a.partials = (float*)(w + l.partials);
     a.partial_stride = l.partial_stride;
-    a.crossing = (uint2*)(w + l.crossing);
+    a.crossing = (uint4*)(w + l.crossing);
     const SortScratch scratch{(item_t*)(w + l.items_a), (item_t*)(w + l.items_b), (uint32_t*)(w + l.hist),
                               (uint32_t*)(w + l.tile_counts)};
-    cudaError_t e = launch_token_sort((cudaStream_t)stream, tokens_of(*tokens), a.s, scratch);
+    cudaError_t e = launch_token_sort((cudaStream_t)stream, tokens_of(*tokens), a.s, scratch, clear, sms);
     if (e == cudaSuccess) e = launch_segment_sums((cudaStream_t)stream, kind, a);
     return launched(e);
 }
@@ -153,18 +163,6 @@ AdamwConsts consts_of(const tensair_adamw& h) {
     c.keep = (float)(1 - h.lr * h.weight_decay);
     c.grad_scale = h.grad_scale;
     return c;
-}
-
-int multiprocessors() {
-    static std::atomic<int> known[kMaxDevices];
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return 0;
-    int sms = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
-    if (!sms) {
-        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
-        if (device < kMaxDevices) known[device].store(sms, std::memory_order_relaxed);
-    }
-    return sms;
 }
 
 }  // namespace
@@ -204,8 +202,9 @@ int tensair_embedding_gradient(const tensair_tokens* tokens, const tensair_rows*
     SumArgs a = {};
     a.out = view_of(*out);
     a.accumulate = accumulate != 0;
-    a.clear_rows = accumulate ? 0 : (uint32_t)tokens->V;
-    return gradient_call(tokens, grad, scale, workspace, workspace_bytes, stream, kSumTable, a, out->d);
+    const uint64_t b = type_bytes(out->type);
+    const ClearRows clear{(uint8_t*)out->data, out->stride * b, out->d * b, accumulate ? 0 : tokens->V};
+    return gradient_call(tokens, grad, scale, workspace, workspace_bytes, stream, kSumTable, a, out->d, clear);
 }
 
 int tensair_embedding_gradient_rows(const tensair_tokens* tokens, const tensair_rows* grad, float scale, uint32_t* row_ids,

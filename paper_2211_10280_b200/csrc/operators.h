@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "common.cuh"
 
 namespace tensair {
@@ -83,8 +85,16 @@ struct SortScratch {
     uint32_t* hist;
     uint32_t* tile_counts;
 };
+// Rows to set to zero, in bytes; rows 0: none.
+struct ClearRows {
+    uint8_t* data;
+    uint64_t stride, width, rows;
+};
 bool sorts_in_one_launch(uint32_t n);
-cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w);
+// Also clears `c`, beside the sort.
+cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w,
+                              const ClearRows& c, int sms);
+cudaError_t launch_clear(cudaStream_t stream, const ClearRows& c, int sms);
 
 // ---- embedding.cu
 struct RowsView {          // rows of d elements, `stride` elements apart
@@ -100,11 +110,11 @@ struct SumArgs {
     float scale;
     float* partials;       // [spans][2][partial_stride]
     uint32_t partial_stride;
-    uint2* crossing;       // [2][spans] (span, rank) of the segments that leave the span they begin in: short, then long
+    uint4* crossing;       // [2][spans] the segments that leave the span they begin in, short, then long:
+                           // (span, rank, last span, token)
     // where a finished row goes
     RowsView out;          // kSumTable: row `token`; kSumRows: row `rank`; kSumAdamw: the table of parameters
-    int accumulate;
-    uint32_t clear_rows;   // kSumTable: rows of `out` to set to zero first
+    int accumulate;        // kSumTable: add to what is there
     uint32_t* out_ids;     // kSumRows
     uint32_t* out_count;   // kSumRows
     float* m;
@@ -117,8 +127,24 @@ uint32_t span_length(uint32_t n, uint32_t d);
 uint32_t longest_with_shorter_spans(uint32_t n, uint32_t d);
 cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView& table, const RowsView& out, uint32_t d,
                           float scale);
-cudaError_t launch_clear_rows(cudaStream_t stream, const RowsView& rows, uint64_t count, uint32_t d);
 cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs& a);
+// A launch that may begin while the launch before it on the stream is still running: its blocks wait in
+// after_previous_launch() before they touch what that one writes.
+template <typename... Params, typename... Args>
+cudaError_t launch_early(void (*kernel)(Params...), uint32_t grid, uint32_t block, cudaStream_t stream, Args&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+__device__ __forceinline__ void after_previous_launch() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- adamw.cu
 struct AdamwTensor {
