@@ -501,7 +501,7 @@ typedef struct tensair_tokens {
     uint32_t reserved;
 } tensair_tokens;
 
-/* Rows of d elements, `stride` elements (>= d) apart. */
+/* Rows of d elements, `stride` elements (d .. 2^31 - 1) apart. */
 typedef struct tensair_rows {
     void* data;
     uint64_t stride;
@@ -574,7 +574,7 @@ typedef struct tensair_adamw_tensor {
 
 /*
  * One AdamW step of `count` tensors, at once: one launch for each combination of parameter and gradient type (and
- * for every 340 tensors).  tensors: host.  Moments in 8 bits start as zeros (codes and scales); a block whose largest
+ * for every 336 tensors).  tensors: host.  Moments in 8 bits start as zeros (codes and scales); a block whose largest
  * first moment is below 2^-110 is stored as zeros.  They are rounded stochastically to a neighbouring e4m3 value with random
  * bits that depend on (seed, step, the element's place in the list of tensors) alone; a positive v is never
  * stored as zero; a non-finite moment is stored as NaN and leaves the other elements of its block alone.

@@ -49,7 +49,8 @@ struct Batch {
     AdamwConsts c;
     uint32_t count, chunks;
     uint32_t chunk;        // elements of a chunk
-    uint32_t key0, key1, step_lo, step_hi;
+    uint32_t step_lo, step_hi;
+    PhiloxKeys keys;
     Entry t[kCount];
 };
 
@@ -93,46 +94,44 @@ __global__ void __launch_bounds__(kThreads)
 k_adamw(const __grid_constant__ Batch<kCount> b) {
     float grad_scale;
     if (!adamw_grad_scale(b.c, &grad_scale)) return;
-    for (uint32_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
-        const Entry& t = b.t[find_tensor(b, chunk)];
-        const uint64_t at = (uint64_t)(chunk - t.chunk0) * b.chunk;
-        if (t.head == kNoVector) {
-            const uint64_t end = at + b.chunk < t.n ? at + b.chunk : t.n;
-            for (uint64_t i = at + threadIdx.x; i < end; i += kThreads) update_one<TP, TG>(t, i, b.c, grad_scale);
-            continue;
-        }
-        if (at == 0 && threadIdx.x < t.head && threadIdx.x < t.n) update_one<TP, TG>(t, threadIdx.x, b.c, grad_scale);
-        const uint64_t end = t.head + at + b.chunk < t.n ? t.head + at + b.chunk : t.n;
-        for (uint64_t i0 = t.head + at + threadIdx.x * kVec; i0 < end; i0 += kThreads * kVec * kUnroll) {
-            Pack<TP, kVec> p[kUnroll];
-            Pack<TG, kVec> g[kUnroll];
-            Pack<float, kVec> m[kUnroll], v[kUnroll];
+    const Entry& t = b.t[find_tensor(b, blockIdx.x)];
+    const uint64_t at = (uint64_t)(blockIdx.x - t.chunk0) * b.chunk;
+    if (t.head == kNoVector) {
+        const uint64_t end = at + b.chunk < t.n ? at + b.chunk : t.n;
+        for (uint64_t i = at + threadIdx.x; i < end; i += kThreads) update_one<TP, TG>(t, i, b.c, grad_scale);
+        return;
+    }
+    if (at == 0 && threadIdx.x < t.head && threadIdx.x < t.n) update_one<TP, TG>(t, threadIdx.x, b.c, grad_scale);
+    const uint64_t end = t.head + at + b.chunk < t.n ? t.head + at + b.chunk : t.n;
+    for (uint64_t i0 = t.head + at + threadIdx.x * kVec; i0 < end; i0 += kThreads * kVec * kUnroll) {
+        Pack<TP, kVec> p[kUnroll];
+        Pack<TG, kVec> g[kUnroll];
+        Pack<float, kVec> m[kUnroll], v[kUnroll];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const uint64_t i = i0 + u * kThreads * kVec;
-                if (i + kVec <= end) {
-                    p[u] = load_pack<TP, kVec>((TP*)t.p + i);
-                    g[u] = load_pack<TG, kVec>((const TG*)t.g + i);
-                    m[u] = load_pack<float, kVec>((float*)t.m + i);
-                    v[u] = load_pack<float, kVec>((float*)t.v + i);
-                }
+        for (int u = 0; u < kUnroll; ++u) {
+            const uint64_t i = i0 + u * kThreads * kVec;
+            if (i + kVec <= end) {
+                p[u] = load_pack<TP, kVec>((TP*)t.p + i);
+                g[u] = load_pack<TG, kVec>((const TG*)t.g + i);
+                m[u] = load_pack<float, kVec>((float*)t.m + i);
+                v[u] = load_pack<float, kVec>((float*)t.v + i);
             }
+        }
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const uint64_t i = i0 + u * kThreads * kVec;
-                if (i + kVec <= end) {
-                    float y[kVec];
+        for (int u = 0; u < kUnroll; ++u) {
+            const uint64_t i = i0 + u * kThreads * kVec;
+            if (i + kVec <= end) {
+                float y[kVec];
 #pragma unroll
-                    for (int e = 0; e < kVec; ++e)
-                        y[e] = adamw_update(to_float(p[u].v[e]), to_float(g[u].v[e]) * grad_scale, m[u].v[e], v[u].v[e], b.c,
-                                            t.step_size, t.keep);
-                    store_pack<TP, kVec>((TP*)t.p + i, y);
-                    store_pack<float, kVec>((float*)t.m + i, m[u].v);
-                    store_pack<float, kVec>((float*)t.v + i, v[u].v);
-                    if (t.copy) store_copies<kVec>(t, i, y);
-                } else {
-                    for (uint64_t j = i; j < end; ++j) update_one<TP, TG>(t, j, b.c, grad_scale);
-                }
+                for (int e = 0; e < kVec; ++e)
+                    y[e] = adamw_update(to_float(p[u].v[e]), to_float(g[u].v[e]) * grad_scale, m[u].v[e], v[u].v[e], b.c,
+                                        t.step_size, t.keep);
+                store_pack<TP, kVec>((TP*)t.p + i, y);
+                store_pack<float, kVec>((float*)t.m + i, m[u].v);
+                store_pack<float, kVec>((float*)t.v + i, v[u].v);
+                if (t.copy) store_copies<kVec>(t, i, y);
+            } else {
+                for (uint64_t j = i; j < end; ++j) update_one<TP, TG>(t, j, b.c, grad_scale);
             }
         }
     }
@@ -141,53 +140,99 @@ k_adamw(const __grid_constant__ Batch<kCount> b) {
 // ------------------------------------------------------------------ moments in 8 bits
 constexpr int kLaneElems = kBlock / 32;  // 8
 
-__device__ __forceinline__ void decode8(uint2 codes, float scale, float (&x)[kLaneElems]) {
+// Two floats in one register pair: the packed instructions do both in one issue slot, each rounded as the single ones.
+struct Two {
+    unsigned long long bits;
+    __device__ __forceinline__ Two() {}
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+    __device__ __forceinline__ float2 floats() const {
+        float2 f;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(bits));
+        return f;
+    }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+
+__device__ __forceinline__ Two decode8(uint16_t codes, Two scale) {
+    uint32_t halves;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(halves) : "h"(codes));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&halves));
+    return Two(f.x, f.y) * scale;
+}
+__device__ __forceinline__ uint32_t encode8(float low, float high) {
+    uint16_t c;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(high), "f"(low));
+    return c;
+}
+__device__ __forceinline__ float approximate_reciprocal(float x) {     // used in the update alone
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// x, already divided by the scale, cut to 3 fraction bits after adding a uniform part of the last place kept (`bits20`: 16 random
+// bits above four zeros, and 8, the half of their last place): for values of e4m3's normal range, where the conversion
+// that follows is exact.
+__device__ __forceinline__ float cut8(float x, uint32_t bits20) {
+    return __uint_as_float((__float_as_uint(x) + bits20 + 8u) & 0xFFF00000u);
+}
+
+// Smallest and largest bit pattern of the magnitudes of a lane's eight values (kPositive: their sign bits are 0 but for NaNs).
+template <bool kPositive>
+__device__ __forceinline__ void range8(const Two (&x)[4], uint32_t* low, uint32_t* top) {
+    *low = 0xFFFFFFFFu;
+    *top = 0;
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-        const uint16_t two = (uint16_t)((h < 2 ? codes.x : codes.y) >> (16 * (h & 1)));
-        uint32_t halves;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(halves) : "h"(two));
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&halves));
-        x[2 * h] = f.x * scale;
-        x[2 * h + 1] = f.y * scale;
+        const float2 f = x[h].floats();
+        const uint32_t a = kPositive ? __float_as_uint(f.x) : magnitude(f.x), b = kPositive ? __float_as_uint(f.y) : magnitude(f.y);
+        *low = __vimin3_u32(*low, a, b);
+        *top = __vimax3_u32(*top, a, b);
     }
+    if (kPositive) *top &= 0x7FFFFFFFu;
 }
 
-// |x| / scale to e4m3, the sign taken from x; bits16: 16 random bits in the low half.
-// Values of e4m3's normal range are cut to 3 fraction bits after adding a uniform part of the last place.
-__device__ __forceinline__ float round8(float x, float inv_scale, uint32_t bits16, bool keep_positive) {
-    float size = fabsf(x) * inv_scale;
-    if (keep_positive && x > 0.0f) size = fmaxf(size, 0x1p-9f);
-    const float near = __uint_as_float((__float_as_uint(size) + (bits16 << 4) + 8u) & 0xFFF00000u);
-    const float y = size < 0x1p-6f ? size : near;
-    return __uint_as_float(__float_as_uint(y) | (__float_as_uint(x) & 0x80000000u));
+// Square roots, correctly rounded like __fsqrt_rn, of values in [2^-96, 2^128): Newton's step from the approximate reciprocal root with
+// the residual x - y^2 formed exactly by a fused multiply-add (Markstein, IBM J. Res. Dev. 34, 1990).  Two at a time.
+__device__ __forceinline__ Two roots(Two x) {
+    const float2 f = x.floats();
+    float r0, r1;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(f.x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(f.y));
+    const Two r(r0, r1), y = x * r;
+    return fma2(fma2(y * Two(-1.0f), y, x), r * Two(0.5f), y);
 }
 
-__device__ __forceinline__ uint2 encode8(const float (&y)[kLaneElems]) {
-    uint32_t two[4];
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        uint16_t c;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(y[2 * h + 1]), "f"(y[2 * h]));
-        two[h] = c;
-    }
-    return make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
-}
-
-// Stores one moment of a warp's block: the scale (lane 0) and this lane's codes.
-__device__ __forceinline__ uint2 store8(const float (&x)[kLaneElems], const uint32_t (&words)[4], bool keep_positive, float* scale_out,
+// One moment of a warp's block to e4m3: this lane's codes, and the scale by lane 0.  low and top: range8 of x.
+template <bool kRoot>
+__device__ __forceinline__ uint2 store8(const Two (&x)[4], uint32_t low, uint32_t top, const uint32_t (&bits20)[8], float* scale_out,
                                         uint32_t lane) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < kLaneElems; ++e) top = max(top, __float_as_uint(x[e]) & 0x7FFFFFFFu);
     top = __reduce_max_sync(0xFFFFFFFFu, top);
-    const bool finite = top < kInfBits;      // of the whole block
+    const bool finite = top < kInfBits;          // of the whole block
     if (!finite) {
         top = 0;
 #pragma unroll
-        for (int e = 0; e < kLaneElems; ++e) {
-            const uint32_t bits = __float_as_uint(x[e]) & 0x7FFFFFFFu;
-            if (bits < kInfBits) top = max(top, bits);
+        for (int h = 0; h < 4; ++h) {
+            const float2 f = x[h].floats();
+            const uint32_t a = magnitude(f.x), b = magnitude(f.y);
+            if (a < kInfBits) top = max(top, a);
+            if (b < kInfBits) top = max(top, b);
         }
         top = __reduce_max_sync(0xFFFFFFFFu, top);
     }
@@ -195,96 +240,162 @@ __device__ __forceinline__ uint2 store8(const float (&x)[kLaneElems], const uint
     const bool any = largest >= kTiny;
     const float inv = any ? __fmul_rn(__frcp_rn(largest), kTop) : 0.0f;
     if (lane == 0) *scale_out = any ? __fmul_rn(largest, 1.0f / kTop) : 0.0f;
-    float y[kLaneElems];
+    uint32_t code[4];
+    // Values below e4m3's normal range are rare in a block (2^-14.8 of its largest): one vote spares the rest the checks.
+    // (A product's rounding keeps the order, so the smallest speaks for all.)
+    if (finite && !__any_sync(0xFFFFFFFFu, __fmul_rn(__uint_as_float(low), inv) < 0x1p-6f)) {
 #pragma unroll
-    for (int e = 0; e < kLaneElems; ++e)
-        y[e] = round8(x[e], inv, e & 1 ? words[e >> 1] >> 16 : words[e >> 1] & 0xFFFFu, keep_positive);
-    if (!finite) {
+        for (int h = 0; h < 4; ++h) {
+            const float2 y = (x[h] * Two(inv)).floats();
+            code[h] = encode8(cut8(y.x, bits20[2 * h]), cut8(y.y, bits20[2 * h + 1]));
+        }
+    } else {
 #pragma unroll
-        for (int e = 0; e < kLaneElems; ++e)
-            if ((__float_as_uint(x[e]) & 0x7FFFFFFFu) >= kInfBits) y[e] = __uint_as_float(0x7FC00000u);
+        for (int h = 0; h < 4; ++h) {
+            const float2 g = x[h].floats(), y = (x[h] * Two(inv)).floats();
+            auto one = [&](float y, float source, uint32_t d) {
+                if (magnitude(source) >= kInfBits) return __uint_as_float(0x7FC00000u);
+                if (kRoot && source > 0.0f) y = fmaxf(y, 0x1p-9f);      // never stored as zero
+                return fabsf(y) < 0x1p-6f ? y : cut8(y, d);
+            };
+            code[h] = encode8(one(y.x, g.x, bits20[2 * h]), one(y.y, g.y, bits20[2 * h + 1]));
+        }
     }
-    return encode8(y);
+    return make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
+}
+
+template <typename TP>
+__device__ __forceinline__ void load_lane(const TP* at, float (&p)[kLaneElems]) {
+    if constexpr (sizeof(TP) == 4) load_eight(at, p);
+    else {
+        const Pack<TP, kLaneElems> x = load_pack<TP, kLaneElems>(at);
+#pragma unroll
+        for (int e = 0; e < kLaneElems; ++e) p[e] = to_float(x.v[e]);
+    }
+}
+template <typename TP>
+__device__ __forceinline__ void store_lane(TP* at, const float (&p)[kLaneElems]) {
+    if constexpr (sizeof(TP) == 4) store_eight(at, p);
+    else store_pack<TP, kLaneElems>(at, p);
+}
+
+// One block of 256 elements, eight to a lane: parameter, moments and codes to their new values.  The caller stores p, mc and vc.
+template <int kCount>
+__device__ __forceinline__ void step8(const Batch<kCount>& b, const Entry& t, uint64_t block, uint32_t lane, float grad_scale,
+                                      float (&p)[kLaneElems], Two (&g)[4], Two m_scale, Two v_scale, uint2& mc, uint2& vc) {
+    Two m[4], v[4];
+                const uint64_t group = (t.block0 + block) * 32 + lane;
+                const Philox4 r = philox4x32_10(Philox4{(uint32_t)group, (uint32_t)(group >> 32), b.step_lo, kTagRounding | b.step_hi}, b.keys);
+                const uint32_t words[4] = {r.x, r.y, r.z, r.w};
+                uint32_t bits20[kLaneElems];
+    #pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    bits20[2 * h] = words[h] << 4 & 0xFFFF0u;
+                    bits20[2 * h + 1] = words[h] >> 12 & 0xFFFF0u;
+                }
+    #pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    // every product and sum rounded by itself, as a program of separate operations has them: what is
+                    // stored then does not depend on which of them a compiler contracts
+                    m[h] = decode8((uint16_t)((h < 2 ? mc.x : mc.y) >> (16 * (h & 1))), m_scale);
+                    v[h] = decode8((uint16_t)((h < 2 ? vc.x : vc.y) >> (16 * (h & 1))), v_scale);
+                    g[h] = g[h] * Two(grad_scale);
+                    m[h] = m[h] * Two(b.c.beta1) + g[h] * Two(b.c.rest1);
+                    v[h] = v[h] * v[h] * Two(b.c.beta2) + g[h] * g[h] * Two(b.c.rest2);
+                }
+                uint32_t m_low, m_top, v_low, v_top;
+                range8<false>(m, &m_low, &m_top);
+                range8<true>(v, &v_low, &v_top);
+                // from here on v is its square root
+                if (__all_sync(0xFFFFFFFFu, v_low >= 0x0F800000u && v_top < kInfBits)) {      // 2^-96
+    #pragma unroll
+                    for (int h = 0; h < 4; ++h) v[h] = roots(v[h]);
+                } else {
+    #pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const float2 f = v[h].floats();
+                        v[h] = Two(__fsqrt_rn(f.x), __fsqrt_rn(f.y));
+                    }
+                }
+                range8<true>(v, &v_low, &v_top);
+    #pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const float2 low = fma2(v[h], Two(b.c.inv_root2), Two(b.c.eps)).floats();
+                    const Two change = m[h] * Two(approximate_reciprocal(low.x), approximate_reciprocal(low.y));
+                    const float2 y = fma2(change, Two(-t.step_size), Two(p[2 * h], p[2 * h + 1]) * Two(t.keep)).floats();
+                    p[2 * h] = y.x;
+                    p[2 * h + 1] = y.y;
+                }
+    mc = store8<false>(m, m_low, m_top, bits20, t.m_scale + block, lane);
+    vc = store8<true>(v, v_low, v_top, bits20, t.v_scale + block, lane);
 }
 
 template <int kCount, typename TP, typename TG>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 k_adamw8(const __grid_constant__ Batch<kCount> b) {
     float grad_scale;
     if (!adamw_grad_scale(b.c, &grad_scale)) return;
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    for (uint32_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
-        const Entry& t = b.t[find_tensor(b, chunk)];
-        const uint64_t at = (uint64_t)(chunk - t.chunk0) * b.chunk;
-        const uint64_t end = at + b.chunk < t.n ? at + b.chunk : t.n;
-        for (uint64_t base = at + wid * kBlock; base < end; base += kThreads / 32 * kBlock) {
-            const uint64_t i = base + lane * kLaneElems, block = base / kBlock;
-            const bool vector = t.head != kNoVector && i + kLaneElems <= t.n;
-            float p[kLaneElems], g[kLaneElems], m[kLaneElems], v[kLaneElems];
-            const float m_scale = t.m_scale[block], v_scale = t.v_scale[block];
-            uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
-            if (vector) {
-                const Pack<TP, kLaneElems> pp = load_pack<TP, kLaneElems>((TP*)t.p + i);
-                const Pack<TG, kLaneElems> gg = load_pack<TG, kLaneElems>((const TG*)t.g + i);
-                mc = *reinterpret_cast<const uint2*>((uint8_t*)t.m + i);
-                vc = *reinterpret_cast<const uint2*>((uint8_t*)t.v + i);
+    const uint32_t tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const Entry& t = b.t[find_tensor(b, blockIdx.x)];
+    const uint64_t at = (uint64_t)(blockIdx.x - t.chunk0) * b.chunk;
+    const uint64_t end = at + b.chunk < t.n ? at + b.chunk : t.n;
+    constexpr uint32_t kStep = kThreads / 32 * kBlock;
+    // ---- whole blocks of aligned tensors
+    const uint64_t whole = t.head == kNoVector ? at : end / kBlock * kBlock;
+    uint64_t base = at + wid * kBlock;
+    for (; base < whole; base += kStep) {
+        const uint64_t i = base + lane * kLaneElems, block = base / kBlock;
+        const float m_scale = t.m_scale[block], v_scale = t.v_scale[block];
+        float p[kLaneElems];
+        load_lane<TP>((const TP*)t.p + i, p);
+        const Pack<TG, kLaneElems> gg = load_pack<TG, kLaneElems>((const TG*)t.g + i);
+        uint2 mc = *reinterpret_cast<const uint2*>((const uint8_t*)t.m + i), vc = *reinterpret_cast<const uint2*>((const uint8_t*)t.v + i);
+        Two g[4];
 #pragma unroll
-                for (int e = 0; e < kLaneElems; ++e) {
-                    p[e] = to_float(pp.v[e]);
-                    g[e] = to_float(gg.v[e]) * grad_scale;
-                }
-            } else {
+        for (int h = 0; h < 4; ++h) g[h] = Two(to_float(gg.v[2 * h]), to_float(gg.v[2 * h + 1]));
+        step8(b, t, block, lane, grad_scale, p, g, Two(m_scale), Two(v_scale), mc, vc);
+        store_lane<TP>((TP*)t.p + i, p);
+        if (t.copy) store_copies<kLaneElems>(t, i, p);
+        *reinterpret_cast<uint2*>((uint8_t*)t.m + i) = mc;
+        *reinterpret_cast<uint2*>((uint8_t*)t.v + i) = vc;
+    }
+    // ---- a tensor's last, incomplete block, and tensors that are not aligned
+    for (base = whole + (t.head == kNoVector ? wid * kBlock : 0); base < end; base += kStep) {
+        if (t.head != kNoVector && wid) break;
+        const uint64_t i = base + lane * kLaneElems, block = base / kBlock;
+        const Two m_scale(t.m_scale[block]), v_scale(t.v_scale[block]);
+        uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
+        float p[kLaneElems], y[kLaneElems];
+        Two g[4];
 #pragma unroll
-                for (int e = 0; e < kLaneElems; ++e) {
-                    const bool in = i + e < t.n;
-                    p[e] = in ? to_float(((TP*)t.p)[i + e]) : 0.0f;
-                    g[e] = in ? to_float(((const TG*)t.g)[i + e]) * grad_scale : 0.0f;
-                    const uint32_t cm = in ? ((uint8_t*)t.m)[i + e] : 0u, cv = in ? ((uint8_t*)t.v)[i + e] : 0u;
-                    if (e < 4) { mc.x |= cm << (8 * e); vc.x |= cv << (8 * e); }
-                    else { mc.y |= cm << (8 * (e - 4)); vc.y |= cv << (8 * (e - 4)); }
-                }
-            }
-            decode8(mc, m_scale, m);
-            decode8(vc, v_scale, v);
-#pragma unroll
-            for (int e = 0; e < kLaneElems; ++e) {
-                // every product and sum rounded by itself, as a program of separate operations has them: what is
-                // stored then does not depend on which of them a compiler contracts
-                m[e] = __fadd_rn(__fmul_rn(m[e], b.c.beta1), __fmul_rn(g[e], b.c.rest1));
-                v[e] = __fadd_rn(__fmul_rn(__fmul_rn(v[e], v[e]), b.c.beta2), __fmul_rn(__fmul_rn(g[e], g[e]), b.c.rest2));
-                v[e] = __fsqrt_rn(v[e]);     // from here on the square root
-                p[e] = fmaf(p[e], t.keep, -t.step_size * (m[e] / fmaf(v[e], b.c.inv_root2, b.c.eps)));
-            }
-            const uint64_t group = (t.block0 + block) * 32 + lane;
-            const Philox4 r = philox4x32_10(Philox4{(uint32_t)group, (uint32_t)(group >> 32), b.step_lo, kTagRounding | b.step_hi},
-                                            b.key0, b.key1);
-            const uint32_t words[4] = {r.x, r.y, r.z, r.w};
-            mc = store8(m, words, false, t.m_scale + block, lane);
-            vc = store8(v, words, true, t.v_scale + block, lane);
-            if (vector) {
-                store_pack<TP, kLaneElems>((TP*)t.p + i, p);
-                *reinterpret_cast<uint2*>((uint8_t*)t.m + i) = mc;
-                *reinterpret_cast<uint2*>((uint8_t*)t.v + i) = vc;
-                if (t.copy) store_copies<kLaneElems>(t, i, p);
-            } else {
-#pragma unroll
-                for (int e = 0; e < kLaneElems; ++e)
-                    if (i + e < t.n) {
-                        ((TP*)t.p)[i + e] = from_float<TP>(p[e]);
-                        ((uint8_t*)t.m)[i + e] = (uint8_t)((e < 4 ? mc.x : mc.y) >> (8 * (e & 3)));
-                        ((uint8_t*)t.v)[i + e] = (uint8_t)((e < 4 ? vc.x : vc.y) >> (8 * (e & 3)));
-                        if (t.copy) store_copy(t, i + e, p[e]);
-                    }
-            }
+        for (int e = 0; e < kLaneElems; ++e) {
+            const bool in = i + e < t.n;
+            p[e] = in ? to_float(((TP*)t.p)[i + e]) : 0.0f;
+            y[e] = in ? to_float(((const TG*)t.g)[i + e]) : 0.0f;
+            const uint32_t cm = in ? ((uint8_t*)t.m)[i + e] : 0u, cv = in ? ((uint8_t*)t.v)[i + e] : 0u;
+            if (e < 4) { mc.x |= cm << (8 * e); vc.x |= cv << (8 * e); }
+            else { mc.y |= cm << (8 * (e - 4)); vc.y |= cv << (8 * (e - 4)); }
         }
+#pragma unroll
+        for (int h = 0; h < 4; ++h) g[h] = Two(y[2 * h], y[2 * h + 1]);
+        step8(b, t, block, lane, grad_scale, p, g, m_scale, v_scale, mc, vc);
+#pragma unroll
+        for (int e = 0; e < kLaneElems; ++e)
+            if (i + e < t.n) {
+                ((TP*)t.p)[i + e] = from_float<TP>(p[e]);
+                ((uint8_t*)t.m)[i + e] = (uint8_t)((e < 4 ? mc.x : mc.y) >> (8 * (e & 3)));
+                ((uint8_t*)t.v)[i + e] = (uint8_t)((e < 4 ? vc.x : vc.y) >> (8 * (e & 3)));
+                if (t.copy) store_copy(t, i + e, p[e]);
+            }
     }
 }
 
 // ------------------------------------------------------------------ host
 // Elements to leave out so that every array of the tensor is aligned for vectors of `vec` elements (or 16 bytes).
 uint32_t aligned_head(const AdamwTensor& t, int bits, uint32_t vec) {
-    auto aligned = [vec](const void* p, uint64_t elem, uint32_t h) {
-        const uint64_t bytes = elem * vec > 16 ? 16 : elem * vec;
+    // vectors of fp32 parameters with 8-bit moments are moved in one 32-byte access, all others in up to 16 bytes
+    auto aligned = [&](const void* p, uint64_t elem, uint32_t h) {
+        const uint64_t most = bits == 8 && p == t.param ? 32 : 16, bytes = elem * vec > most ? most : elem * vec;
         return ((uintptr_t)p + h * elem) % bytes == 0;
     };
     const uint32_t most = bits == 8 ? 1 : vec;     // the blocks of the 8-bit moments begin at the first element
@@ -297,9 +408,8 @@ uint32_t aligned_head(const AdamwTensor& t, int bits, uint32_t vec) {
 
 template <int kCount, typename TP, typename TG>
 cudaError_t launch_batch(cudaStream_t stream, const Batch<kCount>& b, int bits, int sms) {
-    const uint32_t grid = b.chunks < (uint32_t)sms * 16 ? b.chunks : (uint32_t)sms * 16;
-    if (bits == 8) k_adamw8<kCount, TP, TG><<<grid, kThreads, 0, stream>>>(b);
-    else k_adamw<kCount, TP, TG><<<grid, kThreads, 0, stream>>>(b);
+    if (bits == 8) k_adamw8<kCount, TP, TG><<<b.chunks, kThreads, 0, stream>>>(b);
+    else k_adamw<kCount, TP, TG><<<b.chunks, kThreads, 0, stream>>>(b);
     return cudaGetLastError();
 }
 template <int kCount, typename TP>
@@ -350,7 +460,11 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
             for (uint32_t i = 0; i < count; ++i)
                 if (tensors[i].param_type == pt && tensors[i].grad_type == gt) total += tensors[i].n;
             if (!total) continue;
-            b.chunk = total >= (uint64_t)sms * 8 * 4096 ? 4096 : 2048;
+// A block finds its tensor once per chunk.  With 32-bit moments short chunks are best (96 M elements: 395 us with 2,048,
+            // 403 with 4,096, 410 with 8,192: the blocks that run together stay close together in memory); with 8-bit ones the search
+            // is worth sharing (128 M: 442 us with 4,096, 401 with 16,384), as long as all multiprocessors have chunks.
+            b.chunk = bits == 8 ? 16384 : 2048;
+            while (b.chunk > 2048 && total < (uint64_t)sms * 8 * b.chunk) b.chunk /= 2;
             for (uint32_t next = 0; next < count;) {
                 const cudaError_t e = launch_some<kCount>(stream, tensors, count, &next, pt, gt, bits, b, sms);
                 if (e != cudaSuccess) return e;
@@ -359,7 +473,7 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
     return cudaSuccess;
 }
 
-constexpr int kFew = 16, kMany = 340;
+constexpr int kFew = 16, kMany = 336;
 
 }  // namespace
 
@@ -368,8 +482,7 @@ cudaError_t launch_adamw(cudaStream_t stream, const AdamwTensor* tensors, uint32
     static_assert(sizeof(Batch<kMany>) <= 32764, "a kernel's arguments hold at most 32,764 bytes");
     auto set = [&](auto& b) {
         b.c = c;
-        b.key0 = (uint32_t)seed;
-        b.key1 = (uint32_t)(seed >> 32);
+        b.keys = PhiloxKeys(seed);
         b.step_lo = (uint32_t)step;
         b.step_hi = (uint32_t)(step >> 32) & 0xFFFFFFu;
     };

@@ -6,11 +6,18 @@
 
 namespace tensair {
 
+// Square root and quotient go into the update alone, where the approximate instructions' errors (2^-23 and 2 units in the
+// last place) are those of a rounding or two; the exact ones are ten instructions each.
+__device__ __forceinline__ float approximate_root(float x) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float adamw_update(float p, float g, float& m, float& v, const AdamwConsts& c, float step_size,
                                               float keep) {
     m = fmaf(c.beta1, m, c.rest1 * g);
     v = fmaf(c.beta2, v, c.rest2 * g * g);
-    return fmaf(p, keep, -step_size * (m / fmaf(sqrtf(v), c.inv_root2, c.eps)));
+    return fmaf(p, keep, -step_size * __fdividef(m, fmaf(approximate_root(v), c.inv_root2, c.eps)));
 }
 
 // The factor on the gradients, read on the device.  false: it is not finite and the step is left out.

@@ -1,12 +1,12 @@
 // Embedding lookup with scaling, and the sums by token that its gradient and the AdamW step of the touched rows are
 // made of.
 //
-// Sums.  The batch's positions are sorted by token (token_sort.cu).  The sorted positions are cut into spans of equal
-// length; one thread takes one span and one vector of columns, walks the span's gradient rows with several loads in
-// flight and adds them up in fp32, in sorted order.  A token whose positions lie inside one span is finished there:
-// its row goes straight to where it belongs (the gradient table, the message, or through the AdamW update).  A token
-// that crosses spans leaves one partial row per span, and a second launch adds those up in span order.  Every thread
-// has the same number of rows to read whatever the tokens' frequencies are, and no sum depends on timing.
+// Sums.  The batch's positions are sorted by token (token_sort.cu).  A block takes 64 sorted positions (and a slab of the
+// columns), lists the tokens that begin there in shared memory, and each of its threads then works through (token,
+// vector of columns) pairs: it adds up the token's gradient rows in fp32, in sorted order, and puts the finished row where
+// it belongs: the gradient table, the message, or through the AdamW update.  A token with more than 16 positions is added
+// up in pieces, one partial row per window of 16, and a second launch joins those in window order: no thread has more than
+// 16 rows to add, whatever the tokens' frequencies are, and no sum depends on timing.
 #include "adamw.cuh"
 #include "operators.h"
 
@@ -120,9 +120,11 @@ namespace {
 
 // ------------------------------------------------------------------ sums by token
 constexpr int kSumThreads = 256;
-constexpr int kCrossThreads = 512;
-constexpr int kCrossWarps = kCrossThreads / 32;
-constexpr uint32_t kLongCrossing = 16; // a segment over more spans than this is added up by a whole block
+constexpr uint32_t kMaxParts = kSpan;  // every part begins at a position of its own
+enum SumPart : uint32_t { kWholeToken, kPiece0, kPiece1 };   // pieces: see SumArgs::partials
+constexpr uint32_t kSumBlocks = 4;   // blocks per multiprocessor aimed at
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWarps = kJoinThreads / 32;
 
 // What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
 // several tokens' reads are in flight before the first is needed; put() joins and stores.
@@ -169,117 +171,125 @@ struct Finish {
 
 template <SumKind kKind, typename TG, typename TO, int E>
 __global__ void __launch_bounds__(kSumThreads)
-k_segment_sums(const __grid_constant__ SumArgs a, uint32_t span0, uint32_t total, FastDiv vecs) {
-    constexpr int kBatch = kKind == kSumRows ? 8 : 4;   // gradient vectors in flight; fewer where finished rows bring reads of their own
+k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
+    // gradient vectors in flight per thread; few registers, and so many threads, are worth more where a vector or a finished
+    // row takes many
+    constexpr int kSumBatch = kKind == kSumAdamw || E == 8 ? 2 : 4;
+    // What the block adds up, in order: (first position | rows << 8 | SumPart << 16 | piece's window << 24, token, rank).
+    // No large shared arrays: the reads in flight need the level-1 cache, which shares its memory with them.
+    __shared__ __align__(16) uint4 parts[kMaxParts];
+    __shared__ uint32_t pos[kSpan + kWindow], head_masks[kSpan / 32], part_masks[kSpan / 32];
     let_next_launch_begin();
-    const uint32_t w = blockIdx.x * kSumThreads + threadIdx.x;
-    const uint32_t q = vecs.div(w);
-    const uint32_t span = span0 + q, col = (w - q * vecs.divisor) * E;
-    const uint32_t begin = span * a.s.span;
-    const TG* grad = (const TG*)a.grad.data + col;
+    const uint32_t tid = threadIdx.x, begin = blockIdx.x * kSpan;
+    const uint32_t vec0 = blockIdx.y * slab_vecs, all_vecs = a.d / E;
+    const uint32_t vecs = all_vecs - vec0 < slab_vecs ? all_vecs - vec0 : slab_vecs;
     after_previous_launch();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
     const uint32_t n_valid = a.s.info[0];
-    if (kKind == kSumRows && span0 == 0 && w == 0) *a.out_count = a.s.info[1];
-    if (w >= total || begin >= n_valid) return;
-    const uint32_t end = begin + a.s.span < n_valid ? begin + a.s.span : n_valid;
-    uint32_t k[kBatch + 1];
-    k[0] = a.s.key[begin];
-    bool whole = begin == 0 || a.s.key[begin - 1] != k[0];       // the current token begins in this span
-    uint32_t rank = a.s.span_rank[span] - (whole ? 0u : 1u);
-    float* partial = a.partials + (uint64_t)span * 2 * a.partial_stride + col;
-    float sum[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-    bool ended = true;
-    for (uint32_t i = begin; i < end; i += kBatch) {
-        Pack<TG, E> x[kBatch];
-        Finish<kKind, TO, E> row[kBatch];
-        bool ends[kBatch];
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j)
-            if (i + j < end) {
-                k[j + 1] = i + j + 1 < n_valid ? a.s.key[i + j + 1] : 0xFFFFFFFFu;
-                x[j] = load_pack<TG, E>(grad + (uint64_t)a.s.pos[i + j] * a.grad.stride);
-            }
-        bool here = whole;
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            ends[j] = i + j < end && k[j + 1] != k[j];
-            if (ends[j] && here) row[j].fetch(a, k[j], col);
-            here |= ends[j];
+    if (kKind == kSumRows && begin == 0 && vec0 == 0 && tid == 0) *a.out_count = a.s.info[1];
+    if (begin >= n_valid) return;
+    const uint32_t before = a.s.span_rank[blockIdx.x];           // tokens that begin before the span
+    if (tid < kSpan + kWindow && begin + tid < n_valid) pos[tid] = a.s.pos[begin + tid];
+    const uint32_t at = begin + tid;
+    const bool mine = tid < kSpan && at < n_valid;               // this thread has a position of the span
+    uint32_t key = 0;
+    bool head = false;
+    if (tid < kSpan) {
+        if (mine) {
+            key = a.s.key[at];
+            head = at == 0 || a.s.key[at - 1] != key;
         }
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j)
-            if (i + j < end) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
-                if (ends[j]) {
-                    if (whole) row[j].put(a, grad_scale, k[j], rank, col, sum);
-                    else store_pack<float, E>(partial, sum);     // the end of a token from an earlier span
-                    ++rank;
-                    whole = true;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-                }
-                ended = ends[j];
-                k[0] = k[j + 1];
-            }
+        const uint32_t heads = __ballot_sync(0xFFFFFFFFu, head);
+        if (tid % 32 == 0) head_masks[tid / 32] = heads;
     }
-    if (ended) return;
-    // the token goes on in the next span; k[0] is its id
-    store_pack<float, E>(partial + (whole ? a.partial_stride : 0u), sum);
-    if (whole && col == 0) {
-        const uint32_t last = (a.s.seg_start[rank + 1] - 1) / a.s.span;
-        const bool large = last - span > kLongCrossing;
-        const uint32_t at = atomicAdd(a.s.info + (large ? 3 : 2), 1u);   // the list's order changes no sum
-        a.crossing[(large ? (a.n + a.s.span - 1) / a.s.span : 0u) + at] = make_uint4(span, rank, last, k[0]);
+    __syncthreads();
+    // A token with up to kWindow positions is one part, in the span it begins in.  A larger one has a part, a piece, in
+    // every window of kWindow positions that it reaches into.
+    bool part = false;
+    uint32_t first = tid, rows = 0, kind = kWholeToken, rank = 0;
+    if (tid < kSpan) {
+        if (mine) {
+            const unsigned long long heads = (unsigned long long)head_masks[1] << 32 | head_masks[0];
+            rank = before + __popcll(heads & (~0ull >> (63 - tid))) - 1;
+            const uint32_t start = a.s.seg_start[rank], end = a.s.seg_start[rank + 1];
+            const bool large = end - start > kWindow;
+            part = head || (large && tid % kWindow == 0);
+            rows = end - at;
+            if (large) {
+                const uint32_t stop = kWindow - tid % kWindow;
+                if (rows > stop) rows = stop;
+                kind = head ? kPiece1 : kPiece0;
+                if (head && blockIdx.y == 0) {
+                    const uint32_t slot = atomicAdd(a.s.info + 2, 1u);        // the list's order changes no sum
+                    a.large[slot] = make_uint4(at / kWindow, rank, (end - 1) / kWindow, key);
+                }
+            }
+        }
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, part);
+        if (tid % 32 == 0) part_masks[tid / 32] = mask;
+    }
+    __syncthreads();
+    const unsigned long long part_mask = (unsigned long long)part_masks[1] << 32 | part_masks[0];
+    const uint32_t n_parts = __popcll(part_mask);
+    if (part) parts[__popcll(part_mask & ((1ull << tid) - 1))] = make_uint4(first | rows << 8 | kind << 16 | (tid / kWindow) << 24, key, rank, 0);
+    __syncthreads();
+    // A thread takes every kSumThreads-th (part, vector) pair.
+    const uint32_t step_q = kSumThreads / vecs, step_vec = kSumThreads - step_q * vecs;
+    uint32_t q = tid / vecs, vec = tid - q * vecs;
+    for (; q < n_parts; q += step_q, vec += step_vec) {
+        if (vec >= vecs) {
+            vec -= vecs;
+            if (++q >= n_parts) break;
+        }
+        const uint4 p = parts[q];
+        const uint32_t from = p.x & 0xFF, count = p.x >> 8 & 0xFF, what = p.x >> 16 & 0xFF;
+        const uint32_t col = (vec0 + vec) * E;
+        const TG* grad = (const TG*)a.grad.data + col;
+        Finish<kKind, TO, E> row;
+        const Pack<TG, E> x0 = load_pack<TG, E>(grad + (uint64_t)pos[from] * a.grad.stride);
+        if (what == kWholeToken) row.fetch(a, p.y, col);
+        float sum[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = to_float(x0.v[e]);
+        for (uint32_t i = 1; i < count; i += kSumBatch) {
+            Pack<TG, E> x[kSumBatch];
+#pragma unroll
+            for (int j = 0; j < kSumBatch; ++j)
+                if (i + j < count) x[j] = load_pack<TG, E>(grad + (uint64_t)pos[from + i + j] * a.grad.stride);
+#pragma unroll
+            for (int j = 0; j < kSumBatch; ++j)
+                if (i + j < count)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
+        }
+        if (what == kWholeToken) row.put(a, grad_scale, p.y, p.z, col, sum);
+        else {
+            const uint64_t slot = ((uint64_t)blockIdx.x * (kSpan / kWindow) + (p.x >> 24)) * 2 + (what == kPiece1);
+            store_pack<float, E>(a.partials + slot * a.partial_stride + col, sum);
+        }
     }
 }
 
-// Adds up the partial rows of the tokens that cross spans: the tail of the span they begin in, then the heads of the
-// spans that follow.  Short ones take one thread per vector of columns; long ones a block per 32 vectors, whose
-// warps each add a stretch of the spans and join them in order.
+// Joins the pieces of the tokens with more than 64 positions: slot 1 of the window a token begins in, then slot 0 of the
+// windows that follow.  A block takes a token and 32 vectors of columns; its warps each add a stretch of the pieces.
 template <SumKind kKind, typename TO, int E>
-__global__ void __launch_bounds__(kCrossThreads)
-k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs) {
-    __shared__ float join[kCrossWarps][32 * E + 1];
+__global__ void __launch_bounds__(kJoinThreads)
+k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
+    __shared__ float join[kJoinWarps][32 * E + 1];
     after_previous_launch();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
-    const uint64_t n_short = a.s.info[2], n_long = a.s.info[3];
+    const uint64_t work = (uint64_t)a.s.info[2] * slabs;
     const uint64_t step = (uint64_t)2 * a.partial_stride;
-    for (uint64_t w = (uint64_t)blockIdx.x * kCrossThreads + threadIdx.x; w < n_short * vecs.divisor;
-         w += (uint64_t)gridDim.x * kCrossThreads) {
-        const uint32_t q = (uint32_t)(w / vecs.divisor);
-        const uint4 c = a.crossing[q];
-        const uint32_t col = (uint32_t)(w - (uint64_t)q * vecs.divisor) * E;
-        Finish<kKind, TO, E> row;
-        row.fetch(a, c.w, col);
-        const float* at = a.partials + (uint64_t)c.x * step + col;
-        const Pack<float, E> tail = load_pack<float, E>(at + a.partial_stride);
-        float sum[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = tail.v[e];
-#pragma unroll 4
-        for (uint32_t s = c.x + 1; s <= c.z; ++s) {
-            at += step;
-            const Pack<float, E> x = load_pack<float, E>(at);
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum[e] += x.v[e];
-        }
-        row.put(a, grad_scale, c.w, c.y, col, sum);
-    }
-    const uint32_t spans = (a.n + a.s.span - 1) / a.s.span;
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    for (uint64_t w = blockIdx.x; w < n_long * slabs; w += gridDim.x) {
+    for (uint64_t w = blockIdx.x; w < work; w += gridDim.x) {
         const uint32_t q = (uint32_t)(w / slabs);
-        const uint4 c = a.crossing[spans + q];
+        const uint4 c = a.large[q];
         const uint32_t col = ((uint32_t)(w - (uint64_t)q * slabs) * 32 + lane) * E;
-        const uint32_t heads = c.z - c.x;              // partial rows after the first
-        const uint32_t share = (heads + kCrossWarps - 1) / kCrossWarps;
-        const uint32_t from = wid * share, to = from + share < heads ? from + share : heads;
+        const uint32_t rest = c.z - c.x;               // pieces after the first
+        const uint32_t share = (rest + kJoinWarps - 1) / kJoinWarps;
+        const uint32_t from = wid * share, to = from + share < rest ? from + share : rest;
         Finish<kKind, TO, E> row;
         float sum[E];
 #pragma unroll
@@ -288,9 +298,9 @@ k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs)
             const float* at = a.partials + (uint64_t)c.x * step + col;
             if (wid == 0) {
                 row.fetch(a, c.w, col);
-                const Pack<float, E> tail = load_pack<float, E>(at + a.partial_stride);
+                const Pack<float, E> head = load_pack<float, E>(at + a.partial_stride);
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] = tail.v[e];
+                for (int e = 0; e < E; ++e) sum[e] = head.v[e];
             }
             at += (uint64_t)(from + 1) * step;
 #pragma unroll 8
@@ -304,7 +314,7 @@ k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs)
         for (int e = 0; e < E; ++e) join[wid][lane * E + e] = sum[e];
         __syncthreads();
         if (wid == 0 && col < a.d) {
-            for (int x = 1; x < kCrossWarps; ++x)
+            for (int x = 1; x < kJoinWarps; ++x)
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum[e] += join[x][lane * E + e];
             row.put(a, grad_scale, c.w, c.y, col, sum);
@@ -315,32 +325,25 @@ k_crossing_sums(const __grid_constant__ SumArgs a, FastDiv vecs, uint32_t slabs)
 
 }  // namespace
 
-// Sorted positions per span.
-constexpr uint32_t kLongBatch = 8192;
-uint32_t span_length(uint32_t n, uint32_t) { return n >= kLongBatch ? 16 : 8; }
-uint32_t longest_with_shorter_spans(uint32_t n, uint32_t) { return n >= kLongBatch ? kLongBatch - 1 : 0; }
-
 template <SumKind kKind, typename TG, typename TO, int E>
-static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a) {
-    const uint32_t spans = (a.n + a.s.span - 1) / a.s.span;
-    const FastDiv vecs(a.d / E);
-    const uint32_t most = kMaxItems / vecs.divisor;
-    for (uint32_t span0 = 0; span0 < spans; span0 += most) {
-        const uint32_t total = (spans - span0 < most ? spans - span0 : most) * vecs.divisor;
-        const cudaError_t e = launch_early(k_segment_sums<kKind, TG, TO, E>, (total + kSumThreads - 1) / kSumThreads, kSumThreads,
-                                           stream, a, span0, total, vecs);
-        if (e != cudaSuccess) return e;
-    }
-    if (spans > 1) {
-        const uint32_t slabs = (vecs.divisor + 31) / 32;
-        uint64_t blocks = ((uint64_t)spans * vecs.divisor + kCrossThreads - 1) / kCrossThreads;
-        if (blocks > 592) blocks = 592;
-        return launch_early(k_crossing_sums<kKind, TO, E>, (uint32_t)blocks, kCrossThreads, stream, a, vecs, slabs);
-    }
-    return cudaSuccess;
+static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a, int sms) {
+    const uint32_t spans = (a.n + kSpan - 1) / kSpan, vecs = a.d / E;
+    // enough blocks to go round, as long as a block's slab keeps a few vectors
+    uint32_t slabs = (uint32_t)sms * kSumBlocks / spans + 1;
+    const uint32_t most = (vecs + 15) / 16;
+    if (slabs > most) slabs = most;
+    if (slabs < vecs / 65536 + 1) slabs = vecs / 65536 + 1;
+    const uint32_t slab_vecs = (vecs + slabs - 1) / slabs;
+    slabs = (vecs + slab_vecs - 1) / slab_vecs;
+    const cudaError_t e = launch_early(k_token_sums<kKind, TG, TO, E>, dim3(spans, slabs), kSumThreads, 0, stream, a, slab_vecs);
+    if (e != cudaSuccess || a.n <= kWindow) return e;
+    const uint32_t join_slabs = (vecs + 31) / 32;
+    uint64_t blocks = (uint64_t)(a.n / (kWindow + 1)) * join_slabs;
+    if (blocks > (uint64_t)sms * 4) blocks = (uint64_t)sms * 4;
+    return launch_early(k_join_pieces<kKind, TO, E>, dim3((uint32_t)blocks), kJoinThreads, 0, stream, a, join_slabs);
 }
 
-cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs& a) {
+cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms) {
     uint32_t e = vector_of(a.grad, a.d, widest(a.grad, a.out));
     e = vector_of(a.out, a.d, e);
     if (kind == kSumAdamw) {
@@ -353,9 +356,9 @@ cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs
                 using TG = decltype(tg);
                 using TO = decltype(to);
                 constexpr int E = decltype(w)::value;
-                if (kind == kSumAdamw) return launch_sums<kSumAdamw, TG, TO, E>(stream, a);
-                if (kind == kSumTable) return launch_sums<kSumTable, TG, TO, E>(stream, a);
-                if constexpr (sizeof(TO) == 4) return launch_sums<kSumRows, TG, TO, E>(stream, a);
+                if (kind == kSumAdamw) return launch_sums<kSumAdamw, TG, TO, E>(stream, a, sms);
+                if (kind == kSumTable) return launch_sums<kSumTable, TG, TO, E>(stream, a, sms);
+                if constexpr (sizeof(TO) == 4) return launch_sums<kSumRows, TG, TO, E>(stream, a, sms);
                 else return cudaErrorInvalidValue;
             });
         });

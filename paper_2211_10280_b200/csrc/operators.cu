@@ -14,7 +14,7 @@ using namespace tensair;
 
 namespace {
 
-constexpr uint64_t kMaxTokens = 1ull << 30, kMaxVocabulary = 1ull << 30, kMaxWidth = 1ull << 20;
+constexpr uint64_t kMaxTokens = 1ull << 30, kMaxVocabulary = 1ull << 30, kMaxWidth = 1ull << 20, kMaxStride = (1ull << 31) - 1;
 
 // What the last refused or failed operator call of this thread said (these calls have no context to keep it in).
 // A fixed array: setting it can neither allocate nor throw.
@@ -45,7 +45,7 @@ int check_tokens(const tensair_tokens* t) {
 
 int check_rows(const tensair_rows* r, uint32_t d, bool empty, const char* null, const char* bad) {
     TENSAIR_REQUIRE(r && (empty || r->data), null);
-    TENSAIR_REQUIRE(is_float_type(r->type) && r->d == d && (empty || r->stride >= d) &&
+    TENSAIR_REQUIRE(is_float_type(r->type) && r->d == d && (empty || (r->stride >= d && r->stride <= kMaxStride)) &&
                     (uintptr_t)r->data % type_bytes(r->type) == 0, bad);
     return TENSAIR_OK;
 }
@@ -53,17 +53,16 @@ int check_rows(const tensair_rows* r, uint32_t d, bool empty, const char* null, 
 TokenIds tokens_of(const tensair_tokens& t) {
     return TokenIds{t.ids, t.padding_id, t.error, (uint32_t)t.n, (uint32_t)t.V, t.type == TENSAIR_INT64};
 }
-RowsView view_of(const tensair_rows& r) { return RowsView{r.data, r.stride, r.type}; }
+RowsView view_of(const tensair_rows& r) { return RowsView{r.data, (uint32_t)r.stride, r.type}; }
 
 // The workspace of the gradient calls for a batch of n tokens.
 struct Layout {
-    uint64_t key, pos, seg_start, span_rank, info, crossing, partials, items_a, items_b, hist, tile_counts, total;
-    uint32_t span, spans, partial_stride;
+    uint64_t key, pos, seg_start, span_rank, info, large, partials, items_a, items_b, hist, tile_counts, total;
+    uint32_t partial_stride;
 };
 Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     Layout l;
-    l.span = span_length(n, d);
-    l.spans = (uint32_t)(((uint64_t)n + l.span - 1) / l.span);
+    const uint64_t windows = ((uint64_t)n + kWindow - 1) / kWindow;
     l.partial_stride = (uint32_t)round_up(d, 4);
     uint64_t off = 0;
     auto take = [&off](uint64_t bytes) { const uint64_t at = off; off = round_up(off + bytes, 256); return at; };
@@ -71,9 +70,9 @@ Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     l.key = take((uint64_t)n * 4);
     l.pos = take((uint64_t)n * 4);
     l.seg_start = take(((uint64_t)(n < V ? n : V) + 1) * 4);
-    l.span_rank = take((uint64_t)l.spans * 4);
-    l.crossing = take((uint64_t)l.spans * 2 * sizeof(uint4));
-    l.partials = take((uint64_t)l.spans * 2 * l.partial_stride * 4);
+    l.span_rank = take(((uint64_t)n + kSpan - 1) / kSpan * 4);
+    l.large = take((uint64_t)(n / (kWindow + 1)) * sizeof(uint4));
+    l.partials = take(windows * 2 * l.partial_stride * 4);
     const bool large = !sorts_in_one_launch(n);
     l.items_a = take(large ? (uint64_t)n * 8 : 0);
     l.items_b = take(large ? (uint64_t)n * 8 : 0);
@@ -81,18 +80,6 @@ Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     l.tile_counts = take(large ? ((uint64_t)n / 4096 + 1) * 4 : 0);
     l.total = off;
     return l;
-}
-
-uint64_t workspace_bytes(uint32_t n, uint32_t V, uint32_t d) {
-    // shorter batches may be cut into more, shorter spans
-    uint64_t most = 0;
-    for (uint32_t m = n;;) {
-        const uint64_t b = layout_of(m, V, d).total;
-        if (b > most) most = b;
-        const uint32_t shorter = longest_with_shorter_spans(m, d);
-        if (!shorter) return most;
-        m = shorter;
-    }
 }
 
 int multiprocessors() {
@@ -124,7 +111,7 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
     if (!n) return clear.rows ? launched(launch_clear((cudaStream_t)stream, clear, sms)) : TENSAIR_OK;
     uint8_t* w = (uint8_t*)workspace;
     a.s = SortedTokens{(uint32_t*)(w + l.key), (uint32_t*)(w + l.pos), (uint32_t*)(w + l.seg_start),
-                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info), l.span};
+                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info)};
     a.grad = view_of(*grad);
     a.n = n;
     a.V = V;
@@ -132,11 +119,11 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
     a.scale = scale;
     a.partials = (float*)(w + l.partials);
     a.partial_stride = l.partial_stride;
-    a.crossing = (uint4*)(w + l.crossing);
+    a.large = (uint4*)(w + l.large);
     const SortScratch scratch{(item_t*)(w + l.items_a), (item_t*)(w + l.items_b), (uint32_t*)(w + l.hist),
                               (uint32_t*)(w + l.tile_counts)};
     cudaError_t e = launch_token_sort((cudaStream_t)stream, tokens_of(*tokens), a.s, scratch, clear, sms);
-    if (e == cudaSuccess) e = launch_segment_sums((cudaStream_t)stream, kind, a);
+    if (e == cudaSuccess) e = launch_token_sums((cudaStream_t)stream, kind, a, sms);
     return launched(e);
 }
 
@@ -188,7 +175,7 @@ int tensair_embedding_lookup(const tensair_tokens* tokens, const tensair_rows* t
 int tensair_embedding_workspace_bytes(uint64_t n, uint64_t V, uint32_t d, uint64_t* bytes) {
     TENSAIR_REQUIRE(bytes, "bytes: NULL");
     TENSAIR_REQUIRE(n <= kMaxTokens && V >= 1 && V <= kMaxVocabulary && d >= 1 && d <= kMaxWidth, "n, V or d out of range");
-    *bytes = workspace_bytes((uint32_t)n, (uint32_t)V, d);
+    *bytes = layout_of((uint32_t)n, (uint32_t)V, d).total;
     return TENSAIR_OK;
 }
 
@@ -242,8 +229,8 @@ int tensair_embedding_adamw(const tensair_tokens* tokens, const tensair_rows* gr
     a.out = view_of(*table);
     a.m = (float*)m->data;
     a.v = (float*)v->data;
-    a.m_stride = m->stride;
-    a.v_stride = v->stride;
+    a.m_stride = (uint32_t)m->stride;
+    a.v_stride = (uint32_t)v->stride;
     a.adamw = consts_of(*adamw);
     return gradient_call(tokens, grad, scale, workspace, workspace_bytes, stream, kSumAdamw, a, table->d);
 }

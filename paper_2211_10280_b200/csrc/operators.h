@@ -46,6 +46,16 @@ __device__ __forceinline__ void store_pack(T* p, const float (&x)[E]) {
     *reinterpret_cast<Pack<T, E>*>(p) = out;
 }
 
+// Eight floats in one 32-byte access (sm_100 has them), where the address is a multiple of 32.
+__device__ __forceinline__ void load_eight(const float* p, float (&x)[8]) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(p));
+}
+__device__ __forceinline__ void store_eight(float* p, const float (&x)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
+
 // x / divisor for 32-bit x by one multiplication with a reciprocal rounded up (Granlund & Montgomery 1994):
 // exact for x < 2^31 and any divisor >= 1.
 struct FastDiv {
@@ -56,6 +66,14 @@ struct FastDiv {
         mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
     }
     __device__ __forceinline__ uint32_t div(uint32_t x) const { return (__umulhi(x, mul) + x) >> shift; }
+};
+
+// The same for x < 2^16 and divisors below 2^16, made on the device: floor((x + 1/2) / divisor) in fp32 is exact there (the half keeps the
+// quotient at least 1 / (2 divisor) away from an integer; the two roundings move it by less than 2^-7 / divisor).
+struct FastDivSmall {
+    float inverse;
+    __device__ __forceinline__ explicit FastDivSmall(uint32_t divisor) : inverse(1.0f / (float)divisor) {}
+    __device__ __forceinline__ uint32_t div(uint32_t x) const { return (uint32_t)(((float)x + 0.5f) * inverse); }
 };
 
 // The constants of one AdamW step (see adamw.cuh for the formulas).
@@ -76,9 +94,10 @@ struct SortedTokens {
     uint32_t* pos;         // [n] the batch position it came from
     uint32_t* seg_start;   // [min(n, V) + 1] first sorted position of each distinct token, then n_valid
     uint32_t* span_rank;   // [spans] distinct tokens that begin before the span
-    uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2] short, [3] long crossing segments
-    uint32_t span;         // sorted positions per span (a power of two)
+    uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2] set to zero: tokens with more than kWindow positions
 };
+constexpr uint32_t kSpan = 64;         // sorted positions
+constexpr uint32_t kWindow = 16;       // sorted positions; a token with more is added up in pieces
 struct SortScratch {
     item_t* a;
     item_t* b;
@@ -99,7 +118,7 @@ cudaError_t launch_clear(cudaStream_t stream, const ClearRows& c, int sms);
 // ---- embedding.cu
 struct RowsView {          // rows of d elements, `stride` elements apart
     void* data;
-    uint64_t stride;
+    uint32_t stride;       // below 2^31: a row's offset is one 32 x 32 -> 64-bit product
     uint32_t type;
 };
 enum SumKind { kSumTable, kSumRows, kSumAdamw };
@@ -108,10 +127,10 @@ struct SumArgs {
     RowsView grad;         // [n] gradient rows
     uint32_t n, V, d;
     float scale;
-    float* partials;       // [spans][2][partial_stride]
+    float* partials;       // [windows][2][partial_stride]: the pieces of tokens with more than kWindow positions: of one that
+                           // began in an earlier window, of one that begins in this window
     uint32_t partial_stride;
-    uint4* crossing;       // [2][spans] the segments that leave the span they begin in, short, then long:
-                           // (span, rank, last span, token)
+    uint4* large;          // [n / (kWindow + 1)] those tokens: (window, rank, last window, token)
     // where a finished row goes
     RowsView out;          // kSumTable: row `token`; kSumRows: row `rank`; kSumAdamw: the table of parameters
     int accumulate;        // kSumTable: add to what is there
@@ -119,22 +138,20 @@ struct SumArgs {
     uint32_t* out_count;   // kSumRows
     float* m;
     float* v;
-    uint64_t m_stride, v_stride;
+    uint32_t m_stride, v_stride;
     AdamwConsts adamw;
 };
-uint32_t span_length(uint32_t n, uint32_t d);
-// The longest batch below n tokens whose spans are shorter than those of n; 0 if there is none.
-uint32_t longest_with_shorter_spans(uint32_t n, uint32_t d);
 cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView& table, const RowsView& out, uint32_t d,
                           float scale);
-cudaError_t launch_segment_sums(cudaStream_t stream, SumKind kind, const SumArgs& a);
+cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms);
 // A launch that may begin while the launch before it on the stream is still running: its blocks wait in
 // after_previous_launch() before they touch what that one writes.
 template <typename... Params, typename... Args>
-cudaError_t launch_early(void (*kernel)(Params...), uint32_t grid, uint32_t block, cudaStream_t stream, Args&&... args) {
+cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, uint32_t block, size_t shared, cudaStream_t stream, Args&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

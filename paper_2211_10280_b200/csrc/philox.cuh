@@ -47,4 +47,24 @@ __host__ __device__ inline Philox4 philox4x32_10(Philox4 c, uint32_t key0, uint3
     return c;
 }
 
+// The same with the round keys made beforehand (the key is the same for a whole launch).
+struct PhiloxKeys {
+    uint32_t k0[10], k1[10];
+    PhiloxKeys() = default;
+    __host__ explicit PhiloxKeys(uint64_t seed) {
+        for (int r = 0; r < 10; ++r) {
+            k0[r] = (uint32_t)seed + r * kWeyl0;
+            k1[r] = (uint32_t)(seed >> 32) + r * kWeyl1;
+        }
+    }
+};
+__device__ __forceinline__ Philox4 philox4x32_10(Philox4 c, const PhiloxKeys& keys) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)kPhiloxM0 * c.x, b = (uint64_t)kPhiloxM1 * c.z;
+        c = Philox4{(uint32_t)(b >> 32) ^ c.y ^ keys.k0[r], (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ keys.k1[r], (uint32_t)a};
+    }
+    return c;
+}
+
 }  // namespace tensair

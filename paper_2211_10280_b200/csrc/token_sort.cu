@@ -245,13 +245,13 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
             s.key[i] = item[r].x;
             s.pos[i] = item[r].y;
             if (head_bits >> r & 1) s.seg_start[h] = i;
-            if ((i & (s.span - 1)) == 0) s.span_rank[i / s.span] = h;
+            if (i % kSpan == 0) s.span_rank[i / kSpan] = h;
         }
     }
     if (rank == 0 && threadIdx.x == 0) {
         s.info[0] = all_valid;
         s.info[1] = all_heads;
-        s.info[2] = s.info[3] = 0;
+        s.info[2] = 0;
         s.seg_start[all_heads] = all_valid;
     }
 }
@@ -364,7 +364,7 @@ k_write_tokens(const item_t* __restrict__ items, uint32_t n, uint32_t V, const u
             s.key[i] = key;
             s.pos[i] = item_payload(items[i]);
             if (head) s.seg_start[h] = i;
-            if ((i & (s.span - 1)) == 0) s.span_rank[i / s.span] = h;
+            if (i % kSpan == 0) s.span_rank[i / kSpan] = h;
             if (i + 1 == n || (key < V && item_key(items[i + 1]) >= V)) {    // the last valid position, or the batch's end
                 if (key < V) {
                     s.info[0] = i + 1;
@@ -375,7 +375,7 @@ k_write_tokens(const item_t* __restrict__ items, uint32_t n, uint32_t V, const u
                     s.seg_start[0] = 0;
                 }
             }
-            if (i == 0) s.info[2] = s.info[3] = 0;
+            if (i == 0) s.info[2] = 0;
         }
         run += heads;
     }
