@@ -16,7 +16,7 @@ namespace {
 
 // ------------------------------------------------------------------ lookup
 constexpr int kLookupThreads = 256;
-constexpr int kLookupUnroll = 4;
+constexpr int kLookupUnroll = 4;     // 65,536 rows of 300 floats: 25 us; 31 with 1, 25.5 with 2, 29 with 8
 
 // out[i] = scale * table[ids[i]]; a thread moves kLookupUnroll vectors of E elements, a block's width apart.
 template <typename TT, typename TO, int E>
@@ -123,7 +123,8 @@ constexpr int kSumThreads = 256;
 constexpr uint32_t kMaxParts = kSpan;  // every part begins at a position of its own
 enum SumPart : uint32_t { kWholeToken, kPiece0, kPiece1 };   // pieces: see SumArgs::partials
 constexpr uint32_t kSumBlocks = 4;   // blocks per multiprocessor aimed at
-constexpr int kJoinThreads = 512;
+constexpr uint32_t kFewPieces = 8;     // after the first
+constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;
 
 // What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
@@ -221,8 +222,11 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
                 if (rows > stop) rows = stop;
                 kind = head ? kPiece1 : kPiece0;
                 if (head && blockIdx.y == 0) {
-                    const uint32_t slot = atomicAdd(a.s.info + 2, 1u);        // the list's order changes no sum
-                    a.large[slot] = make_uint4(at / kWindow, rank, (end - 1) / kWindow, key);
+                    // many pieces: the list from its front; few: from its end.  The order in it changes no sum.
+                    const uint32_t from = at / kWindow, to = (end - 1) / kWindow;
+                    const bool many = to - from > kFewPieces;
+                    const uint32_t slot = atomicAdd(a.s.info + (many ? 3 : 2), 1u);
+                    a.large[many ? slot : a.n / (kWindow + 1) - 1 - slot] = make_uint4(from, rank, to, key);
                 }
             }
         }
@@ -271,8 +275,9 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
     }
 }
 
-// Joins the pieces of the tokens with more than 64 positions: slot 1 of the window a token begins in, then slot 0 of the
-// windows that follow.  A block takes a token and 32 vectors of columns; its warps each add a stretch of the pieces.
+// Joins the pieces of the tokens with more than kWindow positions: slot 1 of the window a token begins in, then slot 0 of the
+// windows that follow.  A token with few pieces takes a warp for each 32 vectors of columns, one with many takes a block, whose
+// warps each add a stretch of the pieces.
 template <SumKind kKind, typename TO, int E>
 __global__ void __launch_bounds__(kJoinThreads)
 k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
@@ -280,23 +285,28 @@ k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
     after_previous_launch();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
-    const uint64_t work = (uint64_t)a.s.info[2] * slabs;
-    const uint64_t step = (uint64_t)2 * a.partial_stride;
     const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    for (uint64_t w = blockIdx.x; w < work; w += gridDim.x) {
-        const uint32_t q = (uint32_t)(w / slabs);
-        const uint4 c = a.large[q];
-        const uint32_t col = ((uint32_t)(w - (uint64_t)q * slabs) * 32 + lane) * E;
-        const uint32_t rest = c.z - c.x;               // pieces after the first
-        const uint32_t share = (rest + kJoinWarps - 1) / kJoinWarps;
-        const uint32_t from = wid * share, to = from + share < rest ? from + share : rest;
+    const uint64_t few = ((uint64_t)a.s.info[2] * slabs + kJoinWarps - 1) / kJoinWarps, many = (uint64_t)a.s.info[3] * slabs;
+    const uint64_t step = (uint64_t)2 * a.partial_stride;
+    for (uint64_t w = blockIdx.x; w < many + few; w += gridDim.x) {
+        const bool shared = w < many;      // the block's warps share a token
+        const uint64_t item = shared ? w : (w - many) * kJoinWarps + wid;
+        const uint32_t q = (uint32_t)(item / slabs);
+        const bool in = shared || q < a.s.info[2];
+        uint4 c = make_uint4(0, 0, 0, 0);
+        if (in) c = a.large[shared ? q : a.n / (kWindow + 1) - 1 - q];
+        const uint32_t col = ((uint32_t)(item - (uint64_t)q * slabs) * 32 + lane) * E;
+        const uint32_t rest = c.z - c.x;   // pieces after the first
+        const uint32_t share = shared ? (rest + kJoinWarps - 1) / kJoinWarps : rest;
+        const uint32_t from = shared ? wid * share : 0, to = from + share < rest ? from + share : rest;
+        const bool first = in && col < a.d && (!shared || wid == 0);
         Finish<kKind, TO, E> row;
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-        if (col < a.d) {
+        if (in && col < a.d) {
             const float* at = a.partials + (uint64_t)c.x * step + col;
-            if (wid == 0) {
+            if (first) {
                 row.fetch(a, c.w, col);
                 const Pack<float, E> head = load_pack<float, E>(at + a.partial_stride);
 #pragma unroll
@@ -310,16 +320,17 @@ k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
                 for (int e = 0; e < E; ++e) sum[e] += x.v[e];
             }
         }
+        if (shared) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) join[wid][lane * E + e] = sum[e];
-        __syncthreads();
-        if (wid == 0 && col < a.d) {
-            for (int x = 1; x < kJoinWarps; ++x)
+            for (int e = 0; e < E; ++e) join[wid][lane * E + e] = sum[e];
+            __syncthreads();
+            if (first)
+                for (int x = 1; x < kJoinWarps; ++x)
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += join[x][lane * E + e];
-            row.put(a, grad_scale, c.w, c.y, col, sum);
+                    for (int e = 0; e < E; ++e) sum[e] += join[x][lane * E + e];
+            __syncthreads();
         }
-        __syncthreads();
+        if (first) row.put(a, grad_scale, c.w, c.y, col, sum);
     }
 }
 

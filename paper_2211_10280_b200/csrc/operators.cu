@@ -1,6 +1,7 @@
 // C entry points of the language-model operators: argument checks, workspace layout, launches.
 #include "../../include/tensair.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdio>
@@ -73,11 +74,15 @@ Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     l.span_rank = take(((uint64_t)n + kSpan - 1) / kSpan * 4);
     l.large = take((uint64_t)(n / (kWindow + 1)) * sizeof(uint4));
     l.partials = take(windows * 2 * l.partial_stride * 4);
-    const bool large = !sorts_in_one_launch(n);
-    l.items_a = take(large ? (uint64_t)n * 8 : 0);
-    l.items_b = take(large ? (uint64_t)n * 8 : 0);
-    l.hist = take(large ? (uint64_t)sort_hist_words(n) * 4 : 0);
-    l.tile_counts = take(large ? ((uint64_t)n / 4096 + 1) * 4 : 0);
+    // the sort's needs change with the length class: a workspace takes the largest of what shorter batches need
+    SortScratchBytes s = sort_scratch_bytes(n);
+    const SortScratchBytes shorter = sort_scratch_bytes(n < kTiledSort ? n : kTiledSort);
+    s.hist = std::max(s.hist, shorter.hist);
+    s.tile_counts = std::max(s.tile_counts, shorter.tile_counts);
+    l.items_a = take(s.items);
+    l.items_b = take(s.items);
+    l.hist = take(s.hist);
+    l.tile_counts = take(s.tile_counts);
     l.total = off;
     return l;
 }

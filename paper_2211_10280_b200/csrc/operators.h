@@ -94,7 +94,7 @@ struct SortedTokens {
     uint32_t* pos;         // [n] the batch position it came from
     uint32_t* seg_start;   // [min(n, V) + 1] first sorted position of each distinct token, then n_valid
     uint32_t* span_rank;   // [spans] distinct tokens that begin before the span
-    uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2] set to zero: tokens with more than kWindow positions
+    uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2], [3] set to zero: entries of SumArgs::large
 };
 constexpr uint32_t kSpan = 64;         // sorted positions
 constexpr uint32_t kWindow = 16;       // sorted positions; a token with more is added up in pieces
@@ -109,7 +109,11 @@ struct ClearRows {
     uint8_t* data;
     uint64_t stride, width, rows;
 };
-bool sorts_in_one_launch(uint32_t n);
+struct SortScratchBytes {
+    size_t items, hist, tile_counts;   // of a and b each, and of the other two
+};
+SortScratchBytes sort_scratch_bytes(uint32_t n);
+constexpr uint32_t kTiledSort = 1 << 17;   // the longest batch whose scratch is that of the sort in tiles
 // Also clears `c`, beside the sort.
 cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w,
                               const ClearRows& c, int sms);
@@ -130,7 +134,8 @@ struct SumArgs {
     float* partials;       // [windows][2][partial_stride]: the pieces of tokens with more than kWindow positions: of one that
                            // began in an earlier window, of one that begins in this window
     uint32_t partial_stride;
-    uint4* large;          // [n / (kWindow + 1)] those tokens: (window, rank, last window, token)
+    uint4* large;          // [n / (kWindow + 1)] those tokens: (window, rank, last window, token), the ones with many pieces
+                           // from the front, the others from the end
     // where a finished row goes
     RowsView out;          // kSumTable: row `token`; kSumRows: row `rank`; kSumAdamw: the table of parameters
     int accumulate;        // kSumTable: add to what is there

@@ -1,13 +1,17 @@
 // The positions of a batch sorted by token (stable), with the segments of equal tokens: what the embedding gradient
 // sums by.  Positions that hold no token (padding, ids outside [0,V)) sort behind all others, as key V.
 //
-// Up to 2^17 positions the whole sort is one launch of one thread-block cluster.  A batch of that size is a
-// megabyte at most, so it stays in the cluster's shared memory: every pass ranks its items in registers, exchanges the
-// digit totals through distributed shared memory and writes the items, put in digit order first, into the shared memory
-// of the block that owns their place.  What bounds it is latency: issue slots of the ranking (which fall with the number
-// of blocks) and a few barriers per pass, so a batch is spread over as many blocks as a cluster may have, and the digits are
+// A radix sort with one item per thread in blocks of 1,024, so that ranking (some 50 integer instructions per item and pass,
+// which is what a block's time goes into) is spread over as many multiprocessors as there are items for.  Digits are
 // as wide as the counters allow: ten bits, two passes up to V = 2^20 - 1.
-// Larger batches go through the library's multi-launch radix sort.
+//   up to 2^14 positions   one launch of one thread-block cluster.  The items stay in the cluster's shared memory; every pass
+//                          exchanges the digit totals through distributed shared memory and writes the items straight into
+//                          the shared memory of the block that owns their place.  Bound by the latency of its barriers.
+//   up to 2^17             two launches per pass, rank and scatter, and one that lists the tokens; items and totals go through
+//                          the level-2 cache, and every block adds up the totals it needs itself.  Each launch begins
+//                          while the one before it ends.  (One cluster with 4 items per thread took 27 us for 65,536
+//                          tokens, this takes 22.5.)
+//   beyond                 the library's multi-launch radix sort.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -27,7 +31,7 @@ constexpr int kSortBlockWarps = kSortBlock / 32;
 constexpr int kMaxDigitBits = 10;
 constexpr uint32_t kMaxCluster = 16;                           // needs leave of the device; 8 always works
 constexpr uint32_t kPortableCluster = 8;
-constexpr int kMaxItems = 8;                                   // per thread
+constexpr uint32_t kMaxTiles = kTiledSort / kSortBlock;                            // blocks of the sort in several launches
 
 __device__ __forceinline__ uint32_t token_key(const TokenIds& t, uint32_t i) {
     const int64_t id = t.wide ? reinterpret_cast<const int64_t*>(t.ids)[i] : reinterpret_cast<const int32_t*>(t.ids)[i];
@@ -77,22 +81,52 @@ __device__ void clear_part(const ClearRows& c, uint64_t part, uint64_t parts) {
     }
 }
 
+// Rank of the thread's item among the block's items of its digit, in item order.  counts: [warp][digit] in shared memory, 16 bits
+// each.  publish(x, totals) is called once for every pair of digits (2x, 2x + 1) with the block's two totals, 16 bits each.
+//
+// Within a warp the lanes of a digit find each other by one ballot per bit (the match instruction gains nothing: it takes longer
+// the more digits a warp's items have, and the slowest block counts).
+template <typename F>
+__device__ __forceinline__ uint32_t block_rank(uint32_t digit, uint32_t digit_bits, uint32_t* counts, F&& publish) {
+    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5, pairs = 1u << digit_bits >> 1;
+    for (uint32_t x = threadIdx.x; x < kSortBlockWarps * pairs; x += kSortBlock) counts[x] = 0;
+    uint32_t peers = 0xFFFFFFFFu;
+#pragma unroll
+    for (int bit = 0; bit < kMaxDigitBits; ++bit)
+        if (bit < (int)digit_bits) {
+            const bool one = (digit & 1u << bit) != 0;
+            peers &= __ballot_sync(0xFFFFFFFFu, one) ^ (one ? 0u : 0xFFFFFFFFu);
+        }
+    const uint32_t rank = __popc(peers & ((1u << lane) - 1));
+    uint16_t* mine = reinterpret_cast<uint16_t*>(counts) + wid * 2 * pairs;
+    __syncthreads();
+    if (rank == 0) mine[digit] = (uint16_t)__popc(peers);
+    __syncthreads();
+    if (threadIdx.x < pairs) {       // exclusive sum over the warps, two digits at once
+        uint32_t run = 0;
+#pragma unroll 16
+        for (int w = 0; w < kSortBlockWarps; ++w) {
+            const uint32_t c = counts[w * pairs + threadIdx.x];
+            counts[w * pairs + threadIdx.x] = run;
+            run += c;
+        }
+        publish(threadIdx.x, run);
+    }
+    __syncthreads();
+    return rank + mine[digit];
+}
+
 struct ClusterShared {
     uint32_t warp_sums[kSortBlockWarps];
     uint32_t heads[kMaxCluster], valid[kMaxCluster];   // of every block of the cluster, written by that block
     uint32_t digit_base[1 << kMaxDigitBits];
+    uint2 items[kSortBlock];                           // (key, position)
 };
-
-constexpr size_t larger(size_t a, size_t b) { return a > b ? a : b; }
-template <int kItems>
+constexpr size_t counts_bytes(size_t bins) { return kSortBlockWarps * bins * 2; }
 constexpr size_t cluster_shared_bytes(size_t bins, size_t blocks) {
-    return sizeof(ClusterShared) + (size_t)kSortBlock * kItems * 8                          // items
-           + larger(kSortBlockWarps * bins * 2, (size_t)kSortBlock * kItems * 8)            // counters per warp, then staging
-           + blocks * bins * 2;                                                             // digit totals of every block
+    return sizeof(ClusterShared) + counts_bytes(bins) + blocks * bins * 2;     // ..., digit totals of every block
 }
-static_assert(cluster_shared_bytes<kMaxItems>(1 << kMaxDigitBits, kMaxCluster) <= 227 * 1024, "fits a block's shared memory");
 
-template <int kItems>
 __global__ void __launch_bounds__(kSortBlock, 1)
 k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bits, ClearRows clear) {
     cg::cluster_group cluster = cg::this_cluster();
@@ -103,132 +137,45 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
         return;
     }
     extern __shared__ __align__(16) uint8_t raw[];
-    constexpr uint32_t kPerBlock = kSortBlock * kItems;
-    const uint32_t bins = 1u << digit_bits, mask = bins - 1;
+    const uint32_t bins = 1u << digit_bits, mask = bins - 1, tid = threadIdx.x;
     ClusterShared& sh = *reinterpret_cast<ClusterShared*>(raw);
-    uint2* items = reinterpret_cast<uint2*>(raw + sizeof(ClusterShared));         // (key, position)
-    uint2* staged = items + kPerBlock;                                            // the block's items in digit order
-    uint32_t* counts = reinterpret_cast<uint32_t*>(staged);                       // [warp][digit], 16 bits each; then staged
-    uint16_t* totals = reinterpret_cast<uint16_t*>(raw + sizeof(ClusterShared) + kPerBlock * 8 +
-                                                   max(kSortBlockWarps * bins * 2, kPerBlock * 8));   // [block][digit]
-    const uint32_t lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const uint32_t first = rank * kPerBlock;          // first position of this block
-    const uint32_t my = wid * 32 * kItems + lane;     // a warp owns 32 * kItems consecutive items
-    const uint32_t lower = (1u << lane) - 1;
-    uint2 item[kItems];
-    uint32_t place[kItems];
-#pragma unroll
-    for (int r = 0; r < kItems; ++r) {
-        const uint32_t i = first + my + r * 32;
-        // places past the batch sort behind everything, in order
-        item[r] = make_uint2(i < t.n ? token_key(t, i) : 0xFFFFFFFFu, i);
-    }
+    uint32_t* counts = reinterpret_cast<uint32_t*>(raw + sizeof(ClusterShared));
+    uint16_t* totals = reinterpret_cast<uint16_t*>(counts) + kSortBlockWarps * bins;   // [block][digit]
+    const uint32_t at = rank * kSortBlock + tid;
+    // places past the batch sort behind everything, in order
+    uint2 item = make_uint2(at < t.n ? token_key(t, at) : 0xFFFFFFFFu, at);
     for (uint32_t shift = 0; shift < key_bits; shift += digit_bits) {
-        for (uint32_t x = threadIdx.x; x < kSortBlockWarps * bins / 2; x += kSortBlock) counts[x] = 0;
-        __syncthreads();
-        uint16_t* mine = reinterpret_cast<uint16_t*>(counts) + wid * bins;
-        // Rank of an item among the warp's items of its digit, in item order.  The lanes of a digit find each other by one
-        // ballot per bit; the first of them moves the warp's counter on, with a plain store (an atomic add on shared memory, which
-        // would spare the two barriers, took twice as long).  The rounds follow each other in order.
-        constexpr int kGroup = kItems < 4 ? kItems : 4;
-#pragma unroll
-        for (int r0 = 0; r0 < kItems; r0 += kGroup) {
-            uint32_t peers[kGroup];
-#pragma unroll
-            for (int r = 0; r < kGroup; ++r) peers[r] = 0xFFFFFFFFu;
-#pragma unroll
-            for (int bit = 0; bit < kMaxDigitBits; ++bit)
-                if (bit < (int)digit_bits)
-#pragma unroll
-                    for (int r = 0; r < kGroup; ++r) {
-                        const bool one = (item[r0 + r].x >> shift & 1u << bit) != 0;
-                        peers[r] &= __ballot_sync(0xFFFFFFFFu, one) ^ (one ? 0u : 0xFFFFFFFFu);
-                    }
-#pragma unroll
-            for (int r = 0; r < kGroup; ++r) {
-                const uint32_t digit = item[r0 + r].x >> shift & mask;
-                const uint32_t before = mine[digit];
-                place[r0 + r] = before + __popc(peers[r] & lower);
-                __syncwarp();
-                if ((peers[r] & lower) == 0) mine[digit] = (uint16_t)(before + __popc(peers[r]));
-                __syncwarp();
-            }
-        }
-        __syncthreads();
-        // per pair of digits: exclusive sum over the warps, and the block's totals to every block of the cluster
-        if (threadIdx.x < bins / 2) {
-            uint32_t run = 0;     // two 16-bit sums; a block has at most 2^13 items
-#pragma unroll 8
-            for (int w = 0; w < kSortBlockWarps; ++w) {
-                const uint32_t c = counts[w * (bins / 2) + threadIdx.x];
-                counts[w * (bins / 2) + threadIdx.x] = run;
-                run += c;
-            }
-            for (uint32_t b = 0; b < blocks; ++b)
-                reinterpret_cast<uint32_t*>(cluster.map_shared_rank(totals, b))[rank * (bins / 2) + threadIdx.x] = run;
-        }
-        auto arrived = cluster.barrier_arrive();
-        __syncthreads();
-        // the block's own items in digit order, where the counters were
-        const uint32_t own = threadIdx.x < bins ? totals[rank * bins + threadIdx.x] : 0;
-        const uint32_t own_start = block_exclusive(own, sh.warp_sums, nullptr);
-#pragma unroll
-        for (int r = 0; r < kItems; ++r) {
-            const uint32_t digit = item[r].x >> shift & mask;
-            place[r] += mine[digit];
-        }
-        if (threadIdx.x < bins) sh.digit_base[threadIdx.x] = own_start;
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kItems; ++r) staged[sh.digit_base[item[r].x >> shift & mask] + place[r]] = item[r];
-        cluster.barrier_wait(std::move(arrived));   // every block's totals are here, and every block has read its items
+        const uint32_t digit = item.x >> shift & mask;
+        const uint32_t place = block_rank(digit, digit_bits, counts, [&](uint32_t x, uint32_t two) {
+            for (uint32_t b = 0; b < blocks; ++b) reinterpret_cast<uint32_t*>(cluster.map_shared_rank(totals, b))[rank * (bins / 2) + x] = two;
+        });
+        cluster.sync();   // every block's totals are here, and every block has read its items
         uint32_t sum = 0, before = 0;
-        if (threadIdx.x < bins)
+        if (tid < bins)
             for (uint32_t b = 0; b < blocks; ++b) {
-                const uint32_t c = totals[b * bins + threadIdx.x];
+                const uint32_t c = totals[b * bins + tid];
                 if (b < rank) before += c;
                 sum += c;
             }
         const uint32_t digit_start = block_exclusive(sum, sh.warp_sums, nullptr);
-        if (threadIdx.x < bins) sh.digit_base[threadIdx.x] = digit_start + before - own_start;   // from staged place to final place
+        if (tid < bins) sh.digit_base[tid] = digit_start + before;
         __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kItems; ++r) {
-            const uint32_t at = r * kSortBlock + threadIdx.x;
-            const uint2 it = staged[at];
-            const uint32_t to = sh.digit_base[it.x >> shift & mask] + at;
-            cluster.map_shared_rank(items, to / kPerBlock)[to % kPerBlock] = it;
-        }
+        const uint32_t to = sh.digit_base[digit] + place;
+        cluster.map_shared_rank(sh.items, to / kSortBlock)[to % kSortBlock] = item;
         cluster.sync();
-#pragma unroll
-        for (int r = 0; r < kItems; ++r) item[r] = items[my + r * 32];
+        item = sh.items[tid];
     }
-    // this block now holds sorted positions [first, first + kPerBlock): mark the first position of every token
-    uint32_t previous = 0xFFFFFFFFu;                   // of the warp's first item
-    if (lane == 0) {
-        if (my) previous = items[my - 1].x;
-        else if (rank) previous = cluster.map_shared_rank(items, rank - 1)[kPerBlock - 1].x;
-    }
-    uint32_t head_bits = 0, n_valid = 0, n_heads = 0;
-#pragma unroll
-    for (int r = 0; r < kItems; ++r) {
-        const uint32_t left = __shfl_up_sync(0xFFFFFFFFu, item[r].x, 1);
-        const bool valid = item[r].x < t.V;
-        const bool head = valid && item[r].x != (lane ? left : previous);
-        previous = __shfl_sync(0xFFFFFFFFu, item[r].x, 31);
-        const uint32_t heads = __ballot_sync(0xFFFFFFFFu, head);
-        n_valid += __popc(__ballot_sync(0xFFFFFFFFu, valid));
-        place[r] = n_heads + __popc(heads & lower);   // heads of this warp before the item
-        n_heads += __popc(heads);
-        head_bits |= (uint32_t)head << r;
-    }
-    uint32_t block_heads, block_valid;
-    uint32_t before = block_exclusive(lane == 0 ? n_heads : 0, sh.warp_sums, &block_heads);
-    before = __shfl_sync(0xFFFFFFFFu, before, 0);
-    block_exclusive(lane == 0 ? n_valid : 0, sh.warp_sums, &block_valid);
-    if (threadIdx.x < blocks) {
-        cluster.map_shared_rank(sh.heads, threadIdx.x)[rank] = block_heads;
-        cluster.map_shared_rank(sh.valid, threadIdx.x)[rank] = block_valid;
+    // the thread now holds sorted position `at`: mark the first position of every token
+    uint32_t previous = 0xFFFFFFFFu;
+    if (tid) previous = sh.items[tid - 1].x;
+    else if (rank) previous = cluster.map_shared_rank(sh.items, rank - 1)[kSortBlock - 1].x;
+    const bool valid = item.x < t.V, head = valid && item.x != previous;
+    uint32_t block_heads;
+    uint32_t before = block_exclusive(head, sh.warp_sums, &block_heads);
+    const uint32_t block_valid = __syncthreads_count(valid);
+    if (tid < blocks) {
+        cluster.map_shared_rank(sh.heads, tid)[rank] = block_heads;
+        cluster.map_shared_rank(sh.valid, tid)[rank] = block_valid;
     }
     cluster.sync();       // no block reads another one's shared memory after this
     uint32_t all_heads = 0, all_valid = 0;
@@ -237,22 +184,111 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
         all_heads += sh.heads[b];
         all_valid += sh.valid[b];
     }
-#pragma unroll
-    for (int r = 0; r < kItems; ++r) {
-        const uint32_t i = first + my + r * 32;
-        if (i < t.n) {
-            const uint32_t h = before + place[r];
-            s.key[i] = item[r].x;
-            s.pos[i] = item[r].y;
-            if (head_bits >> r & 1) s.seg_start[h] = i;
-            if (i % kSpan == 0) s.span_rank[i / kSpan] = h;
-        }
+    if (at < t.n) {
+        s.key[at] = item.x;
+        s.pos[at] = item.y;
+        if (head) s.seg_start[before] = at;
+        if (at % kSpan == 0) s.span_rank[at / kSpan] = before;
     }
-    if (rank == 0 && threadIdx.x == 0) {
+    if (at == 0) {
         s.info[0] = all_valid;
         s.info[1] = all_heads;
-        s.info[2] = 0;
+        s.info[2] = s.info[3] = 0;
         s.seg_start[all_heads] = all_valid;
+    }
+}
+
+// ---- in several launches.  A tile is the 1,024 items of a block; hist: [tile][digit], 16 bits each.
+// Ranks the tile's items of a pass by digit: place[i] is the rank among the tile's items of its digit.
+template <bool kFirst>
+__global__ void __launch_bounds__(kSortBlock)
+k_tile_rank(TokenIds t, const uint2* __restrict__ items, uint2* __restrict__ out, uint16_t* __restrict__ place, uint32_t* __restrict__ hist,
+            uint32_t shift, uint32_t digit_bits, uint32_t tiles, ClearRows clear) {
+    extern __shared__ __align__(16) uint32_t counts[];
+    let_next_launch_begin();
+    if (!kFirst) after_previous_launch();
+    if (kFirst && blockIdx.x >= tiles) {
+        clear_part(clear, blockIdx.x - tiles, gridDim.x - tiles);
+        return;
+    }
+    const uint32_t at = blockIdx.x * kSortBlock + threadIdx.x, pairs = 1u << digit_bits >> 1;
+    uint32_t key = 0xFFFFFFFFu;
+    if (at < t.n) {
+        key = kFirst ? token_key(t, at) : items[at].x;
+        if (kFirst) out[at] = make_uint2(key, at);
+    }
+    const uint32_t rank = block_rank(key >> shift & (2 * pairs - 1), digit_bits, counts,
+                                     [&](uint32_t x, uint32_t two) { hist[blockIdx.x * pairs + x] = two; });
+    if (at < t.n) place[at] = (uint16_t)rank;
+}
+
+// Moves the items to where the pass has them; the last pass writes keys and positions apart.
+template <bool kLast>
+__global__ void __launch_bounds__(kSortBlock)
+k_tile_scatter(uint32_t n, const uint2* __restrict__ items, uint2* __restrict__ out, const uint16_t* __restrict__ place,
+               const uint16_t* __restrict__ hist, uint32_t shift, uint32_t digit_bits, uint32_t tiles, SortedTokens s) {
+    __shared__ uint32_t base[1 << kMaxDigitBits], warp_sums[kSortBlockWarps];
+    let_next_launch_begin();
+    const uint32_t tid = threadIdx.x, at = blockIdx.x * kSortBlock + tid, bins = 1u << digit_bits;
+    after_previous_launch();
+    uint2 item = make_uint2(0, 0);
+    uint32_t rank = 0;
+    if (at < n) {
+        item = items[at];
+        rank = place[at];
+    }
+    uint32_t all = 0, before = 0;      // items of the digit in all tiles, and in the tiles before this one
+    if (tid < bins) {
+#pragma unroll 16
+        for (uint32_t x = 0; x < tiles; ++x) {
+            const uint32_t c = hist[x * bins + tid];
+            if (x < blockIdx.x) before += c;
+            all += c;
+        }
+    }
+    const uint32_t start = block_exclusive(all, warp_sums, nullptr);
+    if (tid < bins) base[tid] = start + before;
+    __syncthreads();
+    if (at >= n) return;
+    const uint32_t to = base[item.x >> shift & (bins - 1)] + rank;     // below n: the places past the batch come last
+    if (kLast) {
+        s.key[to] = item.x;
+        s.pos[to] = item.y;
+    } else out[to] = item;
+}
+
+// Lists the tokens of the sorted positions.  A block counts the tokens that begin before it from the keys themselves.
+__global__ void __launch_bounds__(kSortBlock)
+k_list_tokens(uint32_t n, uint32_t V, SortedTokens s) {
+    __shared__ uint32_t warp_sums[kSortBlockWarps];
+    let_next_launch_begin();
+    const uint32_t tid = threadIdx.x, first = blockIdx.x * kSortBlock, at = first + tid;
+    after_previous_launch();
+    uint32_t c = 0;
+    const uint4* keys = reinterpret_cast<const uint4*>(s.key);
+#pragma unroll 8
+    for (uint32_t x = tid; x < first / 4; x += kSortBlock) {
+        const uint4 k = keys[x];
+        const uint32_t left = x ? s.key[4 * x - 1] : 0xFFFFFFFFu;
+        c += (k.x < V && k.x != left) + (k.y < V && k.y != k.x) + (k.z < V && k.z != k.y) + (k.w < V && k.w != k.z);
+    }
+    uint32_t run, heads;
+    block_exclusive(c, warp_sums, &run);
+    const uint32_t key = at < n ? s.key[at] : 0xFFFFFFFFu;
+    const bool head = key < V && (at == 0 || s.key[at - 1] != key);
+    const uint32_t h = run + block_exclusive(head, warp_sums, &heads);
+    if (at >= n) return;
+    if (head) s.seg_start[h] = at;
+    if (at % kSpan == 0) s.span_rank[at / kSpan] = h;
+    const bool ends = at + 1 == n || s.key[at + 1] >= V;
+    if (key < V && ends) {             // the last position with a token
+        s.info[0] = at + 1;
+        s.info[1] = h + head;
+        s.seg_start[h + head] = at + 1;
+    }
+    if (at == 0) {
+        s.info[2] = s.info[3] = 0;
+        if (key >= V) s.info[0] = s.info[1] = s.seg_start[0] = 0;
     }
 }
 
@@ -265,7 +301,6 @@ uint32_t clear_blocks(const ClearRows& c, int sms, uint32_t cluster) {
 
 __global__ void __launch_bounds__(kSortBlock) k_clear(ClearRows c) { clear_part(c, blockIdx.x, gridDim.x); }
 
-template <int kItems>
 cudaLaunchConfig_t cluster_launch(cudaStream_t stream, uint32_t blocks, uint32_t digit_bits, cudaLaunchAttribute* attr) {
     attr->id = cudaLaunchAttributeClusterDimension;
     attr->val.clusterDim.x = blocks;
@@ -273,49 +308,64 @@ cudaLaunchConfig_t cluster_launch(cudaStream_t stream, uint32_t blocks, uint32_t
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = blocks;
     cfg.blockDim = kSortBlock;
-    cfg.dynamicSmemBytes = cluster_shared_bytes<kItems>((size_t)1 << digit_bits, blocks);
+    cfg.dynamicSmemBytes = cluster_shared_bytes((size_t)1 << digit_bits, blocks);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cfg;
 }
 
-// What k_cluster_sort<kItems> needs set on a device before its first launch there; returns the largest cluster it may have.
-template <int kItems>
-cudaError_t prepare_cluster(int device, uint32_t* most) {
+// What the kernels need set on a device before their first launch there; *most: the largest cluster it may have.
+cudaError_t prepare_device(uint32_t* most) {
     static std::atomic<uint32_t> known[kMaxDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
     *most = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
     if (*most) return cudaSuccess;
-    cudaError_t e = cudaFuncSetAttribute(k_cluster_sort<kItems>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)cluster_shared_bytes<kItems>(1 << kMaxDigitBits, kMaxCluster));
+    const int counts = (int)counts_bytes(1 << kMaxDigitBits);
+    e = cudaFuncSetAttribute(k_cluster_sort, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)cluster_shared_bytes(1 << kMaxDigitBits, kMaxCluster));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_tile_rank<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, counts);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_tile_rank<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, counts);
     if (e != cudaSuccess) return e;
     *most = kPortableCluster;
-    if (cudaFuncSetAttribute(k_cluster_sort<kItems>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+    if (cudaFuncSetAttribute(k_cluster_sort, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
         cudaLaunchAttribute attr[1];
-        const cudaLaunchConfig_t cfg = cluster_launch<kItems>(nullptr, kMaxCluster, kMaxDigitBits, attr);
+        const cudaLaunchConfig_t cfg = cluster_launch(nullptr, kMaxCluster, kMaxDigitBits, attr);
         int clusters = 0;
-        if (cudaOccupancyMaxActiveClusters(&clusters, k_cluster_sort<kItems>, &cfg) == cudaSuccess && clusters > 0) *most = kMaxCluster;
+        if (cudaOccupancyMaxActiveClusters(&clusters, k_cluster_sort, &cfg) == cudaSuccess && clusters > 0) *most = kMaxCluster;
     }
     cudaGetLastError();       // a refusal of the larger cluster is no error
     if (device < kMaxDevices) known[device].store(*most, std::memory_order_relaxed);
     return cudaSuccess;
 }
 
-template <int kItems>
-cudaError_t cluster_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, uint32_t key_bits, int device,
-                         const ClearRows& clear, int sms, bool* done) {
-    uint32_t most;
-    const cudaError_t e = prepare_cluster<kItems>(device, &most);
-    if (e != cudaSuccess) return e;
-    uint32_t blocks = 1;
-    while (blocks < most && blocks * kSortBlock * kItems < t.n) blocks *= 2;
-    if (blocks * kSortBlock * kItems < t.n) return cudaSuccess;
-    *done = true;
-    const uint32_t passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits, digit_bits = (key_bits + passes - 1) / passes;
-    cudaLaunchAttribute attr[1];
-    cudaLaunchConfig_t cfg = cluster_launch<kItems>(stream, blocks, digit_bits, attr);
-    cfg.gridDim.x += clear_blocks(clear, sms, blocks);
-    return cudaLaunchKernelEx(&cfg, k_cluster_sort<kItems>, t, s, key_bits, digit_bits, clear);
+cudaError_t sort_in_tiles(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w, uint32_t key_bits,
+                          uint32_t digit_bits, const ClearRows& clear, int sms) {
+    const uint32_t tiles = (t.n + kSortBlock - 1) / kSortBlock;
+    const size_t counts = counts_bytes((size_t)1 << digit_bits);
+    uint2* from = reinterpret_cast<uint2*>(w.a);
+    uint2* to = reinterpret_cast<uint2*>(w.b);
+    uint16_t* place = reinterpret_cast<uint16_t*>(w.tile_counts);
+    for (uint32_t shift = 0; shift < key_bits; shift += digit_bits) {
+        cudaError_t e;
+        if (shift == 0) {
+            k_tile_rank<true><<<tiles + clear_blocks(clear, sms, 1), kSortBlock, counts, stream>>>(t, nullptr, from, place, w.hist, shift,
+                                                                                                  digit_bits, tiles, clear);
+            e = cudaGetLastError();
+        } else {
+            e = launch_early(k_tile_rank<false>, tiles, kSortBlock, counts, stream, t, (const uint2*)from, to, place, w.hist, shift,
+                             digit_bits, tiles, ClearRows{});
+        }
+        if (e != cudaSuccess) return e;
+        auto scatter = shift + digit_bits < key_bits ? k_tile_scatter<false> : k_tile_scatter<true>;
+        e = launch_early(scatter, tiles, kSortBlock, 0, stream, t.n, (const uint2*)from, to, (const uint16_t*)place, (const uint16_t*)w.hist, shift,
+                         digit_bits, tiles, s);
+        if (e != cudaSuccess) return e;
+        std::swap(from, to);
+    }
+    return launch_early(k_list_tokens, tiles, kSortBlock, 0, stream, t.n, t.V, s);
 }
 
 // ---- larger batches
@@ -375,7 +425,7 @@ k_write_tokens(const item_t* __restrict__ items, uint32_t n, uint32_t V, const u
                     s.seg_start[0] = 0;
                 }
             }
-            if (i == 0) s.info[2] = 0;
+            if (i == 0) s.info[2] = s.info[3] = 0;
         }
         run += heads;
     }
@@ -383,7 +433,19 @@ k_write_tokens(const item_t* __restrict__ items, uint32_t n, uint32_t V, const u
 
 }  // namespace
 
-bool sorts_in_one_launch(uint32_t n) { return n <= kPortableCluster * kSortBlock * kMaxItems; }
+SortScratchBytes sort_scratch_bytes(uint32_t n) {
+    SortScratchBytes b = {0, 0, 0};
+    if (n <= kPortableCluster * kSortBlock) return b;
+    b.items = (size_t)n * 8;
+    if (n <= kMaxTiles * kSortBlock) {
+        b.hist = ((size_t)n + kSortBlock - 1) / kSortBlock * (2 << kMaxDigitBits);
+        b.tile_counts = (size_t)n * 2;
+    } else {
+        b.hist = (size_t)sort_hist_words(n) * 4;
+        b.tile_counts = ((size_t)n + kTileItems - 1) / kTileItems * 4;
+    }
+    return b;
+}
 
 cudaError_t launch_clear(cudaStream_t stream, const ClearRows& c, int sms) {
     k_clear<<<clear_blocks(c, sms, 1), kSortBlock, 0, stream>>>(c);
@@ -392,17 +454,20 @@ cudaError_t launch_clear(cudaStream_t stream, const ClearRows& c, int sms) {
 
 cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const SortedTokens& s, const SortScratch& w,
                               const ClearRows& c, int sms) {
-    uint32_t key_bits = 1;
+    uint32_t key_bits = 1, most = 0;
     while (key_bits < 32 && t.V >> key_bits) ++key_bits;
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
+    const uint32_t passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits, digit_bits = (key_bits + passes - 1) / passes;
+    cudaError_t e = prepare_device(&most);
     if (e != cudaSuccess) return e;
-    bool done = false;         // with the fewest items per thread that a cluster can hold the batch with
-    if (t.n <= kMaxCluster * kSortBlock) e = cluster_sort<1>(stream, t, s, key_bits, device, c, sms, &done);
-    if (e == cudaSuccess && !done && t.n <= kMaxCluster * kSortBlock * 2) e = cluster_sort<2>(stream, t, s, key_bits, device, c, sms, &done);
-    if (e == cudaSuccess && !done && t.n <= kMaxCluster * kSortBlock * 4) e = cluster_sort<4>(stream, t, s, key_bits, device, c, sms, &done);
-    if (e == cudaSuccess && !done && t.n <= kMaxCluster * kSortBlock * 8) e = cluster_sort<8>(stream, t, s, key_bits, device, c, sms, &done);
-    if (e != cudaSuccess || done) return e;
+    if (t.n <= most * kSortBlock) {
+        uint32_t blocks = 1;
+        while (blocks * kSortBlock < t.n) blocks *= 2;
+        cudaLaunchAttribute attr[1];
+        cudaLaunchConfig_t cfg = cluster_launch(stream, blocks, digit_bits, attr);
+        cfg.gridDim.x += clear_blocks(c, sms, blocks);
+        return cudaLaunchKernelEx(&cfg, k_cluster_sort, t, s, key_bits, digit_bits, c);
+    }
+    if (t.n <= kMaxTiles * kSortBlock) return sort_in_tiles(stream, t, s, w, key_bits, digit_bits, c, sms);
     if (c.rows) {
         e = launch_clear(stream, c, sms);
         if (e != cudaSuccess) return e;
