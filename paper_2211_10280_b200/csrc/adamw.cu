@@ -157,15 +157,17 @@ __device__ __forceinline__ Two operator*(Two a, Two b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
     return r;
 }
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-    return r;
-}
 __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
     Two r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
     return r;
+}
+
+// A sum of products that are rounded first, and then the sum: by single additions, since the assembler contracts a packed
+// product and a packed sum into one operation, whatever their rounding modifiers say.
+__device__ __forceinline__ Two sum_of(Two a, Two b) {
+    const float2 x = a.floats(), y = b.floats();
+    return Two(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
 }
 
 __device__ __forceinline__ Two decode8(uint16_t codes, Two scale) {
@@ -300,8 +302,8 @@ __device__ __forceinline__ void step8(const Batch<kCount>& b, const Entry& t, ui
                     m[h] = decode8((uint16_t)((h < 2 ? mc.x : mc.y) >> (16 * (h & 1))), m_scale);
                     v[h] = decode8((uint16_t)((h < 2 ? vc.x : vc.y) >> (16 * (h & 1))), v_scale);
                     g[h] = g[h] * Two(grad_scale);
-                    m[h] = m[h] * Two(b.c.beta1) + g[h] * Two(b.c.rest1);
-                    v[h] = v[h] * v[h] * Two(b.c.beta2) + g[h] * g[h] * Two(b.c.rest2);
+                    m[h] = sum_of(m[h] * Two(b.c.beta1), g[h] * Two(b.c.rest1));
+                    v[h] = sum_of(v[h] * v[h] * Two(b.c.beta2), g[h] * g[h] * Two(b.c.rest2));
                 }
                 uint32_t m_low, m_top, v_low, v_top;
                 range8<false>(m, &m_low, &m_top);
@@ -473,7 +475,8 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
     return cudaSuccess;
 }
 
-constexpr int kFew = 16, kMany = 336;
+// Tensors that a launch's arguments hold: every launch copies them all, so there are three sizes (1.5, 5.8 and 30 KB).
+constexpr int kFew = 16, kSome = 64, kMany = 336;
 
 }  // namespace
 
@@ -490,6 +493,11 @@ cudaError_t launch_adamw(cudaStream_t stream, const AdamwTensor* tensors, uint32
         Batch<kFew> b;
         set(b);
         return launch_all<kFew>(stream, tensors, count, bits, b, sms);
+    }
+    if (count <= kSome) {
+        Batch<kSome> b;
+        set(b);
+        return launch_all<kSome>(stream, tensors, count, bits, b, sms);
     }
     Batch<kMany> b;
     set(b);

@@ -5,7 +5,6 @@
 #include <atomic>
 #include <cmath>
 #include <cstdio>
-#include <new>
 #include <vector>
 
 #include "context.h"
@@ -278,7 +277,7 @@ int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint
         if (!sms) return refuse(TENSAIR_ECUDA, "no CUDA device is current");
         return launched(launch_adamw((cudaStream_t)stream, list.data(), (uint32_t)list.size(), (int)state_bits, c, adamw->step,
                                      adamw->seed, sms));
-    } catch (const std::bad_alloc&) {
+    } catch (...) {      // the list could not be had
         return refuse(TENSAIR_ENOMEM, "out of host memory");
     }
 }

@@ -56,7 +56,7 @@ class Embedding:
         self.workspace_bytes = size.value
         self.workspace = torch.empty(max(1, size.value), dtype=torch.uint8, device=self.device)
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._workspace_stream = None
+        self._workspace_stream = self._workspace_user = None
         self._lib = lib
         self._tokens = B.Tokens(V=V, padding_id=_NO_PADDING if padding_id is None else padding_id, error=self.error.data_ptr())
         self._rows = [B.Rows(d=d) for _ in range(4)]
@@ -102,10 +102,10 @@ class Embedding:
         """The current stream, after the calls of another stream that may still use the workspace."""
         stream = _current_stream(self.device)
         if stream != self._workspace_stream:
-            if self._workspace_stream is not None and not torch.cuda.is_current_stream_capturing():
-                last = torch.cuda.ExternalStream(self._workspace_stream, self.device)
-                torch.cuda.current_stream(self.device).wait_stream(last)
-            self._workspace_stream = stream
+            now = torch.cuda.current_stream(self.device)
+            if self._workspace_user is not None and not torch.cuda.is_current_stream_capturing():
+                now.wait_stream(self._workspace_user)
+            self._workspace_stream, self._workspace_user = stream, now
         return stream
 
     # ---- calls
@@ -202,6 +202,7 @@ class _Lookup(torch.autograd.Function):
         return embedding.lookup(table, ids)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         ids, = ctx.saved_tensors
         return ctx.embedding.gradient(grad, ids, dtype=ctx.dtype), None, None
@@ -276,7 +277,7 @@ class AdamW:
         self._lib = B.lib()
         self._hyper = B.Adamw()
         self._at = C.byref(self._hyper)
-        self._kinds, self._left_out = None, []     # what the descriptors say now
+        self._said, self._left_out = [None, None, None], []
         self._numel = [p.numel() for p in params]
 
     def _fits(self, x, n, dtypes, name):
@@ -303,11 +304,15 @@ class AdamW:
                 or [g.get_device() for g in grads] != [index] * len(grads)):
             for i, g in enumerate(grads):
                 self._fits(g, self._numel[i], _FLOATS, f"grads[{i}]")
-        a = self._np
-        a["grad"] = [g.data_ptr() for g in grads]
-        a["param"] = [p.data_ptr() for p in self.params]
-        if kinds != self._kinds:
-            a["grad_type"] = self._kinds = kinds
+        a, said = self._np, self._said             # what the descriptors say is written again only where it changed
+        ptrs = [g.data_ptr() for g in grads]
+        if ptrs != said[0]:
+            a["grad"] = said[0] = ptrs
+        ptrs = [p.data_ptr() for p in self.params]
+        if ptrs != said[1]:
+            a["param"] = said[1] = ptrs
+        if kinds != said[2]:
+            a["grad_type"] = said[2] = kinds
         if left_out != self._left_out:
             a["n"] = self._numel
             a["n"][left_out] = 0

@@ -462,6 +462,27 @@ def test_adamw_with_8_bit_moments(param_type, grad_type, off):
 
 
 @gpu
+def test_8_bit_moments_are_those_of_separately_rounded_operations():
+    """Every product, sum, root and quotient that leads to what is stored is one rounded fp32 operation: the scales have the bits
+    that a program of separate operations gives, starting each step from what the step before stored."""
+    n = 256 * 400
+    g = _rand((n,), BF16, 1e-3)
+    for beta1, beta2 in ((0.0, 0.0), (0.9, 0.999)):
+        opt = _ops().AdamW([torch.zeros(n, device="cuda")], state_bits=8, betas=(beta1, beta2))
+        m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        for _ in range(3):
+            opt.step([g])
+            x = g.float()
+            m = m * beta1 + x * (1 - beta1)
+            v = v * beta2 + (x * x) * (1 - beta2)
+            for kept, scale in ((m, opt.m_scale[0]), (v.sqrt(), opt.v_scale[0])):
+                assert torch.equal(scale, kept.abs().view(-1, 256).amax(1) * torch.tensor(1 / 448, dtype=torch.float32))
+            # what the next step starts from
+            m = (opt.m[0].float().view(-1, 256) * opt.m_scale[0][:, None]).view(-1)
+            v = (opt.v[0].float().view(-1, 256) * opt.v_scale[0][:, None]).view(-1).square()
+
+
+@gpu
 def test_8_bit_second_moments_follow_a_gradient_that_changes():
     n = 256 * 64
     p = [torch.zeros(n, device="cuda")]
@@ -526,6 +547,21 @@ def test_calls_of_two_streams_and_of_a_graph():
     torch.cuda.synchronize()
     _ops().AdamW(q, state_bits=32).step(g)
     assert torch.equal(out, want) and torch.equal(rows, want_rows) and torch.equal(p[0], q[0])
+
+
+# ---------------------------------------------------------------- the example
+@gpu
+@pytest.mark.parametrize("state_bits,dense", [(8, False), (32, False), (32, True)])
+def test_next_token_model_learns_from_streamed_embeddings(state_bits, dense):
+    from paper_2211_10280_b200 import next_token
+
+    r = next_token.train(steps=60, V=1000, rows=512, state_bits=state_bits, dense=dense, report=30)
+    # a uniform guess costs ln 1000 = 6.9; the stream's own entropy is under 0.3 * 6.9 + 0.7 = 2.8
+    assert abs(r["losses"][0] - 6.9) < 1.5 and r["losses"][-1] < r["losses"][0] - 0.5
+    unseen = ~r["seen"]
+    if unseen.any():
+        assert torch.equal(r["after"][unseen], r["before"][unseen])
+    assert not torch.equal(r["after"][r["seen"]], r["before"][r["seen"]])
 
 
 # ---------------------------------------------------------------- refusals
