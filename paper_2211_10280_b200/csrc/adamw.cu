@@ -475,8 +475,9 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
     return cudaSuccess;
 }
 
-// Tensors that a launch's arguments hold: every launch copies them all, so there are three sizes (1.5, 5.8 and 30 KB).
-constexpr int kFew = 16, kSome = 64, kMany = 336;
+// Tensors that a launch's arguments hold: every launch copies them all, so there are four sizes (1.6, 3, 6 and 30 KB;
+// a launch takes some 0.6 us per KB).
+constexpr int kFew = 16, kSome = 32, kMore = 64, kMany = 336;
 
 }  // namespace
 
@@ -498,6 +499,11 @@ cudaError_t launch_adamw(cudaStream_t stream, const AdamwTensor* tensors, uint32
         Batch<kSome> b;
         set(b);
         return launch_all<kSome>(stream, tensors, count, bits, b, sms);
+    }
+    if (count <= kMore) {
+        Batch<kMore> b;
+        set(b);
+        return launch_all<kMore>(stream, tensors, count, bits, b, sms);
     }
     Batch<kMany> b;
     set(b);

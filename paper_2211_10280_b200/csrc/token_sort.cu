@@ -128,14 +128,10 @@ constexpr size_t cluster_shared_bytes(size_t bins, size_t blocks) {
 }
 
 __global__ void __launch_bounds__(kSortBlock, 1)
-k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bits, ClearRows clear) {
+k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bits) {
     cg::cluster_group cluster = cg::this_cluster();
     let_next_launch_begin();
     const uint32_t rank = cluster.block_rank(), blocks = cluster.num_blocks();
-    if (blockIdx.x >= blocks) {     // the first cluster sorts; the others clear beside it
-        clear_part(clear, blockIdx.x - blocks, gridDim.x - blocks);
-        return;
-    }
     extern __shared__ __align__(16) uint8_t raw[];
     const uint32_t bins = 1u << digit_bits, mask = bins - 1, tid = threadIdx.x;
     ClusterShared& sh = *reinterpret_cast<ClusterShared*>(raw);
@@ -196,21 +192,29 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
         s.info[2] = s.info[3] = 0;
         s.seg_start[all_heads] = all_valid;
     }
+    after_previous_launch();     // the launch that clears the table, if there is one, has run beside this one and ends with it
 }
 
-// ---- in several launches.  A tile is the 1,024 items of a block; hist: [tile][digit], 16 bits each.
+// ---- in several launches.  Each takes a share of the rows to clear: its blocks past the tiles clear beside the others.
+struct ClearShare {
+    ClearRows rows;
+    uint32_t share, shares;
+    __device__ __forceinline__ void run(uint32_t tiles) const {
+        const uint64_t blocks = gridDim.x - tiles;
+        clear_part(rows, share * blocks + blockIdx.x - tiles, shares * blocks);
+    }
+};
+
+// A tile is the 1,024 items of a block; hist: [tile][digit], 16 bits each.
 // Ranks the tile's items of a pass by digit: place[i] is the rank among the tile's items of its digit.
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortBlock)
 k_tile_rank(TokenIds t, const uint2* __restrict__ items, uint2* __restrict__ out, uint16_t* __restrict__ place, uint32_t* __restrict__ hist,
-            uint32_t shift, uint32_t digit_bits, uint32_t tiles, ClearRows clear) {
+            uint32_t shift, uint32_t digit_bits, uint32_t tiles, ClearShare clear) {
     extern __shared__ __align__(16) uint32_t counts[];
     let_next_launch_begin();
     if (!kFirst) after_previous_launch();
-    if (kFirst && blockIdx.x >= tiles) {
-        clear_part(clear, blockIdx.x - tiles, gridDim.x - tiles);
-        return;
-    }
+    if (blockIdx.x >= tiles) return clear.run(tiles);
     const uint32_t at = blockIdx.x * kSortBlock + threadIdx.x, pairs = 1u << digit_bits >> 1;
     uint32_t key = 0xFFFFFFFFu;
     if (at < t.n) {
@@ -226,11 +230,12 @@ k_tile_rank(TokenIds t, const uint2* __restrict__ items, uint2* __restrict__ out
 template <bool kLast>
 __global__ void __launch_bounds__(kSortBlock)
 k_tile_scatter(uint32_t n, const uint2* __restrict__ items, uint2* __restrict__ out, const uint16_t* __restrict__ place,
-               const uint16_t* __restrict__ hist, uint32_t shift, uint32_t digit_bits, uint32_t tiles, SortedTokens s) {
+               const uint16_t* __restrict__ hist, uint32_t shift, uint32_t digit_bits, uint32_t tiles, SortedTokens s, ClearShare clear) {
     __shared__ uint32_t base[1 << kMaxDigitBits], warp_sums[kSortBlockWarps];
     let_next_launch_begin();
     const uint32_t tid = threadIdx.x, at = blockIdx.x * kSortBlock + tid, bins = 1u << digit_bits;
     after_previous_launch();
+    if (blockIdx.x >= tiles) return clear.run(tiles);
     uint2 item = make_uint2(0, 0);
     uint32_t rank = 0;
     if (at < n) {
@@ -259,11 +264,12 @@ k_tile_scatter(uint32_t n, const uint2* __restrict__ items, uint2* __restrict__ 
 
 // Lists the tokens of the sorted positions.  A block counts the tokens that begin before it from the keys themselves.
 __global__ void __launch_bounds__(kSortBlock)
-k_list_tokens(uint32_t n, uint32_t V, SortedTokens s) {
+k_list_tokens(uint32_t n, uint32_t V, uint32_t tiles, SortedTokens s, ClearShare clear) {
     __shared__ uint32_t warp_sums[kSortBlockWarps];
     let_next_launch_begin();
     const uint32_t tid = threadIdx.x, first = blockIdx.x * kSortBlock, at = first + tid;
     after_previous_launch();
+    if (blockIdx.x >= tiles) return clear.run(tiles);
     uint32_t c = 0;
     const uint4* keys = reinterpret_cast<const uint4*>(s.key);
 #pragma unroll 8
@@ -292,14 +298,12 @@ k_list_tokens(uint32_t n, uint32_t V, SortedTokens s) {
     }
 }
 
-// Blocks that clear: one per 64 KB, at most four per multiprocessor (they are handed out as others end), in whole clusters.
-uint32_t clear_blocks(const ClearRows& c, int sms, uint32_t cluster) {
-    if (!c.rows) return 0;
-    const uint64_t want = (c.rows * c.width + 65535) / 65536, most = (uint64_t)sms * 4;
-    return (uint32_t)(((want < most ? want : most) + cluster - 1) / cluster * cluster);
+// A few blocks per multiprocessor clear all: they start at once, so the launch that follows can run beside them.
+constexpr int kClearThreads = 512;
+__global__ void __launch_bounds__(kClearThreads) k_clear(ClearRows c) {
+    let_next_launch_begin();
+    clear_part(c, blockIdx.x, gridDim.x);
 }
-
-__global__ void __launch_bounds__(kSortBlock) k_clear(ClearRows c) { clear_part(c, blockIdx.x, gridDim.x); }
 
 cudaLaunchConfig_t cluster_launch(cudaStream_t stream, uint32_t blocks, uint32_t digit_bits, cudaLaunchAttribute* attr) {
     attr->id = cudaLaunchAttributeClusterDimension;
@@ -348,24 +352,28 @@ cudaError_t sort_in_tiles(cudaStream_t stream, const TokenIds& t, const SortedTo
     uint2* from = reinterpret_cast<uint2*>(w.a);
     uint2* to = reinterpret_cast<uint2*>(w.b);
     uint16_t* place = reinterpret_cast<uint16_t*>(w.tile_counts);
+    const uint32_t passes = (key_bits + digit_bits - 1) / digit_bits;
+    ClearShare share{clear, 0, 2 * passes + 1};
+    const uint32_t grid = tiles + (clear.rows ? (uint32_t)sms : 0u);
     for (uint32_t shift = 0; shift < key_bits; shift += digit_bits) {
         cudaError_t e;
         if (shift == 0) {
-            k_tile_rank<true><<<tiles + clear_blocks(clear, sms, 1), kSortBlock, counts, stream>>>(t, nullptr, from, place, w.hist, shift,
-                                                                                                  digit_bits, tiles, clear);
+            k_tile_rank<true><<<grid, kSortBlock, counts, stream>>>(t, nullptr, from, place, w.hist, shift, digit_bits, tiles, share);
             e = cudaGetLastError();
         } else {
-            e = launch_early(k_tile_rank<false>, tiles, kSortBlock, counts, stream, t, (const uint2*)from, to, place, w.hist, shift,
-                             digit_bits, tiles, ClearRows{});
+            e = launch_early(k_tile_rank<false>, grid, kSortBlock, counts, stream, t, (const uint2*)from, to, place, w.hist, shift,
+                             digit_bits, tiles, share);
         }
+        ++share.share;
         if (e != cudaSuccess) return e;
         auto scatter = shift + digit_bits < key_bits ? k_tile_scatter<false> : k_tile_scatter<true>;
-        e = launch_early(scatter, tiles, kSortBlock, 0, stream, t.n, (const uint2*)from, to, (const uint16_t*)place, (const uint16_t*)w.hist, shift,
-                         digit_bits, tiles, s);
+        e = launch_early(scatter, grid, kSortBlock, 0, stream, t.n, (const uint2*)from, to, (const uint16_t*)place,
+                         (const uint16_t*)w.hist, shift, digit_bits, tiles, s, share);
+        ++share.share;
         if (e != cudaSuccess) return e;
         std::swap(from, to);
     }
-    return launch_early(k_list_tokens, tiles, kSortBlock, 0, stream, t.n, t.V, s);
+    return launch_early(k_list_tokens, grid, kSortBlock, 0, stream, t.n, t.V, tiles, s, share);
 }
 
 // ---- larger batches
@@ -448,7 +456,7 @@ SortScratchBytes sort_scratch_bytes(uint32_t n) {
 }
 
 cudaError_t launch_clear(cudaStream_t stream, const ClearRows& c, int sms) {
-    k_clear<<<clear_blocks(c, sms, 1), kSortBlock, 0, stream>>>(c);
+    k_clear<<<sms, kClearThreads, 0, stream>>>(c);
     return cudaGetLastError();
 }
 
@@ -462,10 +470,16 @@ cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const Sort
     if (t.n <= most * kSortBlock) {
         uint32_t blocks = 1;
         while (blocks * kSortBlock < t.n) blocks *= 2;
-        cudaLaunchAttribute attr[1];
+        cudaLaunchAttribute attr[2];
         cudaLaunchConfig_t cfg = cluster_launch(stream, blocks, digit_bits, attr);
-        cfg.gridDim.x += clear_blocks(c, sms, blocks);
-        return cudaLaunchKernelEx(&cfg, k_cluster_sort, t, s, key_bits, digit_bits, c);
+        if (c.rows) {          // beside the launch that clears
+            e = launch_clear(stream, c, sms);
+            if (e != cudaSuccess) return e;
+            attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[1].val.programmaticStreamSerializationAllowed = 1;
+            cfg.numAttrs = 2;
+        }
+        return cudaLaunchKernelEx(&cfg, k_cluster_sort, t, s, key_bits, digit_bits);
     }
     if (t.n <= kMaxTiles * kSortBlock) return sort_in_tiles(stream, t, s, w, key_bits, digit_bits, c, sms);
     if (c.rows) {

@@ -298,13 +298,12 @@ class AdamW:
             grads = list(grads)
             for i in left_out:
                 grads[i] = self.params[i]          # stands in for the checks; its n is set to 0
-        index = self.device.index
-        kinds = [_FLOATS.get(g.dtype) for g in grads]
-        if ([g.numel() for g in grads] != self._numel or None in kinds or False in [g.is_contiguous() for g in grads]
+        index, a, said = self.device.index, self._np, self._said     # what the descriptors say is written again only where it changed
+        kinds = [g.dtype for g in grads]
+        if ([g.numel() for g in grads] != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds)) or False in [g.is_contiguous() for g in grads]
                 or [g.get_device() for g in grads] != [index] * len(grads)):
             for i, g in enumerate(grads):
                 self._fits(g, self._numel[i], _FLOATS, f"grads[{i}]")
-        a, said = self._np, self._said             # what the descriptors say is written again only where it changed
         ptrs = [g.data_ptr() for g in grads]
         if ptrs != said[0]:
             a["grad"] = said[0] = ptrs
@@ -312,7 +311,8 @@ class AdamW:
         if ptrs != said[1]:
             a["param"] = said[1] = ptrs
         if kinds != said[2]:
-            a["grad_type"] = said[2] = kinds
+            said[2] = kinds
+            a["grad_type"] = [_FLOATS[k] for k in kinds]
         if left_out != self._left_out:
             a["n"] = self._numel
             a["n"][left_out] = 0
