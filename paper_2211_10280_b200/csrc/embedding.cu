@@ -19,10 +19,11 @@ constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;     // 65,536 rows of 300 floats: 25 us; 31 with 1, 25.5 with 2, 29 with 8
 
 // out[i] = scale * table[ids[i]]; a thread moves kLookupUnroll vectors of E elements, a block's width apart.
-template <typename TT, typename TO, int E>
+template <typename TT, typename TO, typename C>
 __global__ void __launch_bounds__(kLookupThreads)
 k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table_stride, TO* __restrict__ out,
-         uint64_t out_stride, FastDiv vecs, uint32_t total, float scale) {
+         uint64_t out_stride, FastDiv vecs, uint32_t d, uint32_t total, float scale) {
+    constexpr int E = C::E;
     const uint32_t base = blockIdx.x * (kLookupThreads * kLookupUnroll) + threadIdx.x;
     Pack<TT, E> x[kLookupUnroll];
     uint32_t row[kLookupUnroll], col[kLookupUnroll];
@@ -38,7 +39,7 @@ k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table
             const int64_t id = t.wide ? __ldg(reinterpret_cast<const long long*>(t.ids) + row[u])
                                       : __ldg(reinterpret_cast<const int32_t*>(t.ids) + row[u]);
             held[u] = id != t.padding && (uint64_t)id < t.V;
-            if (held[u]) x[u] = load_pack<TT, E>(table + (uint64_t)id * table_stride + col[u]);
+            if (held[u]) x[u] = load_columns<C>(table + (uint64_t)id * table_stride + col[u], d - col[u]);
             else if (id != t.padding && t.err) atomicOr(t.err, kErrBadToken);
         }
     }
@@ -48,7 +49,7 @@ k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table
         float y[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) y[e] = held[u] ? to_float(x[u].v[e]) * scale : 0.0f;
-        store_pack<TO, E>(out + (uint64_t)row[u] * out_stride + col[u], y);
+        store_columns<C>(out + (uint64_t)row[u] * out_stride + col[u], y, d - col[u]);
     }
 }
 
@@ -76,16 +77,16 @@ cudaError_t with_type(uint32_t type, F&& f) {
         default: return f(__half());
     }
 }
-template <int E> struct Width { static constexpr int value = E; };
 template <typename F>
-cudaError_t with_width(uint32_t e, F&& f) {
+cudaError_t with_columns(uint32_t e, F&& f) {
     switch (e) {
-        case 8: return f(Width<8>());
-        case 4: return f(Width<4>());
-        case 2: return f(Width<2>());
-        default: return f(Width<1>());
+        case 8: return f(Columns<8, false>());
+        case 4: return f(Columns<4, false>());
+        case 2: return f(Columns<2, false>());
+        default: return f(Columns<4, true>());
     }
 }
+uint32_t pieces_of(uint32_t d, uint32_t e) { return e > 1 ? d / e : (d + 3) / 4; }
 
 constexpr uint32_t kMaxItems = 0x7FFFFFFFu;   // vectors per launch, so that their numbers stay below 2^31
 
@@ -95,18 +96,18 @@ cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView
                           float scale) {
     uint32_t e = vector_of(table, d, widest(table, out));
     e = vector_of(out, d, e);
-    const FastDiv vecs(d / e);
+    const FastDiv vecs(pieces_of(d, e));
     const uint32_t most = kMaxItems / vecs.divisor;     // rows of one launch
     for (uint32_t row0 = 0; row0 < t.n; row0 += most) {
         const uint32_t total = (t.n - row0 < most ? t.n - row0 : most) * vecs.divisor;
         const uint32_t grid = (uint32_t)(((uint64_t)total + kLookupThreads * kLookupUnroll - 1) / (kLookupThreads * kLookupUnroll));
         const cudaError_t err = with_type(table.type, [&](auto tt) {
             return with_type(out.type, [&](auto to) {
-                return with_width(e, [&](auto w) {
+                return with_columns(e, [&](auto c) {
                     using TT = decltype(tt);
                     using TO = decltype(to);
-                    k_lookup<TT, TO, decltype(w)::value><<<grid, kLookupThreads, 0, stream>>>(
-                        t, row0, (const TT*)table.data, table.stride, (TO*)out.data, out.stride, vecs, total, scale);
+                    k_lookup<TT, TO, decltype(c)><<<grid, kLookupThreads, 0, stream>>>(
+                        t, row0, (const TT*)table.data, table.stride, (TO*)out.data, out.stride, vecs, d, total, scale);
                     return cudaGetLastError();
                 });
             });
@@ -129,17 +130,18 @@ constexpr int kJoinWarps = kJoinThreads / 32;
 
 // What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
 // several tokens' reads are in flight before the first is needed; put() joins and stores.
-template <SumKind kKind, typename TO, int E>
+template <SumKind kKind, typename TO, typename C>
 struct Finish {
+    static constexpr int E = C::E;
     Pack<TO, E> old;
     Pack<float, E> m0, v0;
 
     __device__ __forceinline__ void fetch(const SumArgs& a, uint32_t key, uint32_t col) {
         if (kKind == kSumRows || (kKind == kSumTable && !a.accumulate)) return;
-        old = load_pack<TO, E>((const TO*)a.out.data + (uint64_t)key * a.out.stride + col);
+        old = load_columns<C>((const TO*)a.out.data + (uint64_t)key * a.out.stride + col, a.d - col);
         if (kKind == kSumAdamw) {
-            m0 = load_pack<float, E>(a.m + (uint64_t)key * a.m_stride + col);
-            v0 = load_pack<float, E>(a.v + (uint64_t)key * a.v_stride + col);
+            m0 = load_columns<C>(a.m + (uint64_t)key * a.m_stride + col, a.d - col);
+            v0 = load_columns<C>(a.v + (uint64_t)key * a.v_stride + col, a.d - col);
         }
     }
     __device__ __forceinline__ void put(const SumArgs& a, float grad_scale, uint32_t key, uint32_t rank, uint32_t col,
@@ -162,17 +164,18 @@ struct Finish {
                 v[e] = v0.v[e];
                 y[e] = adamw_update(to_float(old.v[e]), y[e] * grad_scale, m[e], v[e], a.adamw, a.adamw.step_size, a.adamw.keep);
             }
-            store_pack<float, E>(a.m + (uint64_t)key * a.m_stride + col, m);
-            store_pack<float, E>(a.v + (uint64_t)key * a.v_stride + col, v);
+            store_columns<C>(a.m + (uint64_t)key * a.m_stride + col, m, a.d - col);
+            store_columns<C>(a.v + (uint64_t)key * a.v_stride + col, v, a.d - col);
         }
-        store_pack<TO, E>(out, y);
+        store_columns<C>(out, y, a.d - col);
     }
 };
 
 
-template <SumKind kKind, typename TG, typename TO, int E>
+template <SumKind kKind, typename TG, typename TO, typename C>
 __global__ void __launch_bounds__(kSumThreads)
-k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
+k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab_vecs) {
+    constexpr int E = C::E;
     // gradient vectors in flight per thread; few registers, and so many threads, are worth more where a vector or a finished
     // row takes many
     constexpr int kSumBatch = kKind == kSumAdamw || E == 8 ? 2 : 4;
@@ -182,7 +185,7 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
     __shared__ uint32_t pos[kSpan + kWindow], head_masks[kSpan / 32], part_masks[kSpan / 32];
     let_next_launch_begin();
     const uint32_t tid = threadIdx.x, begin = blockIdx.x * kSpan;
-    const uint32_t vec0 = blockIdx.y * slab_vecs, all_vecs = a.d / E;
+    const uint32_t vec0 = blockIdx.y * slab_vecs;
     const uint32_t vecs = all_vecs - vec0 < slab_vecs ? all_vecs - vec0 : slab_vecs;
     after_previous_launch();
     float grad_scale = 1.0f;
@@ -250,8 +253,8 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
         const uint32_t from = p.x & 0xFF, count = p.x >> 8 & 0xFF, what = p.x >> 16 & 0xFF;
         const uint32_t col = (vec0 + vec) * E;
         const TG* grad = (const TG*)a.grad.data + col;
-        Finish<kKind, TO, E> row;
-        const Pack<TG, E> x0 = load_pack<TG, E>(grad + (uint64_t)pos[from] * a.grad.stride);
+        Finish<kKind, TO, C> row;
+        const Pack<TG, E> x0 = load_columns<C>(grad + (uint64_t)pos[from] * a.grad.stride, a.d - col);
         if (what == kWholeToken) row.fetch(a, p.y, col);
         float sum[E];
 #pragma unroll
@@ -260,7 +263,7 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
             Pack<TG, E> x[kSumBatch];
 #pragma unroll
             for (int j = 0; j < kSumBatch; ++j)
-                if (i + j < count) x[j] = load_pack<TG, E>(grad + (uint64_t)pos[from + i + j] * a.grad.stride);
+                if (i + j < count) x[j] = load_columns<C>(grad + (uint64_t)pos[from + i + j] * a.grad.stride, a.d - col);
 #pragma unroll
             for (int j = 0; j < kSumBatch; ++j)
                 if (i + j < count)
@@ -278,9 +281,10 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t slab_vecs) {
 // Joins the pieces of the tokens with more than kWindow positions: slot 1 of the window a token begins in, then slot 0 of the
 // windows that follow.  A token with few pieces takes a warp for each 32 vectors of columns, one with many takes a block, whose
 // warps each add a stretch of the pieces.
-template <SumKind kKind, typename TO, int E>
+template <SumKind kKind, typename TO, typename C>
 __global__ void __launch_bounds__(kJoinThreads)
 k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
+    constexpr int E = C::E;
     __shared__ float join[kJoinWarps][32 * E + 1];
     after_previous_launch();
     float grad_scale = 1.0f;
@@ -300,7 +304,7 @@ k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
         const uint32_t share = shared ? (rest + kJoinWarps - 1) / kJoinWarps : rest;
         const uint32_t from = shared ? wid * share : 0, to = from + share < rest ? from + share : rest;
         const bool first = in && col < a.d && (!shared || wid == 0);
-        Finish<kKind, TO, E> row;
+        Finish<kKind, TO, C> row;
         float sum[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[e] = 0.0f;
@@ -336,9 +340,9 @@ k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
 
 }  // namespace
 
-template <SumKind kKind, typename TG, typename TO, int E>
+template <SumKind kKind, typename TG, typename TO, typename C>
 static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a, int sms) {
-    const uint32_t spans = (a.n + kSpan - 1) / kSpan, vecs = a.d / E;
+    const uint32_t spans = (a.n + kSpan - 1) / kSpan, vecs = (a.d + C::E - 1) / C::E;
     // enough blocks to go round, as long as a block's slab keeps a few vectors
     uint32_t slabs = (uint32_t)sms * kSumBlocks / spans + 1;
     const uint32_t most = (vecs + 15) / 16;
@@ -346,12 +350,12 @@ static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a, int sms) {
     if (slabs < vecs / 65536 + 1) slabs = vecs / 65536 + 1;
     const uint32_t slab_vecs = (vecs + slabs - 1) / slabs;
     slabs = (vecs + slab_vecs - 1) / slab_vecs;
-    const cudaError_t e = launch_early(k_token_sums<kKind, TG, TO, E>, dim3(spans, slabs), kSumThreads, 0, stream, a, slab_vecs);
+    const cudaError_t e = launch_early(k_token_sums<kKind, TG, TO, C>, dim3(spans, slabs), kSumThreads, 0, stream, a, vecs, slab_vecs);
     if (e != cudaSuccess || a.n <= kWindow) return e;
     const uint32_t join_slabs = (vecs + 31) / 32;
     uint64_t blocks = (uint64_t)(a.n / (kWindow + 1)) * join_slabs;
     if (blocks > (uint64_t)sms * 4) blocks = (uint64_t)sms * 4;
-    return launch_early(k_join_pieces<kKind, TO, E>, dim3((uint32_t)blocks), kJoinThreads, 0, stream, a, join_slabs);
+    return launch_early(k_join_pieces<kKind, TO, C>, dim3((uint32_t)blocks), kJoinThreads, 0, stream, a, join_slabs);
 }
 
 cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms) {
@@ -363,13 +367,13 @@ cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& 
     }
     return with_type(a.grad.type, [&](auto tg) {
         return with_type(a.out.type, [&](auto to) {
-            return with_width(e, [&](auto w) {
+            return with_columns(e, [&](auto c) {
                 using TG = decltype(tg);
                 using TO = decltype(to);
-                constexpr int E = decltype(w)::value;
-                if (kind == kSumAdamw) return launch_sums<kSumAdamw, TG, TO, E>(stream, a, sms);
-                if (kind == kSumTable) return launch_sums<kSumTable, TG, TO, E>(stream, a, sms);
-                if constexpr (sizeof(TO) == 4) return launch_sums<kSumRows, TG, TO, E>(stream, a, sms);
+                using C = decltype(c);
+                if (kind == kSumAdamw) return launch_sums<kSumAdamw, TG, TO, C>(stream, a, sms);
+                if (kind == kSumTable) return launch_sums<kSumTable, TG, TO, C>(stream, a, sms);
+                if constexpr (sizeof(TO) == 4) return launch_sums<kSumRows, TG, TO, C>(stream, a, sms);
                 else return cudaErrorInvalidValue;
             });
         });

@@ -46,6 +46,35 @@ __device__ __forceinline__ void store_pack(T* p, const float (&x)[E]) {
     *reinterpret_cast<Pack<T, E>*>(p) = out;
 }
 
+// How rows are cut into the pieces that a thread moves at once: E columns in one access (or two of 16 bytes), where every row
+// begins on a multiple of it; or, for rows of odd widths or places, four columns in an access each, `left` of which are inside
+// the row.  Four to a thread all the same: what it does per piece is worth more than the accesses, whose cache lines its
+// neighbours share.
+template <int kColumns, bool kIsRagged>
+struct Columns {
+    static constexpr int E = kColumns;
+    static constexpr bool kRagged = kIsRagged;
+};
+template <typename C, typename T>
+__device__ __forceinline__ Pack<T, C::E> load_columns(const T* p, uint32_t left) {
+    if constexpr (!C::kRagged) return load_pack<T, C::E>(p);
+    else {
+        Pack<T, C::E> x;
+#pragma unroll
+        for (int e = 0; e < C::E; ++e) x.v[e] = e < (int)left ? p[e] : from_float<T>(0.0f);
+        return x;
+    }
+}
+template <typename C, typename T>
+__device__ __forceinline__ void store_columns(T* p, const float (&x)[C::E], uint32_t left) {
+    if constexpr (!C::kRagged) store_pack<T, C::E>(p, x);
+    else {
+#pragma unroll
+        for (int e = 0; e < C::E; ++e)
+            if (e < (int)left) p[e] = from_float<T>(x[e]);
+    }
+}
+
 // Eight floats in one 32-byte access (sm_100 has them), where the address is a multiple of 32.
 __device__ __forceinline__ void load_eight(const float* p, float (&x)[8]) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
