@@ -2,7 +2,9 @@
 //
 // The tensors' descriptors travel as the kernel's argument block (up to 32 KB), so a step copies nothing to the device
 // and keeps no plan: a block finds its tensor by a binary search in constant memory.  The update itself is one pass:
-// every element of the parameter, the gradient and the moments is read once and written once.  It is bound by memory.
+// every element of the parameter, the gradient and the moments is read once and written once.  With 32-bit moments it is
+// bound by memory: 96 M elements (fp32, bf16 gradients and a bf16 copy, 28 bytes each) take 395 us, 6.8 TB/s, which is the
+// rate of a plain copy.  A small model is bound by the launch (200,000 elements: 4.2 us).
 //
 // Moments in 8 bits.  A block of 256 elements, one warp's work, shares one fp32 scale per moment; stored are m / scale and
 // sqrt(v) / scale in e4m3, with scale = largest magnitude / 448.  The square root halves the exponent range v
@@ -13,6 +15,12 @@
 // (it would be divided by eps alone): it keeps at least the smallest e4m3 value.  Magnitudes in e4m3's subnormal
 // range, below 2^-14 of the block's largest, round to nearest.  Non-finite elements are stored as NaN and leave the
 // block's scale alone, so they stay where they are, as in 32 bits.
+//
+// With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 52 instructions, so the kernel is bound by
+// their issue and latency before memory: 128 M elements take 400 us, 4.5 TB/s (0.69 of the copy rate), at 2.1 instructions
+// per cycle of 4.  What made it so (547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate
+// quotients in the update, Philox with its round keys in the arguments, one vote per block for the rare cases, 64 registers
+// for four blocks per multiprocessor.  Copying the next blocks ahead through shared memory made it slower (443 us).
 #include "adamw.cuh"
 #include "operators.h"
 #include "philox.cuh"
