@@ -10,8 +10,7 @@
 //
 // What bounds it, 65,536 tokens of a Zipf vocabulary of 1 M, d = 300: scattered rows of 1,200 bytes.  Rows (fp32): 28 us for
 // 112 MB.  AdamW (bf16 gradients, fp32 table and moments): 50 us for 237 MB, 4.7 TB/s; the reads and writes of those rows
-// alone, in a kernel that does nothing else, take 45 us.  Two or four gradient vectors in flight per thread and many threads
-// do better than more of them (eight: 28 -> 38 us), and shared memory is kept small because the reads in flight live in the
+// alone, in a kernel that does nothing else, take 45 us.  Shared memory is kept small because the reads in flight live in the
 // level-1 cache beside it (40 KB per block: +14 us).  A short batch is bound by the latency of the launches: 4,096 tokens of
 // 128 floats take 18 us in all, of which the sort takes 9.
 #include "adamw.cuh"
@@ -137,6 +136,8 @@ constexpr uint32_t kFewPieces = 8;     // after the first
 constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;
 
+template <int kCount> struct Rows { static constexpr int value = kCount; };
+
 // What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
 // several tokens' reads are in flight before the first is needed; put() joins and stores.
 template <SumKind kKind, typename TO, typename C>
@@ -185,9 +186,6 @@ template <SumKind kKind, typename TG, typename TO, typename C>
 __global__ void __launch_bounds__(kSumThreads)
 k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab_vecs) {
     constexpr int E = C::E;
-    // gradient vectors in flight per thread; few registers, and so many threads, are worth more where a vector or a finished
-    // row takes many
-    constexpr int kSumBatch = kKind == kSumAdamw || E == 8 ? 2 : 4;      // dense bf16, 16,384 tokens of 512: 47 us with 2, 51 with 4
     // What the block adds up, in order: (first position | rows << 8 | SumPart << 16 | piece's window << 24, token, rank).
     // No large shared arrays: the reads in flight need the level-1 cache, which shares its memory with them.
     __shared__ __align__(16) uint4 parts[kMaxParts];
@@ -263,22 +261,27 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
         const uint32_t col = (vec0 + vec) * E;
         const TG* grad = (const TG*)a.grad.data + col;
         Finish<kKind, TO, C> row;
-        const Pack<TG, E> x0 = load_columns<C>(grad + (uint64_t)pos[from] * a.grad.stride, a.d - col);
         if (what == kWholeToken) row.fetch(a, p.y, col);
         float sum[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = to_float(x0.v[e]);
-        for (uint32_t i = 1; i < count; i += kSumBatch) {
-            Pack<TG, E> x[kSumBatch];
+        for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+        auto add = [&](uint32_t i, auto batch) {
+            constexpr int kRows = decltype(batch)::value;
+            Pack<TG, E> x[kRows];
 #pragma unroll
-            for (int j = 0; j < kSumBatch; ++j)
-                if (i + j < count) x[j] = load_columns<C>(grad + (uint64_t)pos[from + i + j] * a.grad.stride, a.d - col);
+            for (int j = 0; j < kRows; ++j) x[j] = load_columns<C>(grad + (uint64_t)pos[from + i + j] * a.grad.stride, a.d - col);
 #pragma unroll
-            for (int j = 0; j < kSumBatch; ++j)
-                if (i + j < count)
+            for (int j = 0; j < kRows; ++j)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
-        }
+                for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
+        };
+        // whole batches, then what is left in halves: no access is guarded, and few are waited for alone
+        constexpr int kWhole = kKind == kSumAdamw ? 8 : 4;
+        uint32_t i = 0;
+        for (; i + kWhole <= count; i += kWhole) add(i, Rows<kWhole>());
+        if (kWhole > 4 && i + 4 <= count) { add(i, Rows<4>()); i += 4; }
+        if (i + 2 <= count) { add(i, Rows<2>()); i += 2; }
+        if (i < count) add(i, Rows<1>());
         if (what == kWholeToken) row.put(a, grad_scale, p.y, p.z, col, sum);
         else {
             const uint64_t slot = ((uint64_t)blockIdx.x * (kSpan / kWindow) + (p.x >> 24)) * 2 + (what == kPiece1);

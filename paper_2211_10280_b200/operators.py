@@ -22,15 +22,16 @@ _FLOATS = {torch.float32: B.FLOAT32, torch.bfloat16: B.BFLOAT16, torch.float16: 
 _INTS = {torch.int32: B.INT32, torch.int64: B.INT64}
 # the current stream's handle without a Stream object around it (2 us of a call that takes 10)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _NO_PADDING = -(1 << 63)
 BLOCK = 256                      # elements that share a scale of the 8-bit moments
 
 
-def _current_stream(device) -> int:
-    """The cudaStream_t of the current stream of `device`, which has to be the current device."""
-    if torch.cuda.current_device() != device.index:
-        raise ValueError(f"the tensors' device {device} is not the current one")
-    return _raw_stream(device.index)
+def _current_stream(index: int) -> int:
+    """The cudaStream_t of the current stream of device `index`, which has to be the current device."""
+    if _current_device() != index:
+        raise ValueError(f"the tensors' device {index} is not the current one")
+    return _raw_stream(index)
 
 
 def _need(cond, what: str):
@@ -49,7 +50,7 @@ class Embedding:
     def __init__(self, V: int, d: int, max_tokens: int, scale: float = 1.0, padding_id: Optional[int] = None, device: int = 0):
         _need(torch.cuda.is_available(), "no CUDA device: the operators have no CPU implementation")
         self.V, self.d, self.max_tokens, self.scale = V, d, max_tokens, scale
-        self.device = torch.device("cuda", device)
+        self.device, self.index = torch.device("cuda", device), device
         lib = B.lib()
         size = C.c_uint64(0)
         B._check(lib.tensair_embedding_workspace_bytes(max_tokens, V, d, C.byref(size)), "tensair_embedding_workspace_bytes")
@@ -69,7 +70,7 @@ class Embedding:
     def _set_tokens(self, ids):
         kind = _INTS.get(ids.dtype)
         n = ids.numel()
-        if kind is None or ids.device != self.device or n > self.max_tokens:
+        if kind is None or ids.get_device() != self.index or n > self.max_tokens:
             raise ValueError(f"ids: {n} of {ids.dtype} on {ids.device}; up to {self.max_tokens} int32 or int64 on {self.device} go")
         if not ids.is_contiguous():
             ids = ids.contiguous()
@@ -80,7 +81,7 @@ class Embedding:
     def _set_rows(self, which, x, rows, name):
         kind = _FLOATS.get(x.dtype)
         shape, stride = x.shape, x.stride()
-        if (kind is None or x.device != self.device or len(shape) != 2 or shape[0] != rows or shape[1] != self.d
+        if (kind is None or x.get_device() != self.index or len(shape) != 2 or shape[0] != rows or shape[1] != self.d
                 or (stride[1] != 1 and self.d > 1) or (stride[0] < self.d and rows > 1)):
             raise ValueError(f"{name}: {tuple(shape)} of {x.dtype} with strides {stride} on {x.device}; ({rows}, {self.d}) of float32, "
                              f"bfloat16 or float16 on {self.device} with columns next to each other go")
@@ -100,7 +101,7 @@ class Embedding:
 
     def _workspace_on(self):
         """The current stream, after the calls of another stream that may still use the workspace."""
-        stream = _current_stream(self.device)
+        stream = _current_stream(self.index)
         if stream != self._workspace_stream:
             now = torch.cuda.current_stream(self.device)
             if self._workspace_user is not None and not torch.cuda.is_current_stream_capturing():
@@ -115,13 +116,17 @@ class Embedding:
         rt = self._set_rows(0, table, self.V, "table")
         shaped = out
         if out is None:
-            out = shaped = torch.empty(n, self.d, dtype=dtype or table.dtype, device=self.device)
+            dtype = dtype or table.dtype
+            _need(dtype in _FLOATS, "dtype: float32, bfloat16 or float16")
+            out = shaped = torch.empty((n, self.d), dtype=dtype, device=self.device)
+            r = self._rows[1]
+            r.data, r.stride, r.type = out.data_ptr(), self.d, _FLOATS[dtype]
+            ro = self._at[2]
             if ids.dim() != 1:
                 shaped = out.view(*ids.shape, self.d)
-        elif out.dim() != 2:
-            out = out.view(n, self.d)
-        ro = self._set_rows(1, out, n, "out")
-        rc = self._lib.tensair_embedding_lookup(self._at[0], rt, ro, self.scale, _current_stream(self.device))
+        else:
+            ro = self._set_rows(1, out if out.dim() == 2 else out.view(n, self.d), n, "out")
+        rc = self._lib.tensair_embedding_lookup(self._at[0], rt, ro, self.scale, _current_stream(self.index))
         if rc:
             B._check(rc, "tensair_embedding_lookup")
         return shaped
@@ -247,6 +252,7 @@ class AdamW:
         self.state_bits, self.step_count, self.seed = state_bits, step, seed
         self.device = params[0].device
         _need(self.device.type == "cuda", "no CUDA device: the operators have no CPU implementation")
+        self.index = self.device.index
         kept = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         names = ["m", "v"] + (["m_scale", "v_scale"] if state_bits == 8 else [])
         state = state or {k: [torch.zeros(-(-p.numel() // BLOCK) if k.endswith("scale") else p.numel(),
@@ -298,7 +304,7 @@ class AdamW:
             grads = list(grads)
             for i in left_out:
                 grads[i] = self.params[i]          # stands in for the checks; its n is set to 0
-        index, a, said = self.device.index, self._np, self._said     # what the descriptors say is written again only where it changed
+        index, a, said = self.index, self._np, self._said     # what the descriptors say is written again only where it changed
         kinds = [g.dtype for g in grads]
         if ([g.numel() for g in grads] != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds)) or False in [g.is_contiguous() for g in grads]
                 or [g.get_device() for g in grads] != [index] * len(grads)):
@@ -318,7 +324,7 @@ class AdamW:
             a["n"][left_out] = 0
             self._left_out = left_out
         _set_adamw(self._hyper, self.lr, self.betas, self.eps, self.weight_decay, self.step_count + 1, self.seed, grad_scale, self.device)
-        rc = self._lib.tensair_adamw_step(self._t, len(grads), self.state_bits, self._at, _current_stream(self.device))
+        rc = self._lib.tensair_adamw_step(self._t, len(grads), self.state_bits, self._at, _current_stream(self.index))
         if rc:
             B._check(rc, "tensair_adamw_step")
         self.step_count += 1
