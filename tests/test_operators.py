@@ -198,6 +198,28 @@ def test_gradient_over_vocabularies_of_one_to_three_digits(V):
 
 
 @gpu
+@pytest.mark.parametrize("n", [63, 64, 65, 2047, 2048, 16_383, 16_384, 16_385, 65_536, 131_071, 131_072, 131_073])
+def test_gradient_where_the_sort_changes_its_way(n):
+    d = 3
+    for V, law in ((1 << 30, "uniform"), (70_000, "zipf"), (5000, "runs")):
+        ids = _ids(n, V, law, n, padding=-1, dtype=torch.int32)
+        grad = _rand((n, d), seed=n)
+        e = _ops().Embedding(V, d, max_tokens=n, padding_id=-1)
+        row, rows, m = e.gradient_rows(grad, ids)
+        m = int(m)
+        held = ids >= 0
+        want, index = torch.unique(ids[held].long(), return_inverse=True)
+        assert m == want.numel() and torch.equal(row[:m].long(), want)
+        total, size = (torch.zeros(m, d, dtype=torch.float64, device="cuda") for _ in range(2))
+        total.index_add_(0, index, grad[held].double())
+        size.index_add_(0, index, grad[held].double().abs())
+        _close(rows[:m], total, size * (torch.bincount(index, minlength=m) + 1)[:, None] * U * 1.01)
+        if V < 1 << 20:
+            table = e.gradient(grad, ids)
+            assert torch.equal(table[want], rows[:m]) and int((table != 0).any(1).sum()) == int((rows[:m] != 0).any(1).sum())
+
+
+@gpu
 def test_gradient_of_strided_and_broadcast_rows():
     V, d, n = 40, 24, 300
     ids = _ids(n, V, "zipf")
@@ -598,7 +620,7 @@ REFUSED = [
     (dict(tokens=dict(ids=None)), ALL, "ids are NULL"), (dict(tokens=dict(ids=4098)), ALL, "aligned"),
     (dict(tokens=dict(error=4097)), ALL, "error word"), (dict(out=None), ALL, ""), (dict(grad=None), ALL, ""),
     (dict(out=dict(data=None)), ALL, ""), (dict(grad=dict(data=None)), ALL, ""), (dict(out=dict(stride=7)), ALL, "stride"),
-    (dict(grad=dict(stride=7)), ALL, "stride"), (dict(out=dict(d=0)), ALL, "d not in"), (dict(grad=dict(d=4)), ALL, "width"),
+    (dict(grad=dict(stride=7)), ALL, "stride"), (dict(out=dict(stride=2 ** 31)), ALL, "stride"), (dict(out=dict(d=0)), ALL, "d not in"), (dict(grad=dict(d=4)), ALL, "width"),
     (dict(grad=dict(type=3)), ALL, "type"), (dict(out=dict(type=7)), ALL, ""), (dict(grad=dict(data=4098)), ALL, "alignment"),
     (dict(out=dict(type=B.BFLOAT16)), ("rows",), "must be TENSAIR_FLOAT32"), (dict(m=dict(type=B.FLOAT16)), ("adamw",), "m and v"),
     (dict(v=None), ("adamw",), "v: NULL"), (dict(m=dict(d=9)), ("adamw",), "m:"), (dict(adamw=None), ("adamw",), "adamw"),
@@ -691,7 +713,8 @@ def test_the_python_calls_refuse():
            lambda: e.adamw(grad, ids, table, table.half(), table, step=1), lambda: o.AdamW([]), lambda: o.AdamW([table.cpu()]),
            lambda: o.AdamW([table.t()]), lambda: o.AdamW([table], state_bits=4), lambda: o.AdamW([table], copies=[table]),
            lambda: o.AdamW([table], state=dict(m=[table])), lambda: o.AdamW([table]).step([grad]), lambda: o.AdamW([table]).step([]),
-           lambda: e.adamw(grad, ids, table, table, table, step=1, grad_scale=torch.ones(2, device="cuda"))]
+           lambda: e.adamw(grad, ids, table, table, table, step=1, grad_scale=torch.ones(2, device="cuda")),
+           lambda: e.lookup(table, ids, dtype=torch.float64)]
     for i, call in enumerate(bad):
         with pytest.raises((ValueError, B.TensairError)):
             call()
