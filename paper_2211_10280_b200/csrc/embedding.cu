@@ -1,5 +1,5 @@
 // Embedding lookup with scaling, and the sums by token that its gradient and the AdamW step of the touched rows are
-// made of.
+// made of (for batches of more than 1,024 positions; embedding_short.cu has the others).
 //
 // Sums.  The batch's positions are sorted by token (token_sort.cu).  A block takes 64 sorted positions (and a slab of the
 // columns), lists the tokens that begin there in shared memory, and each of its threads then works through (token,
@@ -8,13 +8,12 @@
 // up in pieces, one partial row per window of 16, and a second launch joins those in window order: no thread has more than
 // 16 rows to add, whatever the tokens' frequencies are, and no sum depends on timing.
 //
-// What bounds it, 65,536 tokens of a Zipf vocabulary of 1 M, d = 300: scattered rows of 1,200 bytes.  Rows (fp32): 28 us for
-// 112 MB.  AdamW (bf16 gradients, fp32 table and moments): 50 us for 237 MB, 4.7 TB/s; the reads and writes of those rows
+// What bounds it, 65,536 tokens of a Zipf vocabulary of 1 M, d = 300: scattered rows of 1,200 bytes.  Rows (fp32): 24 us for
+// 112 MB, 4.7 TB/s.  AdamW (bf16 gradients, fp32 table and moments): 47 us for 237 MB, 5.0 TB/s; the reads and writes of those rows
 // alone, in a kernel that does nothing else, take 45 us.  Shared memory is kept small because the reads in flight live in the
 // level-1 cache beside it (40 KB per block: +14 us).  A short batch is bound by the latency of the launches: 4,096 tokens of
 // 128 floats take 18 us in all, of which the sort takes 9.
-#include "adamw.cuh"
-#include "operators.h"
+#include "embedding.cuh"
 
 namespace tensair {
 
@@ -61,41 +60,6 @@ k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table
     }
 }
 
-// Widest vector, in elements, that rows of d elements can be moved by (at most `limit`): every row begins on a multiple
-// of it, or of 16 bytes where it is wider than that.
-uint32_t vector_of(const RowsView& r, uint32_t d, uint32_t limit) {
-    uint32_t e = limit;
-    for (; e > 1; e /= 2) {
-        const uint32_t bytes = e * type_bytes(r.type) > 16 ? 16 : e * type_bytes(r.type);
-        if (d % e == 0 && r.stride * type_bytes(r.type) % bytes == 0 && (uintptr_t)r.data % bytes == 0) break;
-    }
-    return e;
-}
-// 16 bytes of the narrower of two types
-uint32_t widest(const RowsView& a, const RowsView& b) {
-    return 16 / (type_bytes(a.type) < type_bytes(b.type) ? type_bytes(a.type) : type_bytes(b.type));
-}
-
-// Calls f with a value of the element type as its argument.
-template <typename F>
-cudaError_t with_type(uint32_t type, F&& f) {
-    switch (type) {
-        case 0: return f(float());
-        case 1: return f(__nv_bfloat16());
-        default: return f(__half());
-    }
-}
-template <typename F>
-cudaError_t with_columns(uint32_t e, F&& f) {
-    switch (e) {
-        case 8: return f(Columns<8, false>());
-        case 4: return f(Columns<4, false>());
-        case 2: return f(Columns<2, false>());
-        default: return f(Columns<4, true>());
-    }
-}
-uint32_t pieces_of(uint32_t d, uint32_t e) { return e > 1 ? d / e : (d + 3) / 4; }
-
 constexpr uint32_t kMaxItems = 0x7FFFFFFFu;   // vectors per launch, so that their numbers stay below 2^31
 
 }  // namespace
@@ -135,52 +99,6 @@ constexpr uint32_t kSumBlocks = 4;   // blocks per multiprocessor aimed at
 constexpr uint32_t kFewPieces = 8;     // after the first
 constexpr int kJoinThreads = 256;
 constexpr int kJoinWarps = kJoinThreads / 32;
-
-template <int kCount> struct Rows { static constexpr int value = kCount; };
-
-// What becomes of the finished sum of a token, E columns from `col` on.  fetch() reads what it is joined with, so that
-// several tokens' reads are in flight before the first is needed; put() joins and stores.
-template <SumKind kKind, typename TO, typename C>
-struct Finish {
-    static constexpr int E = C::E;
-    Pack<TO, E> old;
-    Pack<float, E> m0, v0;
-
-    __device__ __forceinline__ void fetch(const SumArgs& a, uint32_t key, uint32_t col) {
-        if (kKind == kSumRows || (kKind == kSumTable && !a.accumulate)) return;
-        old = load_columns<C>((const TO*)a.out.data + (uint64_t)key * a.out.stride + col, a.d - col);
-        if (kKind == kSumAdamw) {
-            m0 = load_columns<C>(a.m + (uint64_t)key * a.m_stride + col, a.d - col);
-            v0 = load_columns<C>(a.v + (uint64_t)key * a.v_stride + col, a.d - col);
-        }
-    }
-    __device__ __forceinline__ void put(const SumArgs& a, float grad_scale, uint32_t key, uint32_t rank, uint32_t col,
-                                        const float (&sum)[E]) {
-        float y[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = sum[e] * a.scale;
-        TO* out = (TO*)a.out.data + (uint64_t)(kKind == kSumRows ? rank : key) * a.out.stride + col;
-        if (kKind == kSumTable) {
-            if (a.accumulate)
-#pragma unroll
-                for (int e = 0; e < E; ++e) y[e] += to_float(old.v[e]);
-        } else if (kKind == kSumRows) {
-            if (col == 0) a.out_ids[rank] = key;
-        } else {
-            float m[E], v[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                m[e] = m0.v[e];
-                v[e] = v0.v[e];
-                y[e] = adamw_update(to_float(old.v[e]), y[e] * grad_scale, m[e], v[e], a.adamw, a.adamw.step_size, a.adamw.keep);
-            }
-            store_columns<C>(a.m + (uint64_t)key * a.m_stride + col, m, a.d - col);
-            store_columns<C>(a.v + (uint64_t)key * a.v_stride + col, v, a.d - col);
-        }
-        store_columns<C>(out, y, a.d - col);
-    }
-};
-
 
 template <SumKind kKind, typename TG, typename TO, typename C>
 __global__ void __launch_bounds__(kSumThreads)
@@ -263,25 +181,7 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
         Finish<kKind, TO, C> row;
         if (what == kWholeToken) row.fetch(a, p.y, col);
         float sum[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-        auto add = [&](uint32_t i, auto batch) {
-            constexpr int kRows = decltype(batch)::value;
-            Pack<TG, E> x[kRows];
-#pragma unroll
-            for (int j = 0; j < kRows; ++j) x[j] = load_columns<C>(grad + (uint64_t)pos[from + i + j] * a.grad.stride, a.d - col);
-#pragma unroll
-            for (int j = 0; j < kRows; ++j)
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] += to_float(x[j].v[e]);
-        };
-        // whole batches, then what is left in halves: no access is guarded, and few are waited for alone
-        constexpr int kWhole = kKind == kSumAdamw ? 8 : 4;
-        uint32_t i = 0;
-        for (; i + kWhole <= count; i += kWhole) add(i, Rows<kWhole>());
-        if (kWhole > 4 && i + 4 <= count) { add(i, Rows<4>()); i += 4; }
-        if (i + 2 <= count) { add(i, Rows<2>()); i += 2; }
-        if (i < count) add(i, Rows<1>());
+        add_rows<kKind, C>(grad, a.grad.stride, pos + from, count, a.d - col, sum);
         if (what == kWholeToken) row.put(a, grad_scale, p.y, p.z, col, sum);
         else {
             const uint64_t slot = ((uint64_t)blockIdx.x * (kSpan / kWindow) + (p.x >> 24)) * 2 + (what == kPiece1);
@@ -372,24 +272,8 @@ static cudaError_t launch_sums(cudaStream_t stream, const SumArgs& a, int sms) {
 }
 
 cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms) {
-    uint32_t e = vector_of(a.grad, a.d, widest(a.grad, a.out));
-    e = vector_of(a.out, a.d, e);
-    if (kind == kSumAdamw) {
-        e = vector_of(RowsView{a.m, a.m_stride, 0}, a.d, e);
-        e = vector_of(RowsView{a.v, a.v_stride, 0}, a.d, e);
-    }
-    return with_type(a.grad.type, [&](auto tg) {
-        return with_type(a.out.type, [&](auto to) {
-            return with_columns(e, [&](auto c) {
-                using TG = decltype(tg);
-                using TO = decltype(to);
-                using C = decltype(c);
-                if (kind == kSumAdamw) return launch_sums<kSumAdamw, TG, TO, C>(stream, a, sms);
-                if (kind == kSumTable) return launch_sums<kSumTable, TG, TO, C>(stream, a, sms);
-                if constexpr (sizeof(TO) == 4) return launch_sums<kSumRows, TG, TO, C>(stream, a, sms);
-                else return cudaErrorInvalidValue;
-            });
-        });
+    return with_sum(kind, a, [&](auto k, auto tg, auto to, auto c) {
+        return launch_sums<decltype(k)::value, decltype(tg), decltype(to), decltype(c)>(stream, a, sms);
     });
 }
 

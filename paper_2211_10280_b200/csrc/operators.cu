@@ -113,14 +113,19 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
     const int sms = multiprocessors();
     if (!sms) return refuse(TENSAIR_ECUDA, "no CUDA device is current");
     if (!n) return clear.rows ? launched(launch_clear((cudaStream_t)stream, clear, sms)) : TENSAIR_OK;
-    uint8_t* w = (uint8_t*)workspace;
-    a.s = SortedTokens{(uint32_t*)(w + l.key), (uint32_t*)(w + l.pos), (uint32_t*)(w + l.seg_start),
-                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info)};
     a.grad = view_of(*grad);
     a.n = n;
     a.V = V;
     a.d = d;
     a.scale = scale;
+    if (is_short(n)) {
+        cudaError_t e = clear.rows ? launch_clear((cudaStream_t)stream, clear, sms) : cudaSuccess;
+        if (e == cudaSuccess) e = launch_short_sums((cudaStream_t)stream, kind, a, tokens_of(*tokens), sms);
+        return launched(e);
+    }
+    uint8_t* w = (uint8_t*)workspace;
+    a.s = SortedTokens{(uint32_t*)(w + l.key), (uint32_t*)(w + l.pos), (uint32_t*)(w + l.seg_start),
+                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info)};
     a.partials = (float*)(w + l.partials);
     a.partial_stride = l.partial_stride;
     a.large = (uint4*)(w + l.large);

@@ -179,6 +179,10 @@ struct SumArgs {
 };
 cudaError_t launch_lookup(cudaStream_t stream, const TokenIds& t, const RowsView& table, const RowsView& out, uint32_t d,
                           float scale);
+// embedding_short.cu: sort and sums of a batch of up to 1,024 positions in one launch, without a workspace; for kSumTable without
+// accumulate the launch before it on the stream has to be launch_clear.
+bool is_short(uint32_t n);
+cudaError_t launch_short_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, const TokenIds& t, int sms);
 cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms);
 // A launch that may begin while the launch before it on the stream is still running: its blocks wait in
 // after_previous_launch() before they touch what that one writes.
