@@ -16,11 +16,12 @@
 // range, below 2^-14 of the block's largest, round to nearest.  Non-finite elements are stored as NaN and leave the
 // block's scale alone, so they stay where they are, as in 32 bits.
 //
-// With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 59 instructions (26 of them integer: Philox, the roundings, addresses), so the kernel is bound by
-// their issue and latency before memory: 128 M elements take 400 us, 4.5 TB/s (0.69 of the copy rate), at 2.1 instructions
-// per cycle of 4.  What made it so (547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate
-// quotients in the update, Philox with its round keys in the arguments, one vote per block for the rare cases, 64 registers
-// for four blocks per multiprocessor.  Copying the next blocks ahead through shared memory made it slower (443 us).
+// With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 59 instructions, 26 of them integer (Philox,
+// the roundings, addresses), so the kernel is bound by both: 128 M elements take 325 us, 5.5 TB/s (0.84 of the copy rate).
+// What made it so (547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate quotients in the
+// update, Philox with its round keys in the arguments, one vote per block for the rare cases, 64 registers for four blocks per
+// multiprocessor (401 us), and the next turn's reads prefetched into the level-2 cache.  Copying them ahead through shared memory
+// instead made it slower (443 us).
 #include "adamw.cuh"
 #include "operators.h"
 #include "philox.cuh"
@@ -356,6 +357,12 @@ k_adamw8(const __grid_constant__ Batch<kCount> b) {
     for (; base < whole; base += kStep) {
         const uint64_t i = base + lane * kLaneElems, block = base / kBlock;
         const float m_scale = t.m_scale[block], v_scale = t.v_scale[block];
+        if (base + kStep < whole) {      // what the next turn reads, into the level-2 cache: 401 -> 325 us, and no registers
+            prefetch((const TP*)t.p + i + kStep);
+            prefetch((const TG*)t.g + i + kStep);
+            prefetch((const uint8_t*)t.m + i + kStep);
+            prefetch((const uint8_t*)t.v + i + kStep);
+        }
         float p[kLaneElems];
         load_lane<TP>((const TP*)t.p + i, p);
         const Pack<TG, kLaneElems> gg = load_pack<TG, kLaneElems>((const TG*)t.g + i);

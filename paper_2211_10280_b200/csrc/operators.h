@@ -75,6 +75,9 @@ __device__ __forceinline__ void store_columns(T* p, const float (&x)[C::E], uint
     }
 }
 
+// Asks for a line to be brought into the level-2 cache.
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // Eight floats in one 32-byte access (sm_100 has them), where the address is a multiple of 32.
 __device__ __forceinline__ void load_eight(const float* p, float (&x)[8]) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
