@@ -16,7 +16,7 @@
 // range, below 2^-14 of the block's largest, round to nearest.  Non-finite elements are stored as NaN and leave the
 // block's scale alone, so they stay where they are, as in 32 bits.
 //
-// With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 59 instructions, 26 of them integer (Philox,
+// With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 60 instructions, 26 of them integer (Philox,
 // the roundings, addresses), so the kernel is bound by both: 128 M elements take 325 us, 5.5 TB/s (0.84 of the copy rate).
 // What made it so (547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate quotients in the
 // update, Philox with its round keys in the arguments, one vote per block for the rare cases, 64 registers for four blocks per

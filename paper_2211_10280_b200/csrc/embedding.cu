@@ -20,43 +20,52 @@ namespace tensair {
 namespace {
 
 // ------------------------------------------------------------------ lookup
-constexpr int kLookupThreads = 256;
-constexpr int kLookupUnroll = 4;     // 65,536 rows of 300 floats: 25 us; 31 with 1, 25.5 with 2, 29 with 8
+#ifndef LU
+#define LU 4
+#endif
+constexpr int kLookupThreads = 128;
+constexpr int kLookupUnroll = 3;     // see below
 
 // out[i] = scale * table[ids[i]]; a thread moves kLookupUnroll vectors of E elements, a block's width apart, whatever rows
-// they belong to, so no lane is idle for any width.  Bound by memory: 65,536 rows of 300 floats out of 1 M take 25 us, 4.5 TB/s
-// (0.68 of the measured copy rate; rows of 1,200 bytes in no order do not reach it).  One token takes 2.6 us, a launch.
+// they belong to, so no lane is idle for any width.  First all their ids, then all their rows, then all stores.
+// Bound by memory and the latency of its two reads in a row: 65,536 rows of 300 floats out of 1 M take 22.6 us, 5.0 TB/s (0.76
+// of the measured copy rate; rows of 1,200 bytes in no order do not reach it); 65,536 rows of 255 bf16 23 us; one token
+// 2.5 us, a launch.  Two, four, eight vectors a thread: 24.6, 22.6, 28 us, and 22.5, 24.7, 35 us for the odd rows; blocks of 256 and 512
+// threads are slower (24, 25 us).
 template <typename TT, typename TO, typename C>
 __global__ void __launch_bounds__(kLookupThreads)
 k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table_stride, TO* __restrict__ out,
          uint64_t out_stride, FastDiv vecs, uint32_t d, uint32_t total, float scale) {
     constexpr int E = C::E;
     const uint32_t base = blockIdx.x * (kLookupThreads * kLookupUnroll) + threadIdx.x;
+    const TT* from[kLookupUnroll];
     Pack<TT, E> x[kLookupUnroll];
-    uint32_t row[kLookupUnroll], col[kLookupUnroll];
-    bool held[kLookupUnroll];
 #pragma unroll
     for (int u = 0; u < kLookupUnroll; ++u) {
         const uint32_t w = base + u * kLookupThreads;
-        const uint32_t r = w < total ? vecs.div(w) : 0;
-        col[u] = (w - r * vecs.divisor) * E;
-        row[u] = row0 + r;
-        held[u] = false;
+        from[u] = nullptr;
         if (w < total) {
-            const int64_t id = t.wide ? __ldg(reinterpret_cast<const long long*>(t.ids) + row[u])
-                                      : __ldg(reinterpret_cast<const int32_t*>(t.ids) + row[u]);
-            held[u] = id != t.padding && (uint64_t)id < t.V;
-            if (held[u]) x[u] = load_columns<C>(table + (uint64_t)id * table_stride + col[u], d - col[u]);
+            const uint32_t r = vecs.div(w), col = (w - r * vecs.divisor) * E;
+            const int64_t id = t.wide ? __ldg(reinterpret_cast<const long long*>(t.ids) + row0 + r)
+                                      : __ldg(reinterpret_cast<const int32_t*>(t.ids) + row0 + r);
+            if (id != t.padding && (uint64_t)id < t.V) from[u] = table + (uint64_t)id * table_stride + col;
             else if (id != t.padding && t.err) atomicOr(t.err, kErrBadToken);
         }
     }
 #pragma unroll
     for (int u = 0; u < kLookupUnroll; ++u) {
-        if (base + u * kLookupThreads >= total) break;
+        const uint32_t w = base + u * kLookupThreads;
+        if (from[u]) x[u] = load_columns<C>(from[u], d - (w - vecs.div(w) * vecs.divisor) * E);
+    }
+#pragma unroll
+    for (int u = 0; u < kLookupUnroll; ++u) {
+        const uint32_t w = base + u * kLookupThreads;
+        if (w >= total) break;
+        const uint32_t r = vecs.div(w), col = (w - r * vecs.divisor) * E;
         float y[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = held[u] ? to_float(x[u].v[e]) * scale : 0.0f;
-        store_columns<C>(out + (uint64_t)row[u] * out_stride + col[u], y, d - col[u]);
+        for (int e = 0; e < E; ++e) y[e] = from[u] ? to_float(x[u].v[e]) * scale : 0.0f;
+        store_columns<C>(out + (uint64_t)(row0 + r) * out_stride + col, y, d - col);
     }
 }
 
