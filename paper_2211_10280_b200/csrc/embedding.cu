@@ -20,9 +20,6 @@ namespace tensair {
 namespace {
 
 // ------------------------------------------------------------------ lookup
-#ifndef LU
-#define LU 4
-#endif
 constexpr int kLookupThreads = 128;
 constexpr int kLookupUnroll = 3;     // see below
 
