@@ -70,6 +70,9 @@ __global__ void __launch_bounds__(kSortBlock, 1)
 k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bits) {
     cg::cluster_group cluster = cg::this_cluster();
     let_next_launch_begin();
+    // Another block's shared memory may be written only once that block is known to have started: every block says so here, and
+    // all wait for it behind the read of the ids, before the first pass's totals go out.
+    auto started = cluster.barrier_arrive();
     const uint32_t rank = cluster.block_rank(), blocks = cluster.num_blocks();
     extern __shared__ __align__(16) uint8_t raw[];
     const uint32_t bins = 1u << digit_bits, mask = bins - 1, tid = threadIdx.x;
@@ -79,6 +82,7 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
     const uint32_t at = rank * kSortBlock + tid;
     // places past the batch sort behind everything, in order
     uint2 item = make_uint2(at < t.n ? token_key(t, at) : 0xFFFFFFFFu, at);
+    cluster.barrier_wait(std::move(started));
     for (uint32_t shift = 0; shift < key_bits; shift += digit_bits) {
         const uint32_t digit = item.x >> shift & mask;
         const uint32_t place = block_rank(digit, digit_bits, counts, [&](uint32_t x, uint32_t two) {
