@@ -114,11 +114,11 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
     // No large shared arrays: the reads in flight need the level-1 cache, which shares its memory with them.
     __shared__ __align__(16) uint4 parts[kMaxParts];
     __shared__ uint32_t pos[kSpan + kWindow], head_masks[kSpan / 32], part_masks[kSpan / 32];
-    let_next_launch_begin();
     const uint32_t tid = threadIdx.x, begin = blockIdx.x * kSpan;
     const uint32_t vec0 = blockIdx.y * slab_vecs;
     const uint32_t vecs = all_vecs - vec0 < slab_vecs ? all_vecs - vec0 : slab_vecs;
     after_previous_launch();
+    let_next_launch_begin();
     float grad_scale = 1.0f;
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
     const uint32_t n_valid = a.s.info[0];

@@ -188,7 +188,9 @@ bool is_short(uint32_t n);
 cudaError_t launch_short_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, const TokenIds& t, int sms);
 cudaError_t launch_token_sums(cudaStream_t stream, SumKind kind, const SumArgs& a, int sms);
 // A launch that may begin while the launch before it on the stream is still running: its blocks wait in
-// after_previous_launch() before they touch what that one writes.
+// after_previous_launch() before they touch what that one writes, and let their own successor begin only after that (the sort in a
+// cluster lets it begin at once: no launch before it writes what it or its successor reads).  What the launch before writes is read through plain pointers (no const __restrict__, no __ldg): reads of memory that is taken to stay
+// unchanged for the whole kernel are not ordered by the wait.
 template <typename... Params, typename... Args>
 cudaError_t launch_early(void (*kernel)(Params...), dim3 grid, uint32_t block, size_t shared, cudaStream_t stream, Args&&... args) {
     cudaLaunchConfig_t cfg = {};

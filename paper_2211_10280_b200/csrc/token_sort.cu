@@ -148,15 +148,19 @@ struct ClearShare {
     }
 };
 
+// What these kernels read was written while they were already waiting, so their parameters are not marked const __restrict__: that
+// would allow the compiler reads that count on memory which no one changes while the kernel runs.  Each lets its successor begin
+// only behind its own wait: no launch is ever more than one ahead of the one that runs.
+//
 // A tile is the 1,024 items of a block; hist: [tile][digit], 16 bits each.
 // Ranks the tile's items of a pass by digit: place[i] is the rank among the tile's items of its digit.
 template <bool kFirst>
 __global__ void __launch_bounds__(kSortBlock)
-k_tile_rank(TokenIds t, const uint2* __restrict__ items, uint2* __restrict__ out, uint16_t* __restrict__ place, uint32_t* __restrict__ hist,
-            uint32_t shift, uint32_t digit_bits, uint32_t tiles, ClearShare clear) {
+k_tile_rank(TokenIds t, const uint2* items, uint2* out, uint16_t* place, uint32_t* hist, uint32_t shift, uint32_t digit_bits,
+            uint32_t tiles, ClearShare clear) {
     extern __shared__ __align__(16) uint32_t counts[];
-    let_next_launch_begin();
     if (!kFirst) after_previous_launch();
+    let_next_launch_begin();
     if (blockIdx.x >= tiles) return clear.run(tiles);
     const uint32_t at = blockIdx.x * kSortBlock + threadIdx.x, pairs = 1u << digit_bits >> 1;
     uint32_t key = 0xFFFFFFFFu;
@@ -172,12 +176,12 @@ k_tile_rank(TokenIds t, const uint2* __restrict__ items, uint2* __restrict__ out
 // Moves the items to where the pass has them; the last pass writes keys and positions apart.
 template <bool kLast>
 __global__ void __launch_bounds__(kSortBlock)
-k_tile_scatter(uint32_t n, const uint2* __restrict__ items, uint2* __restrict__ out, const uint16_t* __restrict__ place,
-               const uint16_t* __restrict__ hist, uint32_t shift, uint32_t digit_bits, uint32_t tiles, SortedTokens s, ClearShare clear) {
+k_tile_scatter(uint32_t n, const uint2* items, uint2* out, const uint16_t* place, const uint16_t* hist, uint32_t shift,
+               uint32_t digit_bits, uint32_t tiles, SortedTokens s, ClearShare clear) {
     __shared__ uint32_t base[1 << kMaxDigitBits], warp_sums[kSortBlockWarps];
-    let_next_launch_begin();
     const uint32_t tid = threadIdx.x, at = blockIdx.x * kSortBlock + tid, bins = 1u << digit_bits;
     after_previous_launch();
+    let_next_launch_begin();
     if (blockIdx.x >= tiles) return clear.run(tiles);
     uint2 item = make_uint2(0, 0);
     uint32_t rank = 0;
@@ -209,9 +213,9 @@ k_tile_scatter(uint32_t n, const uint2* __restrict__ items, uint2* __restrict__ 
 __global__ void __launch_bounds__(kSortBlock)
 k_list_tokens(uint32_t n, uint32_t V, uint32_t tiles, SortedTokens s, ClearShare clear) {
     __shared__ uint32_t warp_sums[kSortBlockWarps];
-    let_next_launch_begin();
     const uint32_t tid = threadIdx.x, first = blockIdx.x * kSortBlock, at = first + tid;
     after_previous_launch();
+    let_next_launch_begin();
     if (blockIdx.x >= tiles) return clear.run(tiles);
     uint32_t c = 0;
     const uint4* keys = reinterpret_cast<const uint4*>(s.key);

@@ -60,3 +60,22 @@ def test_sorts_in_a_cluster_whose_blocks_start_while_the_device_is_busy(n, V):
     torch.cuda.synchronize()
     for got, (ids, grad) in zip(outs, batches * 2):
         _same_rows(got, ids, grad)
+
+
+@gpu
+@pytest.mark.parametrize("V", [900, 300_000, (1 << 20) + 77])      # one, two and three digits
+@pytest.mark.parametrize("n", [16_385, 40_000, 131_072])
+def test_chained_launches_read_what_the_launch_before_them_wrote(n, V):
+    """Digit counts and places are rewritten in every pass and every call, by launches that begin while the ones that read the old
+    values still run: batches in a row without a pause, every one unlike the one before."""
+    e = _ops().Embedding(V, 4, max_tokens=n)
+    batches = [_batch(n, V, s) for s in range(4)]
+    batches = [(torch.roll(ids, k * 777), torch.roll(grad, k * 777, 0)) for k in range(3) for ids, grad in batches]
+    torch.cuda.synchronize()
+    outs = [e.gradient_rows(grad, ids) for ids, grad in batches]
+    tables = [e.gradient(grad, ids) for ids, grad in batches[:3]]
+    torch.cuda.synchronize()
+    for got, (ids, grad) in zip(outs, batches):
+        _same_rows(got, ids, grad)
+    for table, (ids, grad) in zip(tables, batches):
+        assert torch.equal(table, torch.zeros(V, 4, device="cuda").index_add_(0, ids, grad))
