@@ -241,6 +241,9 @@ class AdamW:
     copies: tensors (bfloat16 or float16, or None) that receive the updated parameters, rounded.  lr_factors and
     decay_factors: per-parameter factors on lr and weight_decay.  state: dict of lists to start from (m, v and for 8 bits
     m_scale, v_scale; they become the optimizer's own), zeros by default; step: steps already made.
+
+    A parameter may change its place or its type between steps (model.bfloat16()), not its size.  The moments and copies are those of
+    the constructor: they can be written into, not replaced.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32,
@@ -261,30 +264,52 @@ class AdamW:
         _need(sorted(state) == sorted(names), f"state: needs {names}")
         self._t = (B.AdamwTensor * len(params))()
         self._np = np.frombuffer(self._t, dtype=_DESCRIPTOR)
-        self.copies = list(copies) if copies is not None else [None] * len(params)
-        lists = [self.copies, lr_factors or params, decay_factors or params] + [state[k] for k in names]
+        self._copies = tuple(copies) if copies is not None else (None,) * len(params)
+        self._state = {k: tuple(state[k]) for k in names}
+        lists = [self._copies, lr_factors or params, decay_factors or params] + [self._state[k] for k in names]
         _need(all(len(x) == len(params) for x in lists), "copies, factors and state need one entry per parameter")
         for i, p in enumerate(params):
             t = self._t[i]
             self._fits(p, p.numel(), _FLOATS, f"params[{i}]")
-            t.n, t.param_type = p.numel(), _FLOATS[p.dtype]
+            t.n = p.numel()
             for k in names:
                 want = -(-p.numel() // BLOCK) if k.endswith("scale") else p.numel()
-                self._fits(state[k][i], want, (torch.float32,) if k.endswith("scale") else (kept,), f"{k}[{i}]")
-                setattr(t, k, state[k][i].data_ptr())
-            c = self.copies[i]
+                self._fits(self._state[k][i], want, (torch.float32,) if k.endswith("scale") else (kept,), f"{k}[{i}]")
+                setattr(t, k, self._state[k][i].data_ptr())
+            c = self._copies[i]
             if c is not None:
                 self._fits(c, p.numel(), (torch.bfloat16, torch.float16), f"copies[{i}]")
                 t.copy, t.copy_type = c.data_ptr(), _FLOATS[c.dtype]
             t.lr_factor = lr_factors[i] if lr_factors else 1.0
             t.decay_factor = decay_factors[i] if decay_factors else 1.0
-        self.m, self.v = state["m"], state["v"]
-        self.m_scale, self.v_scale = state.get("m_scale"), state.get("v_scale")
+        # what the descriptors point to is held here, whatever becomes of the tensors that the caller has
+        self._held = [x.detach() for xs in [self._copies, *self._state.values()] for x in xs if x is not None]
         self._lib = B.lib()
         self._hyper = B.Adamw()
         self._at = C.byref(self._hyper)
-        self._said, self._left_out = [None, None, None], []
+        self._said, self._left_out = [None, None, None, None], []
         self._numel = [p.numel() for p in params]
+
+    # The tensors that the descriptors point to, once and for all: tuples, so that an entry cannot be replaced unseen.
+    @property
+    def m(self):
+        return self._state["m"]
+
+    @property
+    def v(self):
+        return self._state["v"]
+
+    @property
+    def m_scale(self):
+        return self._state.get("m_scale")
+
+    @property
+    def v_scale(self):
+        return self._state.get("v_scale")
+
+    @property
+    def copies(self):
+        return self._copies
 
     def _fits(self, x, n, dtypes, name):
         _need(x.device == self.device and x.dtype in dtypes and x.numel() == n and x.is_contiguous(),
@@ -313,9 +338,14 @@ class AdamW:
         ptrs = [g.data_ptr() for g in grads]
         if ptrs != said[0]:
             a["grad"] = said[0] = ptrs
-        ptrs = [p.data_ptr() for p in self.params]
-        if ptrs != said[1]:
-            a["param"] = said[1] = ptrs
+        # a parameter may have been converted or moved: its place and type are looked at in every step, the rest where one of them changed
+        ptrs, param_kinds = [p.data_ptr() for p in self.params], [p.dtype for p in self.params]
+        if ptrs != said[1] or param_kinds != said[3]:
+            for i, p in enumerate(self.params):
+                self._fits(p, self._numel[i], _FLOATS, f"params[{i}]")
+            a["param_type"] = [_FLOATS[k] for k in param_kinds]
+            a["param"] = ptrs
+            said[1], said[3] = ptrs, param_kinds
         if kinds != said[2]:
             said[2] = kinds
             a["grad_type"] = [_FLOATS[k] for k in kinds]

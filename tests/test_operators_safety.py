@@ -79,3 +79,109 @@ def test_chained_launches_read_what_the_launch_before_them_wrote(n, V):
         _same_rows(got, ids, grad)
     for table, (ids, grad) in zip(tables, batches):
         assert torch.equal(table, torch.zeros(V, 4, device="cuda").index_add_(0, ids, grad))
+
+
+# ---------------------------------------------------------------- parameters that change between steps
+class _Recorder:
+    """Stands in for the library: keeps what each AdamW step was asked to do."""
+
+    def __init__(self):
+        self.asked = []
+
+    def tensair_adamw_step(self, tensors, count, bits, hyper, stream):
+        self.asked.append([(t.param, t.param_type, t.grad, t.grad_type, t.m, t.v, t.copy, t.n) for t in tensors[:count]])
+        return 0
+
+
+@pytest.fixture
+def recorder(monkeypatch):
+    """operators on CPU tensors over a stand-in for the library."""
+    ops, lib = _ops(), _Recorder()
+    need = ops._need
+    monkeypatch.setattr(ops, "_need", lambda cond, what: need(cond or "no CUDA device" in what, what))
+    monkeypatch.setattr(ops, "_current_stream", lambda index: 0)
+    monkeypatch.setattr(ops.B, "lib", lambda: lib)
+    return lib
+
+
+def _with_grads(model, dtype=None):
+    for p in model.parameters():
+        p.grad = torch.ones_like(p, dtype=dtype)
+
+
+def test_a_step_follows_parameters_that_were_converted(recorder):
+    model = torch.nn.Linear(64, 64)
+    opt = _ops().AdamW(model.parameters(), state_bits=32)
+    for convert, kind in ((lambda: None, B.FLOAT32), (model.bfloat16, B.BFLOAT16), (model.half, B.FLOAT16), (model.float, B.FLOAT32)):
+        convert()
+        _with_grads(model)
+        opt.step()
+        for p, (place, param_type, _, grad_type, _, _, _, n) in zip(model.parameters(), recorder.asked[-1]):
+            assert place == p.data_ptr() and param_type == kind and grad_type == kind and n == p.numel()
+    # the same place with another type: as when the allocator hands a freed block out again
+    for p in model.parameters():
+        p.data = p.data.view(torch.int32).view(torch.float32)
+    _with_grads(model)
+    opt.step()
+    model.half()
+    flat = [p.data for p in model.parameters()]
+    _with_grads(model)
+    opt.step()
+    for p, x in zip(model.parameters(), flat):
+        p.data = x.view(torch.bfloat16)
+    _with_grads(model)
+    opt.step()
+    assert [t[1] for t in recorder.asked[-1]] == [B.BFLOAT16] * 2 and [t[0] for t in recorder.asked[-1]] == [t[0] for t in recorder.asked[-2]]
+
+
+@pytest.mark.parametrize("change", [lambda x: x[:5].clone(), lambda x: x.t().clone(), lambda x: x.double(), lambda x: torch.cat([x, x]),
+                                    lambda x: x[:5], lambda x: x.t()])
+def test_a_step_refuses_parameters_that_no_longer_fit(recorder, change):
+    p = torch.nn.Parameter(torch.ones(8, 6))
+    opt = _ops().AdamW([p], state_bits=32)
+    grad = torch.ones(8, 6)
+    opt.step([grad])
+    old, p.data = p.data, change(p.data)
+    for _ in range(2):
+        if p.data_ptr() != old.data_ptr():
+            with pytest.raises(ValueError):
+                opt.step([grad])
+        with pytest.raises(ValueError):           # in the same place the gradient says that the parameter is another one
+            opt.step([torch.ones_like(p)])
+    assert len(recorder.asked) == 1 and opt.step_count == 1
+    p.data = old
+    opt.step([grad])
+    assert recorder.asked[0] == recorder.asked[1]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_and_copies_cannot_be_replaced_unseen(recorder, bits):
+    p = torch.ones(300)
+    opt = _ops().AdamW([p], state_bits=bits, copies=[torch.empty(300, dtype=torch.bfloat16)])
+    for name in ["m", "v", "copies"] + (["m_scale", "v_scale"] if bits == 8 else []):
+        with pytest.raises(TypeError):
+            getattr(opt, name)[0] = torch.ones(300)
+        with pytest.raises(AttributeError):
+            setattr(opt, name, [torch.ones(300)])
+    place = opt.m[0].data_ptr()
+    opt.m[0].data = torch.zeros(300)              # the memory that a step writes is held all the same
+    opt.step([torch.ones(300)])
+    assert recorder.asked[0][0][4] == place and place in [x.data_ptr() for x in opt._held]
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_converted_parameters_take_the_steps_of_their_type(bits):
+    torch.manual_seed(0)
+    model = torch.nn.Linear(300, 70).cuda()
+    opt = _ops().AdamW(model.parameters(), state_bits=bits, seed=3)
+    _with_grads(model)
+    opt.step()
+    state = {k: [x.clone() for x in xs] for k, xs in opt._state.items()}
+    model.bfloat16()
+    _with_grads(model)
+    twin = [p.detach().clone() for p in model.parameters()]
+    _ops().AdamW(twin, state_bits=bits, seed=3, state=state, step=1).step([p.grad for p in model.parameters()])
+    opt.step()
+    assert all(torch.equal(a, b) for a, b in zip(model.parameters(), twin))
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for k in state for a, b in zip(opt._state[k], state[k]))
