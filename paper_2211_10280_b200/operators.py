@@ -192,10 +192,12 @@ class Embedding:
         return _Lookup.apply(table, ids, self)
 
     def check(self):
-        """Waits for the device and raises TensairError (EBADTOKEN) if a call since the last check met an id outside [0, V)."""
+        """Waits for the device, all its streams, and raises TensairError (EBADTOKEN) if a call since the last check met an id outside [0, V)."""
+        torch.cuda.synchronize(self.device)
         flags = int(self.error.item())
         if flags:
             self.error.zero_()
+            torch.cuda.current_stream(self.device).synchronize()      # whatever stream the next call is on
             raise B.TensairError(B.tensair_error_of_flags(flags), "Embedding")
 
 

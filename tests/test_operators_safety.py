@@ -185,3 +185,23 @@ def test_converted_parameters_take_the_steps_of_their_type(bits):
     opt.step()
     assert all(torch.equal(a, b) for a, b in zip(model.parameters(), twin))
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for k in state for a, b in zip(opt._state[k], state[k]))
+
+
+# ---------------------------------------------------------------- other streams
+BUSY = 20_000_000          # clock cycles that a stream is kept busy for: some 10 ms
+
+
+
+@gpu
+def test_check_waits_for_calls_of_other_streams():
+    V = 50
+    e = _ops().Embedding(V, 4, max_tokens=8)
+    table, bad = torch.zeros(V, 4, device="cuda"), torch.full((3,), V, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(BUSY)
+            e.lookup(table, bad)
+        with pytest.raises(B.TensairError):
+            e.check()
