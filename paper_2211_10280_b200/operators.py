@@ -23,6 +23,7 @@ _INTS = {torch.int32: B.INT32, torch.int64: B.INT64}
 # the current stream's handle without a Stream object around it (2 us of a call that takes 10)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
 _NO_PADDING = -(1 << 63)
 BLOCK = 256                      # elements that share a scale of the 8-bit moments
 
@@ -32,6 +33,13 @@ def _current_stream(index: int) -> int:
     if _current_device() != index:
         raise ValueError(f"the tensors' device {index} is not the current one")
     return _raw_stream(index)
+
+
+def _settle(device):
+    """Waits for the current stream, once, when an object has allocated memory of its own: whatever stream it is used on then, neither
+    the memory's earlier users nor the zeros written to it are still to come."""
+    if not _capturing():
+        torch.cuda.current_stream(device).synchronize()
 
 
 def _need(cond, what: str):
@@ -44,7 +52,8 @@ class Embedding:
 
     scale multiplies every looked-up row (and so every gradient row).  padding_id names an id that stands for "no token":
     its positions read as zero rows and have no gradient.  The object owns the workspace of the gradient calls and the error
-    word that ids outside [0, V) are reported in (`check`); it is used from one thread at a time.
+    word that ids outside [0, V) are reported in (`check`), and orders their use where calls come on several streams; it is used
+    from one thread at a time, and has to outlive the graphs that its calls were captured into.
     """
 
     def __init__(self, V: int, d: int, max_tokens: int, scale: float = 1.0, padding_id: Optional[int] = None, device: int = 0):
@@ -57,6 +66,8 @@ class Embedding:
         self.workspace_bytes = size.value
         self.workspace = torch.empty(max(1, size.value), dtype=torch.uint8, device=self.device)
         self.error = torch.zeros(1, dtype=torch.int32, device=self.device)
+        _settle(self.device)
+        self._known = {torch.cuda.current_stream(self.device).cuda_stream}
         self._workspace_stream = self._workspace_user = None
         self._lib = lib
         self._tokens = B.Tokens(V=V, padding_id=_NO_PADDING if padding_id is None else padding_id, error=self.error.data_ptr())
@@ -99,15 +110,25 @@ class Embedding:
             grad = grad.contiguous()
         return grad
 
-    def _workspace_on(self):
-        """The current stream, after the calls of another stream that may still use the workspace."""
+    def _stream(self):
+        """The current stream, on which the object's memory is in use from now on: the allocator hands it out again only after that."""
         stream = _current_stream(self.index)
+        if stream not in self._known and not _capturing():
+            now = torch.cuda.current_stream(self.device)
+            self.error.record_stream(now)
+            self.workspace.record_stream(now)
+            self._known.add(stream)
+        return stream
+
+    def _workspace_on(self):
+        """(workspace, its address, current stream), after the calls of another stream that may still use the workspace."""
+        stream = self._stream()
         if stream != self._workspace_stream:
             now = torch.cuda.current_stream(self.device)
-            if self._workspace_user is not None and not torch.cuda.is_current_stream_capturing():
+            if self._workspace_user is not None and not _capturing():
                 now.wait_stream(self._workspace_user)
             self._workspace_stream, self._workspace_user = stream, now
-        return stream
+        return self.workspace, self._workspace_at, stream
 
     # ---- calls
     def lookup(self, table, ids, out=None, dtype=None):
@@ -126,7 +147,7 @@ class Embedding:
                 shaped = out.view(*ids.shape, self.d)
         else:
             ro = self._set_rows(1, out if out.dim() == 2 else out.view(n, self.d), n, "out")
-        rc = self._lib.tensair_embedding_lookup(self._at[0], rt, ro, self.scale, _current_stream(self.index))
+        rc = self._lib.tensair_embedding_lookup(self._at[0], rt, ro, self.scale, self._stream())
         if rc:
             B._check(rc, "tensair_embedding_lookup")
         return shaped
@@ -142,8 +163,8 @@ class Embedding:
             out = torch.empty(self.V, self.d, dtype=dtype or grad.dtype, device=self.device)
         rg = self._set_rows(0, grad, n, "grad")
         ro = self._set_rows(1, out, self.V, "out")
-        rc = self._lib.tensair_embedding_gradient(self._at[0], rg, ro, self.scale, accumulate, self._workspace_at,
-                                                  self.workspace_bytes, self._workspace_on())
+        workspace, at, stream = self._workspace_on()
+        rc = self._lib.tensair_embedding_gradient(self._at[0], rg, ro, self.scale, accumulate, at, self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_gradient")
         return out
@@ -166,8 +187,9 @@ class Embedding:
         _need(rows.shape[0] >= most, "rows: fewer than the batch can touch")
         rg = self._set_rows(0, grad, n, "grad")
         ro = self._set_rows(1, rows, rows.shape[0], "rows")
-        rc = self._lib.tensair_embedding_gradient_rows(self._at[0], rg, self.scale, row_ids.data_ptr(), ro, count.data_ptr(),
-                                                       self._workspace_at, self.workspace_bytes, self._workspace_on())
+        workspace, at, stream = self._workspace_on()
+        rc = self._lib.tensair_embedding_gradient_rows(self._at[0], rg, self.scale, row_ids.data_ptr(), ro, count.data_ptr(), at,
+                                                       self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_gradient_rows")
         return out
@@ -182,8 +204,8 @@ class Embedding:
         rv = self._set_rows(3, v, self.V, "v")
         h = self._adamw
         _set_adamw(h, lr, betas, eps, weight_decay, step, 0, grad_scale, self.device)
-        rc = self._lib.tensair_embedding_adamw(self._at[0], rg, self.scale, rt, rm, rv, self._at[5], self._workspace_at,
-                                               self.workspace_bytes, self._workspace_on())
+        workspace, at, stream = self._workspace_on()
+        rc = self._lib.tensair_embedding_adamw(self._at[0], rg, self.scale, rt, rm, rv, self._at[5], at, self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_adamw")
 
@@ -245,7 +267,9 @@ class AdamW:
     m_scale, v_scale; they become the optimizer's own), zeros by default; step: steps already made.
 
     A parameter may change its place or its type between steps (model.bfloat16()), not its size.  The moments and copies are those of
-    the constructor: they can be written into, not replaced.
+    the constructor: they can be written into, not replaced.  Moments that the constructor made are there on any stream; steps on
+    several streams are ordered by the caller, as everything else that uses the parameters.  The optimizer has to outlive the graphs
+    that its steps were captured into.
     """
 
     def __init__(self, params: Sequence[torch.Tensor], lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32,
@@ -260,9 +284,13 @@ class AdamW:
         self.index = self.device.index
         kept = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         names = ["m", "v"] + (["m_scale", "v_scale"] if state_bits == 8 else [])
-        state = state or {k: [torch.zeros(-(-p.numel() // BLOCK) if k.endswith("scale") else p.numel(),
-                                          dtype=torch.float32 if k.endswith("scale") else kept, device=self.device) for p in params]
-                          for k in names}
+        self._known = None                 # streams that the moments are known to be used on, where they were made here
+        if not state:
+            state = {k: [torch.zeros(-(-p.numel() // BLOCK) if k.endswith("scale") else p.numel(),
+                                     dtype=torch.float32 if k.endswith("scale") else kept, device=self.device) for p in params]
+                     for k in names}
+            _settle(self.device)
+            self._known = {_raw_stream(self.index)}
         _need(sorted(state) == sorted(names), f"state: needs {names}")
         self._t = (B.AdamwTensor * len(params))()
         self._np = np.frombuffer(self._t, dtype=_DESCRIPTOR)
@@ -356,7 +384,14 @@ class AdamW:
             a["n"][left_out] = 0
             self._left_out = left_out
         _set_adamw(self._hyper, self.lr, self.betas, self.eps, self.weight_decay, self.step_count + 1, self.seed, grad_scale, self.device)
-        rc = self._lib.tensair_adamw_step(self._t, len(grads), self.state_bits, self._at, _current_stream(self.index))
+        stream = _current_stream(index)
+        if self._known is not None and stream not in self._known and not _capturing():
+            now = torch.cuda.current_stream(self.device)
+            for xs in self._state.values():
+                for x in xs:
+                    x.record_stream(now)
+            self._known.add(stream)
+        rc = self._lib.tensair_adamw_step(self._t, len(grads), self.state_bits, self._at, stream)
         if rc:
             B._check(rc, "tensair_adamw_step")
         self.step_count += 1

@@ -100,6 +100,8 @@ def recorder(monkeypatch):
     need = ops._need
     monkeypatch.setattr(ops, "_need", lambda cond, what: need(cond or "no CUDA device" in what, what))
     monkeypatch.setattr(ops, "_current_stream", lambda index: 0)
+    monkeypatch.setattr(ops, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(ops, "_settle", lambda device: None)
     monkeypatch.setattr(ops.B, "lib", lambda: lib)
     return lib
 
@@ -193,6 +195,36 @@ BUSY = 20_000_000          # clock cycles that a stream is kept busy for: some 1
 
 
 @gpu
+@pytest.mark.parametrize("n", [700, 5000, 40_000])
+def test_an_object_is_first_used_on_another_stream_than_it_was_made_on(n):
+    """What is pending on the constructor's stream, a write to memory that the allocator hands on, or the error word's zero, is
+    over before the first call uses that memory."""
+    V = 3000
+    ids, grad = _batch(n, V, 1)
+    table, bad = torch.zeros(V, 4, device="cuda"), ids.clone()
+    bad[5] = V
+    size = _ops().Embedding(V, 4, max_tokens=n).workspace_bytes
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        left = torch.empty(size, dtype=torch.uint8, device="cuda")
+        word = torch.empty(1, dtype=torch.int32, device="cuda")
+        torch.cuda._sleep(BUSY)
+        left.fill_(255)
+        word.fill_(-1)
+        del left, word
+        e = _ops().Embedding(V, 4, max_tokens=n)
+        with torch.cuda.stream(side):
+            got = e.gradient_rows(grad, ids)
+            e.lookup(table, bad)
+        with pytest.raises(B.TensairError):
+            e.check()
+        e.check()
+        _same_rows(got, ids, grad)
+
+
+
+@gpu
 def test_check_waits_for_calls_of_other_streams():
     V = 50
     e = _ops().Embedding(V, 4, max_tokens=8)
@@ -205,3 +237,54 @@ def test_check_waits_for_calls_of_other_streams():
             e.lookup(table, bad)
         with pytest.raises(B.TensairError):
             e.check()
+
+
+
+@gpu
+@pytest.mark.parametrize("n", [5000, 40_000])
+def test_memory_of_an_object_that_is_gone_is_not_reused_before_its_calls_are_done(n):
+    V = 3000
+    ids, grad = _batch(n, V, 2)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        e = _ops().Embedding(V, 4, max_tokens=n)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(BUSY)
+            got = e.gradient_rows(grad, ids)
+        size = e.workspace_bytes
+        del e
+        held = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        torch.cuda.synchronize()
+        _same_rows(got, ids, grad)
+        del held
+
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_that_the_optimizer_makes_are_zero_and_held_on_any_stream(bits):
+    n = 100_000
+    p, q, r = (torch.linspace(-1, 1, n, device="cuda") for _ in range(3))
+    g = torch.linspace(0, 2, n, device="cuda")
+    again = _ops().AdamW([q], state_bits=bits)
+    again.step([g])
+    r.copy_(q)
+    again.step([g])
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    left = [torch.empty(n * bits // 8, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda._sleep(BUSY)
+    for x in left:
+        x.fill_(66)
+    del left, x
+    opt = _ops().AdamW([p], state_bits=bits)
+    with torch.cuda.stream(side):
+        opt.step([g])
+        first = p.clone()
+        torch.cuda._sleep(BUSY)
+        opt.step([g])
+    del opt
+    held = [torch.full((n * bits // 8,), 66, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    assert torch.equal(first, r) and torch.equal(p, q) and len(held) == 3
