@@ -121,11 +121,15 @@ class Embedding:
         return stream
 
     def _workspace_on(self):
-        """(workspace, its address, current stream), after the calls of another stream that may still use the workspace."""
+        """(workspace, its address, current stream), after the calls of another stream that may still use the workspace.  A call that is
+        captured into a graph has one of its own, out of the graph's memory: nobody here knows when the graph runs."""
         stream = self._stream()
+        if _capturing():
+            own = torch.empty(max(1, self.workspace_bytes), dtype=torch.uint8, device=self.device)
+            return own, own.data_ptr(), stream
         if stream != self._workspace_stream:
             now = torch.cuda.current_stream(self.device)
-            if self._workspace_user is not None and not _capturing():
+            if self._workspace_user is not None:
                 now.wait_stream(self._workspace_user)
             self._workspace_stream, self._workspace_user = stream, now
         return self.workspace, self._workspace_at, stream

@@ -193,7 +193,6 @@ def test_converted_parameters_take_the_steps_of_their_type(bits):
 BUSY = 20_000_000          # clock cycles that a stream is kept busy for: some 10 ms
 
 
-
 @gpu
 @pytest.mark.parametrize("n", [700, 5000, 40_000])
 def test_an_object_is_first_used_on_another_stream_than_it_was_made_on(n):
@@ -223,7 +222,6 @@ def test_an_object_is_first_used_on_another_stream_than_it_was_made_on(n):
         _same_rows(got, ids, grad)
 
 
-
 @gpu
 def test_check_waits_for_calls_of_other_streams():
     V = 50
@@ -237,7 +235,6 @@ def test_check_waits_for_calls_of_other_streams():
             e.lookup(table, bad)
         with pytest.raises(B.TensairError):
             e.check()
-
 
 
 @gpu
@@ -258,7 +255,6 @@ def test_memory_of_an_object_that_is_gone_is_not_reused_before_its_calls_are_don
         torch.cuda.synchronize()
         _same_rows(got, ids, grad)
         del held
-
 
 
 @gpu
@@ -288,3 +284,30 @@ def test_moments_that_the_optimizer_makes_are_zero_and_held_on_any_stream(bits):
     held = [torch.full((n * bits // 8,), 66, dtype=torch.uint8, device="cuda") for _ in range(3)]
     torch.cuda.synchronize()
     assert torch.equal(first, r) and torch.equal(p, q) and len(held) == 3
+
+
+@gpu
+@pytest.mark.parametrize("n", [5000, 40_000])
+def test_captured_calls_run_beside_others_of_the_same_object(n):
+    V = 3000
+    first, second = _batch(n, V, 3), _batch(n - 100, V, 4)
+    e = _ops().Embedding(V, 4, max_tokens=n)
+    side, outs = torch.cuda.Stream(), []
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        captured = e.gradient_rows(first[1], first[0])
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            graph.replay()
+        outs += [e.gradient_rows(second[1], second[0]) for _ in range(3)]
+    torch.cuda.synchronize()
+    _same_rows(captured, *first)
+    for got in outs:
+        _same_rows(got, *second)
+    with torch.cuda.stream(side):          # the stream that captured, now without a graph
+        got = e.gradient_rows(second[1], second[0])
+    graph.replay()
+    torch.cuda.synchronize()
+    _same_rows(got, *second)
+    _same_rows(captured, *first)
