@@ -46,6 +46,13 @@ def streamed_table(V: int, d: int, batches: int = 20, batch: int = 2048) -> torc
     return table
 
 
+def clip_factor(grads, max_norm: float) -> torch.Tensor:
+    """The factor, on the device, that brings the gradients' global norm down to max_norm; not finite where the norm is not (max_norm
+    over an infinite norm would be a zero like any other), so that the optimizers leave the step out."""
+    norm = torch.stack([g.float().square().sum() for g in grads]).sum().sqrt()
+    return torch.where(torch.isfinite(norm), (max_norm / (norm + 1e-6)).clamp(max=1.0), norm)
+
+
 def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows: int = 1024, window: int = 4, state_bits: int = 8,
           dense: bool = False, lr: float = 3e-3, max_norm: float = 1.0, report: int = 50, quiet: bool = True):
     """Trains the model; returns the table before and after, the ids that occurred, and the reported losses."""
@@ -80,8 +87,7 @@ def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows:
         loss = torch.nn.functional.cross_entropy((h @ w[2].t() + w[3]).float(), target)
         grads = list(torch.autograd.grad(loss, w + [table if dense else x]))
         table.requires_grad_(False)
-        norm = torch.stack([g.float().square().sum() for g in grads]).sum().sqrt()
-        clip = (max_norm / (norm + 1e-6)).clamp(max=1.0)                          # not finite: the step is left out
+        clip = clip_factor(grads, max_norm)
         optimizer.step(grads if dense else grads[:4], grad_scale=clip)
         if not dense:
             embedding.adamw(grads[4], ids, table, m, v, step=step, lr=lr, weight_decay=0.0, grad_scale=clip)

@@ -311,3 +311,40 @@ def test_captured_calls_run_beside_others_of_the_same_object(n):
     torch.cuda.synchronize()
     _same_rows(got, *second)
     _same_rows(captured, *first)
+
+
+# ---------------------------------------------------------------- the example's clipping
+BAD = {"inf": float("inf"), "minus inf": -float("inf"), "nan": float("nan"), "a square that overflows": 1e30}
+
+
+def test_the_clip_factor_is_finite_only_where_the_norm_is():
+    from paper_2211_10280_b200.next_token import clip_factor
+
+    grads = [torch.full((3,), 2.0), torch.full((4,), 1.0, dtype=torch.bfloat16)]      # norm 4
+    assert clip_factor(grads, 5.0).item() == 1.0
+    assert abs(clip_factor(grads, 1.0).item() - 0.25) < 1e-6
+    assert clip_factor([torch.zeros(5)], 1.0).item() == 1.0
+    for bad in BAD.values():
+        assert not torch.isfinite(clip_factor(grads + [torch.tensor([1.0, bad])], 1.0))
+
+
+@gpu
+@pytest.mark.parametrize("bad", BAD.values(), ids=BAD.keys())
+def test_a_step_whose_gradient_norm_is_not_finite_is_left_out(bad):
+    from paper_2211_10280_b200.next_token import clip_factor
+
+    V, d, n = 50, 8, 300
+    ids, _ = _batch(n, V, 1)
+    layer, table, m, v = (torch.randn(x, d, device="cuda") for x in (70, V, V, V))
+    v.square_()
+    grads = [torch.randn(70, d, device="cuda"), torch.randn(n, d, device="cuda")]
+    grads[1][7, 3] = bad
+    clip = clip_factor(grads, 1.0)
+    for bits in (32, 8):
+        opt = _ops().AdamW([layer], state_bits=bits)
+        opt.step([torch.ones_like(layer)])
+        kept = [x.clone() for x in (layer, table, m, v, *opt.m, *opt.v)]
+        opt.step(grads[:1], grad_scale=clip)
+        _ops().Embedding(V, d, max_tokens=n).adamw(grads[1], ids, table, m, v, step=2, grad_scale=clip)
+        for x, y in zip(kept, (layer, table, m, v, *opt.m, *opt.v)):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
