@@ -480,7 +480,9 @@ TENSAIR_API int tensair_raise_error_flags(tensair_ctx* ctx, uint32_t flags);
  * gradient of the table, an AdamW step over many tensors, and the AdamW step of the rows that a batch touched.
  * They need no context.  Each call enqueues its work on `stream` (a cudaStream_t of the calling thread's current
  * device; NULL = the legacy default stream), allocates no device memory, does not synchronise and can be
- * captured into a CUDA graph.  All pointers inside the argument blocks are device pointers that must stay valid until
+ * captured into a CUDA graph.  A graph holds the values of the argument blocks: a captured AdamW call is the step of the number,
+ * seed and learning rate that it was given, at every replay, with that step's bias corrections (tensair_adamw_step therefore
+ * refuses to be captured with 8-bit moments, whose rounding would repeat its random bits).  All pointers inside the argument blocks are device pointers that must stay valid until
  * the stream has passed the call; the argument blocks themselves are read during the call.  Arguments are checked
  * before anything is enqueued; tensair_last_error(NULL) says what the calling thread's last refused call was refused for.
  * Everything is computed in fp32 whatever the tensors' types are, and rounded to nearest once, when it is stored.
@@ -577,7 +579,8 @@ typedef struct tensair_adamw_tensor {
  * for every 336 tensors).  tensors: host.  Moments in 8 bits start as zeros (codes and scales); a block whose largest
  * first moment is below 2^-110 is stored as zeros.  They are rounded stochastically to a neighbouring e4m3 value with random
  * bits that depend on (seed, step, the element's place in the list of tensors) alone; a positive v is never
- * stored as zero; a non-finite moment is stored as NaN and leaves the other elements of its block alone.
+ * stored as zero; a non-finite moment is stored as NaN and leaves the other elements of its block alone.  EINVAL when `stream` is being
+ * captured: replays would round with the same random bits.
  */
 TENSAIR_API int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint32_t state_bits,
                                    const tensair_adamw* adamw, void* stream);

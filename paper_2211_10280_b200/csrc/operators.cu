@@ -278,6 +278,13 @@ int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint
             block0 += (t.n + 255) / 256;
         }
         if (list.empty()) return TENSAIR_OK;
+        if (state_bits == 8) {
+            cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+            const cudaError_t e = cudaStreamIsCapturing((cudaStream_t)stream, &status);
+            if (e != cudaSuccess) return launched(e);
+            TENSAIR_REQUIRE(status == cudaStreamCaptureStatusNone,
+                            "a step with 8-bit moments cannot be captured: replays would repeat its random bits");
+        }
         const int sms = multiprocessors();
         if (!sms) return refuse(TENSAIR_ECUDA, "no CUDA device is current");
         return launched(launch_adamw((cudaStream_t)stream, list.data(), (uint32_t)list.size(), (int)state_bits, c, adamw->step,

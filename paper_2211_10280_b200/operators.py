@@ -199,7 +199,9 @@ class Embedding:
         return out
 
     def adamw(self, grad, ids, table, m, v, step: int, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
-        """The AdamW step, in place, of the rows of table, m and v (float32) whose tokens occur; see AdamW for the formula."""
+        """The AdamW step, in place, of the rows of table, m and v (float32) whose tokens occur; see AdamW for the formula.
+
+        A graph that captures it repeats the step of this number, lr and constants at every replay."""
         flat, n = self._set_tokens(ids)
         grad = self._grad_rows(grad, n)
         rg = self._set_rows(0, grad, n, "grad")
@@ -353,7 +355,10 @@ class AdamW:
         """One step with `grads` (default: the parameters' .grad; a parameter whose gradient is None is left alone).
 
         grad_scale: a float32 on the device that multiplies every gradient; if it is not finite the parameters and moments
-        stay as they are (the step still counts)."""
+        stay as they are (the step still counts).
+
+        A captured step (32-bit moments alone) counts when it is captured; every replay is that step again, with the bias
+        corrections of its number and the lr and other constants of that moment."""
         if grads is None:
             grads = [p.grad for p in self.params]
         _need(len(grads) == len(self.params), "grads: one for each parameter, or None")

@@ -348,3 +348,46 @@ def test_a_step_whose_gradient_norm_is_not_finite_is_left_out(bad):
         _ops().Embedding(V, d, max_tokens=n).adamw(grads[1], ids, table, m, v, step=2, grad_scale=clip)
         for x, y in zip(kept, (layer, table, m, v, *opt.m, *opt.v)):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+# ---------------------------------------------------------------- captured steps
+@gpu
+def test_a_captured_step_is_the_same_step_at_every_replay():
+    V, d, n = 40, 8, 200
+    ids, _ = _batch(n, V, 1)
+    p, g, rows = (torch.randn(x, d, device="cuda") for x in (500, 500, n))
+    state = [torch.randn(V, d, device="cuda") for _ in range(2)] + [torch.rand(V, d, device="cuda")]      # table, m, v
+    q, twin = p.clone(), [x.clone() for x in state]
+    e, opt = _ops().Embedding(V, d, max_tokens=n), _ops().AdamW([p], step=3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step([g])
+        e.adamw(rows, ids, *state, step=4)
+    assert opt.step_count == 4
+    opt.lr = 100.0                     # the graph holds the values that it was captured with
+    plain = _ops().AdamW([q], step=3)
+    for _ in range(3):
+        graph.replay()
+        plain.step_count = 3
+        plain.step([g])
+        e.adamw(rows, ids, *twin, step=4)
+        torch.cuda.synchronize()
+        assert torch.equal(p, q) and all(torch.equal(x, y) for x, y in zip(state, twin))
+
+
+@gpu
+def test_a_step_with_8_bit_moments_is_not_captured():
+    p, g = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    opt = _ops().AdamW([p], state_bits=8)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g.add_(1)
+        with pytest.raises(B.TensairError, match="captured"):
+            opt.step([g])
+    assert opt.step_count == 0
+    graph.replay()
+    opt.step([g])
+    torch.cuda.synchronize()
+    assert (p < 1).all() and (g == 2).all()
