@@ -24,6 +24,10 @@ _INTS = {torch.int32: B.INT32, torch.int64: B.INT64}
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
+# Every tensor that a call has written into is told to autograd: a backward pass that still needs what was there is an error then, as
+# after torch's own in-place operations.
+_written = torch.autograd.graph.increment_version
+_T = torch.Tensor
 _NO_PADDING = -(1 << 63)
 BLOCK = 256                      # elements that share a scale of the 8-bit moments
 
@@ -139,7 +143,7 @@ class Embedding:
         """scale * table[ids], zero rows at padding; shape ids.shape + (d,), of `dtype` (default: the table's)."""
         flat, n = self._set_tokens(ids)
         rt = self._set_rows(0, table, self.V, "table")
-        shaped = out
+        given = shaped = out
         if out is None:
             dtype = dtype or table.dtype
             _need(dtype in _FLOATS, "dtype: float32, bfloat16 or float16")
@@ -154,6 +158,8 @@ class Embedding:
         rc = self._lib.tensair_embedding_lookup(self._at[0], rt, ro, self.scale, self._stream())
         if rc:
             B._check(rc, "tensair_embedding_lookup")
+        if given is not None:
+            _written(given)
         return shaped
 
     def gradient(self, grad, ids, out=None, dtype=None, accumulate=False):
@@ -163,6 +169,7 @@ class Embedding:
         flat, n = self._set_tokens(ids)
         grad = self._grad_rows(grad, n)
         _need(out is not None or not accumulate, "accumulate needs out")
+        given = out
         if out is None:
             out = torch.empty(self.V, self.d, dtype=dtype or grad.dtype, device=self.device)
         rg = self._set_rows(0, grad, n, "grad")
@@ -171,6 +178,8 @@ class Embedding:
         rc = self._lib.tensair_embedding_gradient(self._at[0], rg, ro, self.scale, accumulate, at, self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_gradient")
+        if given is not None:
+            _written(given)
         return out
 
     def gradient_rows(self, grad, ids, out=None):
@@ -180,6 +189,7 @@ class Embedding:
         flat, n = self._set_tokens(ids)
         grad = self._grad_rows(grad, n)
         most = min(n, self.V)
+        given = out
         if out is None:
             out = (torch.empty(most, dtype=torch.int32, device=self.device),
                    torch.empty(most, self.d, dtype=torch.float32, device=self.device),
@@ -196,6 +206,8 @@ class Embedding:
                                                        self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_gradient_rows")
+        if given is not None:
+            _written(given)
         return out
 
     def adamw(self, grad, ids, table, m, v, step: int, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
@@ -214,6 +226,7 @@ class Embedding:
         rc = self._lib.tensair_embedding_adamw(self._at[0], rg, self.scale, rt, rm, rv, self._at[5], at, self.workspace_bytes, stream)
         if rc:
             B._check(rc, "tensair_embedding_adamw")
+        _written((table, m, v))
 
     def __call__(self, table, ids):
         """lookup(table, ids) with autograd: the table's gradient is `gradient` of the incoming one."""
@@ -325,6 +338,11 @@ class AdamW:
         self._at = C.byref(self._hyper)
         self._said, self._left_out = [None, None, None, None], []
         self._numel = [p.numel() for p in params]
+        self._written = self._all_written(())
+
+    def _all_written(self, left_out):
+        """What a step writes that may be part of a graph: parameters and copies, but for those that are left out."""
+        return [x for i, pair in enumerate(zip(self.params, self._copies)) if i not in left_out for x in pair if x is not None]
 
     # The tensors that the descriptors point to, once and for all: tuples, so that an entry cannot be replaced unseen.
     @property
@@ -362,7 +380,7 @@ class AdamW:
         if grads is None:
             grads = [p.grad for p in self.params]
         _need(len(grads) == len(self.params), "grads: one for each parameter, or None")
-        # one list per property, each made by a comprehension: a fifth of the time of a loop with its checks
+        # one list per property, each made in one go: a fifth of the time of a loop with its checks
         left_out = [i for i, g in enumerate(grads) if g is None]
         if left_out:
             grads = list(grads)
@@ -370,21 +388,22 @@ class AdamW:
                 grads[i] = self.params[i]          # stands in for the checks; its n is set to 0
         index, a, said = self.index, self._np, self._said     # what the descriptors say is written again only where it changed
         kinds = [g.dtype for g in grads]
-        if ([g.numel() for g in grads] != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds)) or False in [g.is_contiguous() for g in grads]
-                or [g.get_device() for g in grads] != [index] * len(grads)):
+        if (list(map(_T.numel, grads)) != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds))
+                or False in map(_T.is_contiguous, grads) or list(map(_T.get_device, grads)) != [index] * len(grads)):
             for i, g in enumerate(grads):
                 self._fits(g, self._numel[i], _FLOATS, f"grads[{i}]")
-        ptrs = [g.data_ptr() for g in grads]
+        ptrs = list(map(_T.data_ptr, grads))
         if ptrs != said[0]:
             a["grad"] = said[0] = ptrs
         # a parameter may have been converted or moved: its place and type are looked at in every step, the rest where one of them changed
-        ptrs, param_kinds = [p.data_ptr() for p in self.params], [p.dtype for p in self.params]
+        ptrs, param_kinds = list(map(_T.data_ptr, self.params)), [p.dtype for p in self.params]
         if ptrs != said[1] or param_kinds != said[3]:
             for i, p in enumerate(self.params):
                 self._fits(p, self._numel[i], _FLOATS, f"params[{i}]")
             a["param_type"] = [_FLOATS[k] for k in param_kinds]
             a["param"] = ptrs
             said[1], said[3] = ptrs, param_kinds
+            self._written = self._all_written(self._left_out)
         if kinds != said[2]:
             said[2] = kinds
             a["grad_type"] = [_FLOATS[k] for k in kinds]
@@ -392,6 +411,7 @@ class AdamW:
             a["n"] = self._numel
             a["n"][left_out] = 0
             self._left_out = left_out
+            self._written = self._all_written(left_out)
         _set_adamw(self._hyper, self.lr, self.betas, self.eps, self.weight_decay, self.step_count + 1, self.seed, grad_scale, self.device)
         stream = _current_stream(index)
         if self._known is not None and stream not in self._known and not _capturing():
@@ -404,6 +424,7 @@ class AdamW:
         if rc:
             B._check(rc, "tensair_adamw_step")
         self.step_count += 1
+        _written(self._written)
 
     def moments(self, i: int):
         """(m, v) of parameter i as float32 tensors, whatever they are kept in."""

@@ -391,3 +391,50 @@ def test_a_step_with_8_bit_moments_is_not_captured():
     opt.step([g])
     torch.cuda.synchronize()
     assert (p < 1).all() and (g == 2).all()
+
+
+# ---------------------------------------------------------------- autograd
+def test_a_step_between_forward_and_backward_is_an_error(recorder):
+    p, q = (torch.nn.Parameter(torch.ones(10)) for _ in range(2))
+    copies = [torch.ones(10, dtype=torch.bfloat16) for _ in range(2)]
+    opt = _ops().AdamW([p, q], copies=copies)
+    leaves = [c.detach().requires_grad_() for c in copies]
+    for x in (p, leaves[0]):
+        loss = (x * x).sum()
+        opt.step([torch.ones(10), None])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    for x in (q, leaves[1]):           # what a step leaves alone can still be gone back through
+        loss = (x * x).sum()
+        opt.step([torch.ones(10), None])
+        loss.backward()
+    loss = (q * q).sum()
+    opt.step([torch.ones(10)] * 2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    (p * p).sum().backward()
+
+
+@gpu
+def test_calls_of_an_embedding_tell_autograd_what_they_wrote():
+    V, d, n = 20, 4, 30
+    ids, grad = _batch(n, V, 1)
+    table, m, v = (torch.ones(V, d, device="cuda") for _ in range(3))
+    e = _ops().Embedding(V, d, max_tokens=n)
+    leaf = table.detach().requires_grad_()
+    for call in (lambda: e.adamw(grad, ids, table, m, v, step=1), lambda: e.gradient(grad, ids, out=table),
+                 lambda: e.gradient(grad, ids, out=table, accumulate=True), lambda: e.lookup(m, ids[:V], out=table),
+                 lambda: e.lookup(m, ids[:V].view(4, 5), out=table.view(4, 5, d)),
+                 lambda: e.gradient_rows(grad, ids, out=(torch.empty(n, dtype=torch.int32, device="cuda"), table, torch.empty(1, dtype=torch.int32, device="cuda")))):
+        loss = (leaf * leaf).sum()
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    loss = e(leaf, ids).sum()          # needs the ids alone
+    e.adamw(grad, ids, table, m, v, step=2)
+    loss.backward()
+    with torch.inference_mode():       # tensors without a version
+        t = torch.ones(V, d, device="cuda")
+        e.adamw(grad, ids, t, t.clone(), t.clone(), step=1)
+        _ops().AdamW([t]).step([torch.ones_like(t)])
+    torch.cuda.synchronize()
