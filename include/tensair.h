@@ -571,14 +571,14 @@ typedef struct tensair_adamw_tensor {
     double lr_factor;         /* on lr, for this tensor */
     double decay_factor;      /* on weight_decay, for this tensor */
     uint32_t param_type, grad_type, copy_type;
-    uint32_t reserved;
+    uint32_t skip;            /* not 0: the tensor is left alone in this step, and keeps its place in the list; only n is looked at */
 } tensair_adamw_tensor;
 
 /*
  * One AdamW step of `count` tensors, at once: one launch for each combination of parameter and gradient type (and
  * for every 336 tensors).  tensors: host.  Moments in 8 bits start as zeros (codes and scales); a block whose largest
  * first moment is below 2^-110 is stored as zeros.  They are rounded stochastically to a neighbouring e4m3 value with random
- * bits that depend on (seed, step, the element's place in the list of tensors) alone; a positive v is never
+ * bits that depend on (seed, step, the element's place in the list of tensors, skipped ones included) alone; a positive v is never
  * stored as zero; a non-finite moment is stored as NaN and leaves the other elements of its block alone.  EINVAL when `stream` is being
  * captured: replays would round with the same random bits.
  */

@@ -81,7 +81,7 @@ class AdamwTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_uint64), ("lr_factor", C.c_double),
                 ("decay_factor", C.c_double), ("param_type", C.c_uint32), ("grad_type", C.c_uint32),
-                ("copy_type", C.c_uint32), ("reserved", C.c_uint32)]
+                ("copy_type", C.c_uint32), ("skip", C.c_uint32)]
 
 
 class TensairError(RuntimeError):

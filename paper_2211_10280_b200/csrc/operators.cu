@@ -259,6 +259,9 @@ int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint
         for (uint64_t i = 0; i < count; ++i) {
             const tensair_adamw_tensor& t = tensors[i];
             TENSAIR_REQUIRE(t.n < (1ull << 40), "tensors: n must be below 2^40");
+            const uint64_t place = block0;
+            block0 += (t.n + 255) / 256;
+            if (t.skip) continue;
             TENSAIR_REQUIRE(is_float_type(t.param_type) && is_float_type(t.grad_type), "tensors: param_type or grad_type");
             TENSAIR_REQUIRE(!t.copy || t.copy_type == TENSAIR_BFLOAT16 || t.copy_type == TENSAIR_FLOAT16,
                             "tensors: a copy must be TENSAIR_BFLOAT16 or TENSAIR_FLOAT16");
@@ -271,11 +274,10 @@ int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint
                             (state_bits == 8 || ((uintptr_t)t.m % 4 == 0 && (uintptr_t)t.v % 4 == 0)) &&
                             (uintptr_t)t.m_scale % 4 == 0 && (uintptr_t)t.v_scale % 4 == 0 && (uintptr_t)t.copy % 2 == 0,
                             "tensors: a pointer is not aligned to its type");
-            list.push_back(AdamwTensor{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, block0,
+            list.push_back(AdamwTensor{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.n, place,
                                        (float)(c.step_size * t.lr_factor),
                                        (float)(1 - adamw->lr * t.lr_factor * adamw->weight_decay * t.decay_factor),
                                        t.param_type, t.grad_type, t.copy_type});
-            block0 += (t.n + 255) / 256;
         }
         if (list.empty()) return TENSAIR_OK;
         if (state_bits == 8) {

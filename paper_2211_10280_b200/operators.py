@@ -280,7 +280,8 @@ class AdamW:
         p <- p (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
 
     state_bits 32 keeps m and v as float32; 8 keeps m and sqrt(v) as float8_e4m3fn with a float32 scale for every 256 elements
-    (`m_scale`, `v_scale`), rounded stochastically with bits that depend on `seed`, the step and the element's place alone.
+    (`m_scale`, `v_scale`), rounded stochastically with bits that depend on `seed`, the step and the element's place in the list of
+    parameters alone, whichever of them have a gradient.
     copies: tensors (bfloat16 or float16, or None) that receive the updated parameters, rounded.  lr_factors and
     decay_factors: per-parameter factors on lr and weight_decay.  state: dict of lists to start from (m, v and for 8 bits
     m_scale, v_scale; they become the optimizer's own), zeros by default; step: steps already made.
@@ -385,7 +386,7 @@ class AdamW:
         if left_out:
             grads = list(grads)
             for i in left_out:
-                grads[i] = self.params[i]          # stands in for the checks; its n is set to 0
+                grads[i] = self.params[i]          # stands in for the checks
         index, a, said = self.index, self._np, self._said     # what the descriptors say is written again only where it changed
         kinds = [g.dtype for g in grads]
         if (list(map(_T.numel, grads)) != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds))
@@ -408,8 +409,8 @@ class AdamW:
             said[2] = kinds
             a["grad_type"] = [_FLOATS[k] for k in kinds]
         if left_out != self._left_out:
-            a["n"] = self._numel
-            a["n"][left_out] = 0
+            a["skip"] = 0
+            a["skip"][left_out] = 1
             self._left_out = left_out
             self._written = self._all_written(left_out)
         _set_adamw(self._hyper, self.lr, self.betas, self.eps, self.weight_decay, self.step_count + 1, self.seed, grad_scale, self.device)

@@ -90,6 +90,7 @@ class _Recorder:
 
     def tensair_adamw_step(self, tensors, count, bits, hyper, stream):
         self.asked.append([(t.param, t.param_type, t.grad, t.grad_type, t.m, t.v, t.copy, t.n) for t in tensors[:count]])
+        self.skipped = [t.skip for t in tensors[:count]]
         return 0
 
 
@@ -438,3 +439,36 @@ def test_calls_of_an_embedding_tell_autograd_what_they_wrote():
         e.adamw(grad, ids, t, t.clone(), t.clone(), step=1)
         _ops().AdamW([t]).step([torch.ones_like(t)])
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------- parameters without a gradient
+def test_parameters_without_a_gradient_keep_their_place(recorder):
+    sizes = [300, 1, 7, 513]
+    ps = [torch.ones(n) for n in sizes]
+    opt = _ops().AdamW(ps)
+    for left in ((), (1,), (0, 3), (), (2,)):
+        opt.step([None if i in left else torch.ones(n) for i, n in enumerate(sizes)])
+        assert recorder.skipped == [int(i in left) for i in range(4)] and [t[7] for t in recorder.asked[-1]] == sizes
+
+
+def test_a_skipped_tensor_is_not_looked_at():
+    t = (B.AdamwTensor * 2)(B.AdamwTensor(n=10, skip=1, lr_factor=float("nan"), param_type=9), B.AdamwTensor(n=0))
+    h = B.Adamw(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+    assert B.lib().tensair_adamw_step(t, 2, 8, h, None) == B.OK          # nothing to do
+    t[0].n = 2 ** 40
+    assert B.lib().tensair_adamw_step(t, 2, 8, h, None) == B.EINVAL
+
+
+@gpu
+def test_rounding_of_8_bit_moments_does_not_depend_on_the_gradients_that_others_have():
+    sizes = [1000, 300, 0, 5000]
+    gs = [torch.linspace(0.1, 1.7, n, device="cuda") for n in sizes]
+    kept = []
+    for use in (gs, [gs[0], None, gs[2], gs[3]], [None, None, None, gs[3]]):
+        opt = _ops().AdamW([torch.ones(n, device="cuda") for n in sizes], state_bits=8, seed=5)
+        opt.step(use)
+        opt.step(use)
+        assert use[1] is not None or not opt.m[1].float().any()
+        kept.append((opt.m[3].view(torch.uint8), opt.v[3].view(torch.uint8), opt.params[3]))
+    for other in kept[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(kept[0], other))
