@@ -220,7 +220,8 @@ __device__ __forceinline__ void range8(const Two (&x)[4], uint32_t* low, uint32_
 }
 
 // Square roots, correctly rounded like __fsqrt_rn, of values in [2^-96, 2^128): Newton's step from the approximate reciprocal root with
-// the residual x - y^2 formed exactly by a fused multiply-add (Markstein, IBM J. Res. Dev. 34, 1990).  Two at a time.
+// the residual x - y^2 formed by a fused multiply-add (Markstein, IBM J. Res. Dev. 34, 1990).  Two at a time.  Not proven, counted: all
+// 1,879,048,192 values of the range have the bits of __fsqrt_rn.
 __device__ __forceinline__ Two roots(Two x) {
     const float2 f = x.floats();
     float r0, r1;

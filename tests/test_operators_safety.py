@@ -472,3 +472,66 @@ def test_rounding_of_8_bit_moments_does_not_depend_on_the_gradients_that_others_
         kept.append((opt.m[3].view(torch.uint8), opt.v[3].view(torch.uint8), opt.params[3]))
     for other in kept[1:]:
         assert all(torch.equal(x, y) for x, y in zip(kept[0], other))
+
+
+# ---------------------------------------------------------------- what 8-bit moments are made of, bit for bit
+@gpu
+def test_roots_of_second_moments_over_the_whole_range_of_exponents():
+    """Blocks of one value each, from below 2^-96, where the kernel takes another way to its roots, to 2^127: a block's scale is its
+    root, as torch.sqrt rounds it, over 448.  With beta2 = 0.3 the second moments are no squares."""
+    gen = torch.Generator("cuda").manual_seed(0)
+    size = torch.ldexp(torch.rand(60_000, device="cuda", generator=gen) + 1, torch.randint(-52, 63, (60_000,), device="cuda", generator=gen))
+    ends = torch.ldexp(torch.linspace(0.99, 1.5, 2000, device="cuda"), torch.tensor(-48, device="cuda"))      # around 2^-96
+    size = torch.cat([size, ends, torch.ldexp(torch.ones(114, device="cuda"), torch.arange(-51, 63, device="cuda"))])
+    size = size * torch.where(torch.arange(size.numel(), device="cuda") % 2 > 0, -1.0, 1.0)
+    opt = _ops().AdamW([torch.zeros(256 * size.numel(), device="cuda")], lr=0.0, betas=(0.9, 0.3), state_bits=8)
+    opt.step([size.repeat_interleave(256)])
+    v = (size * size) * torch.tensor(1 - 0.3, device="cuda")
+    over = torch.tensor(1 / 448, device="cuda")
+    assert (v < 2.0 ** -96).any() and (v > 2.0 ** 124).any() and torch.isfinite(v).all()
+    assert torch.equal(opt.v_scale[0], v.sqrt() * over)
+    assert torch.equal(opt.m_scale[0], (size * torch.tensor(1 - 0.9, device="cuda")).abs() * over)
+
+
+def _bits16(groups, step, seed):
+    """16 random bits for every element, from Philox4x32-10 over (group of 8 elements, step) with the seed as its key."""
+    low = 0xFFFFFFFF
+    at = torch.arange(groups, device="cuda")
+    c, key = [at, torch.zeros_like(at), torch.full_like(at, step), torch.full_like(at, 5 << 24)], [seed & low, seed >> 32]
+    for _ in range(10):
+        a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+        c = [((b >> 32) & low) ^ c[1] ^ key[0], b & low, ((a >> 32) & low) ^ c[3] ^ key[1], a & low]
+        key = [(key[0] + 0x9E3779B9) & low, (key[1] + 0xBB67AE85) & low]
+    words = torch.stack(c, 1)
+    return torch.stack([words & 0xFFFF, words >> 16], 2).view(-1).to(torch.int32)
+
+
+@gpu
+@pytest.mark.parametrize("spread", [0.0, 3.0, 12.0])
+def test_every_code_of_8_bit_moments_is_that_of_separately_rounded_operations(spread):
+    """Every element of both moments, from gradients of one size or of sizes over many orders of magnitude (codes in the format's
+    subnormal range), step after step from what the step before stored."""
+    n, seed = 256 * 500, (3 << 32) + 11
+    gen = torch.Generator("cuda").manual_seed(1)
+    opt = _ops().AdamW([torch.zeros(n, device="cuda")], state_bits=8, seed=seed)
+    m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    c = [torch.tensor(x, device="cuda") for x in (0.9, 1 - 0.9, 0.999, 1 - 0.999)]
+    for step in range(1, 5):
+        g = torch.randn(n, device="cuda", generator=gen) * torch.exp(torch.randn(n, device="cuda", generator=gen) * spread) * 1e-3
+        opt.step([g])
+        m = m * c[0] + g * c[1]
+        v = (v * v) * c[2] + (g * g) * c[3]                   # v: the stored root
+        bits = _bits16(n // 8, step, seed)
+        for x, code, scale in ((m, opt.m[0], opt.m_scale[0]), (v.sqrt(), opt.v[0], opt.v_scale[0])):
+            finite = torch.isfinite(x)                        # a square that overflows is kept as NaN, and not in the block's scale
+            top = torch.where(finite, x.abs(), 0.0).view(-1, 256).amax(1)
+            assert torch.equal(scale, top * torch.tensor(1 / 448, device="cuda"))
+            y = (x.abs().view(-1, 256) * ((1 / top) * 448)[:, None]).view(-1)
+            if code is opt.v[0]:
+                y = torch.where((x > 0) & (y < 2.0 ** -9), 2.0 ** -9, y)
+            cut = ((y.view(torch.int32) + (bits << 4) + 8) & -0x100000).view(torch.float32).clamp(max=448.0)
+            want = torch.copysign(torch.where(y < 2.0 ** -6, y, cut), x).to(torch.float8_e4m3fn)
+            assert torch.equal(code.view(torch.uint8)[finite], want.view(torch.uint8)[finite]), step
+            assert torch.isnan(code[~finite].float()).all() and finite.float().mean() > 0.99
+        m = (opt.m[0].float().view(-1, 256) * opt.m_scale[0][:, None]).view(-1)
+        v = (opt.v[0].float().view(-1, 256) * opt.v_scale[0][:, None]).view(-1)
