@@ -79,8 +79,8 @@ constexpr uint32_t kErrBounds = 4u;     // checked build: an index left its arra
 constexpr uint32_t kErrOverflow = 8u;   // a merged message had more rows than its slot holds; the rest was dropped
 
 // Sizes of the arrays that kernels index with values computed from data.  In a checked build (-DTENSAIR_BOUNDS)
-// every such index is compared with its bound first; one out of bounds raises kErrBounds in the error word and the
-// access is skipped - nothing traps.  In a normal build the checks compile to nothing.
+// every such index is compared with its bound first; one out of bounds raises kErrBounds in the error word (where there is
+// one) and the access is skipped - nothing traps.  In a normal build the checks compile to nothing.
 struct Limits {
     uint32_t* err;
     uint32_t table_rows;   // 2V rows of one replica's unified table
@@ -93,14 +93,15 @@ struct Limits {
     uint32_t chunks;       // entries of the chunk list and of the chunk partials
 };
 #ifdef TENSAIR_BOUNDS
-__device__ inline bool in_bounds(const Limits& lim, uint64_t index, uint64_t bound) {
+__device__ inline bool in_bounds(uint32_t* err, uint64_t index, uint64_t bound) {
     if (index < bound) return true;
-    atomicOr(lim.err, kErrBounds);
+    if (err) atomicOr(err, kErrBounds);
     return false;
 }
 #else
-__device__ __forceinline__ bool in_bounds(const Limits&, uint64_t, uint64_t) { return true; }
+__device__ __forceinline__ bool in_bounds(uint32_t*, uint64_t, uint64_t) { return true; }
 #endif
+__device__ __forceinline__ bool in_bounds(const Limits& lim, uint64_t index, uint64_t bound) { return in_bounds(lim.err, index, bound); }
 
 struct Shape {
     uint32_t V, d, d4, stride, w, k, K1;

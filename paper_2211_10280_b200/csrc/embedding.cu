@@ -123,9 +123,12 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
     if (kKind == kSumAdamw && !adamw_grad_scale(a.adamw, &grad_scale)) return;
     const uint32_t n_valid = a.s.info[0];
     if (kKind == kSumRows && begin == 0 && vec0 == 0 && tid == 0) *a.out_count = a.s.info[1];
-    if (begin >= n_valid) return;
+    if (begin >= n_valid || !in_bounds(a.s.err, n_valid, a.n + 1)) return;
     const uint32_t before = a.s.span_rank[blockIdx.x];           // tokens that begin before the span
-    if (tid < kSpan + kWindow && begin + tid < n_valid) pos[tid] = a.s.pos[begin + tid];
+    if (tid < kSpan + kWindow && begin + tid < n_valid) {
+        const uint32_t p = a.s.pos[begin + tid];
+        pos[tid] = in_bounds(a.s.err, p, a.n) ? p : 0;
+    }
     const uint32_t at = begin + tid;
     const bool mine = tid < kSpan && at < n_valid;               // this thread has a position of the span
     uint32_t key = 0;
@@ -147,6 +150,8 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
         if (mine) {
             const unsigned long long heads = (unsigned long long)head_masks[1] << 32 | head_masks[0];
             rank = before + __popcll(heads & (~0ull >> (63 - tid))) - 1;
+        }
+        if (mine && in_bounds(a.s.err, rank, a.n < a.V ? a.n : a.V) && in_bounds(a.s.err, key, a.V)) {
             const uint32_t start = a.s.seg_start[rank], end = a.s.seg_start[rank + 1];
             const bool large = end - start > kWindow;
             part = head || (large && tid % kWindow == 0);
@@ -160,7 +165,8 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
                     const uint32_t from = at / kWindow, to = (end - 1) / kWindow;
                     const bool many = to - from > kFewPieces;
                     const uint32_t slot = atomicAdd(a.s.info + (many ? 3 : 2), 1u);
-                    a.large[many ? slot : a.n / (kWindow + 1) - 1 - slot] = make_uint4(from, rank, to, key);
+                    if (in_bounds(a.s.err, slot, a.n / (kWindow + 1)))
+                        a.large[many ? slot : a.n / (kWindow + 1) - 1 - slot] = make_uint4(from, rank, to, key);
                 }
             }
         }
@@ -182,6 +188,7 @@ k_token_sums(const __grid_constant__ SumArgs a, uint32_t all_vecs, uint32_t slab
         }
         const uint4 p = parts[q];
         const uint32_t from = p.x & 0xFF, count = p.x >> 8 & 0xFF, what = p.x >> 16 & 0xFF;
+        if (!in_bounds(a.s.err, from + count, kSpan + kWindow + 1)) continue;
         const uint32_t col = (vec0 + vec) * E;
         const TG* grad = (const TG*)a.grad.data + col;
         Finish<kKind, TO, C> row;
@@ -215,9 +222,13 @@ k_join_pieces(const __grid_constant__ SumArgs a, uint32_t slabs) {
         const bool shared = w < many;      // the block's warps share a token
         const uint64_t item = shared ? w : (w - many) * kJoinWarps + wid;
         const uint32_t q = (uint32_t)(item / slabs);
-        const bool in = shared || q < a.s.info[2];
+        bool in = (shared || q < a.s.info[2]) && in_bounds(a.s.err, q, a.n / (kWindow + 1));
         uint4 c = make_uint4(0, 0, 0, 0);
-        if (in) c = a.large[shared ? q : a.n / (kWindow + 1) - 1 - q];
+        if (in) {
+            c = a.large[shared ? q : a.n / (kWindow + 1) - 1 - q];
+            in = in_bounds(a.s.err, c.z, (a.n + kWindow - 1) / kWindow) && in_bounds(a.s.err, c.x, c.z + 1) && in_bounds(a.s.err, c.w, a.V) &&
+                 in_bounds(a.s.err, c.y, a.n < a.V ? a.n : a.V);
+        }
         const uint32_t col = ((uint32_t)(item - (uint64_t)q * slabs) * 32 + lane) * E;
         const uint32_t rest = c.z - c.x;   // pieces after the first
         const uint32_t share = shared ? (rest + kJoinWarps - 1) / kJoinWarps : rest;

@@ -37,7 +37,7 @@ static_assert(offsetof(ShortShared<kFewTokens>, parts) % 16 == 0, "the keys that
 static_assert(offsetof(ShortShared<1024>, digit_base) % 8 == 0, "totals are written two at a time");
 // After it: counters of the radix sort (kThreads 1,024), then the sums of the pieces: [slot][columns of the block].
 template <int kThreads>
-constexpr uint32_t max_pieces() { return kThreads / 16 + kThreads / 17 + 1; }
+constexpr uint32_t kMaxPieces = kThreads / 16 + kThreads / 17 + 1;
 
 template <SumKind kKind, typename TG, typename TO, typename C, int kThreads>
 __global__ void __launch_bounds__(kThreads)
@@ -63,7 +63,8 @@ k_short_sums(const __grid_constant__ SumArgs a, TokenIds t, uint32_t all_vecs, u
             const uint32_t start = block_exclusive(total, sh.warp_sums, nullptr);
             if (tid < bins) sh.digit_base[tid] = start;
             __syncthreads();
-            sh.items[sh.digit_base[digit] + place] = item;
+            const uint32_t to = sh.digit_base[digit] + place;
+            if (in_bounds(t.err, to, kThreads)) sh.items[to] = item;
             __syncthreads();
             item = sh.items[tid];
         }
@@ -79,12 +80,13 @@ k_short_sums(const __grid_constant__ SumArgs a, TokenIds t, uint32_t all_vecs, u
             place += (k.x < item.x || (k.x == item.x && 4 * x < tid)) + (k.y < item.x || (k.y == item.x && 4 * x + 1 < tid)) +
                      (k.z < item.x || (k.z == item.x && 4 * x + 2 < tid)) + (k.w < item.x || (k.w == item.x && 4 * x + 3 < tid));
         }
-        sh.items[tid < n ? place : tid] = item;        // places past the batch stay where they are
+        const uint32_t to = tid < n ? place : tid;     // places past the batch stay where they are
+        if (in_bounds(t.err, to, kThreads)) sh.items[to] = item;
         __syncthreads();
         item = sh.items[tid];
     }
     // ---- the tokens and their parts
-    sh.pos[tid] = item.y;
+    sh.pos[tid] = tid >= n || in_bounds(t.err, item.y, n) ? item.y : 0;
     const bool valid = item.x < t.V;
     const bool head = valid && (tid == 0 || sh.items[tid - 1].x != item.x);
     uint32_t tokens;
@@ -119,12 +121,14 @@ k_short_sums(const __grid_constant__ SumArgs a, TokenIds t, uint32_t all_vecs, u
         const uint32_t q = w / vecs, vec = w - q * vecs, col = (vec0 + vec) * E;
         const uint2 p = sh.parts[q];
         const uint32_t first = p.x & 0x7FF, rows = p.x >> 11 & 0x3F, key = sh.items[first].x;
+        if (!in_bounds(t.err, first + rows, n + 1) || !in_bounds(t.err, key, t.V)) continue;
         Finish<kKind, TO, C> row;
         if (!(p.x >> 31)) row.fetch(a, key, col);
         float sum[E];
         add_rows<kKind, C>((const TG*)a.grad.data + col, a.grad.stride, sh.pos + first, rows, a.d - col, sum);
         if (!(p.x >> 31)) row.put(a, grad_scale, key, p.y, col, sum);
-        else store_pack<float, E>(sums + ((p.x >> 17 & 0x3FFF) * slab_vecs + vec) * E, sum);
+        else if (in_bounds(t.err, p.x >> 17 & 0x3FFF, kMaxPieces<kThreads>))
+            store_pack<float, E>(sums + ((p.x >> 17 & 0x3FFF) * slab_vecs + vec) * E, sum);
     }
     if (!pieces) return;
     __syncthreads();
@@ -133,6 +137,7 @@ k_short_sums(const __grid_constant__ SumArgs a, TokenIds t, uint32_t all_vecs, u
         const uint2 p = sh.parts[sh.large[q]];
         const uint32_t first = p.x & 0x7FF, key = sh.items[first].x;
         const uint32_t slot0 = p.x >> 17 & 0x3FFF, count = (starts[p.y + 1] - first + kWindow - 1) / kWindow;
+        if (!in_bounds(t.err, slot0 + count, kMaxPieces<kThreads> + 1) || !in_bounds(t.err, key, t.V)) continue;
         Finish<kKind, TO, C> row;
         row.fetch(a, key, col);
         float sum[E];
@@ -153,7 +158,7 @@ cudaError_t launch_short(cudaStream_t stream, const SumArgs& a, const TokenIds& 
     while (key_bits < 32 && t.V >> key_bits) ++key_bits;
     const uint32_t passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits, digit_bits = (key_bits + passes - 1) / passes;
     const uint32_t vecs = (a.d + C::E - 1) / C::E;
-    const size_t starts = (size_t)(kThreads + 2) * 2 / 16 * 16 + 16, sums = (size_t)max_pieces<kThreads>() * kShortVecs * C::E * 4;
+    const size_t starts = (size_t)(kThreads + 2) * 2 / 16 * 16 + 16, sums = (size_t)kMaxPieces<kThreads> * kShortVecs * C::E * 4;
     const size_t counters = kThreads == 1024 ? (size_t)kSortBlockWarps * 2 << digit_bits : 0;
     const size_t shared = (sizeof(ShortShared<kThreads>) + 15) / 16 * 16 + (starts + sums > counters ? starts + sums : counters);
     auto kernel = k_short_sums<kKind, TG, TO, C, kThreads>;

@@ -125,7 +125,7 @@ int gradient_call(const tensair_tokens* tokens, const tensair_rows* grad, float 
     }
     uint8_t* w = (uint8_t*)workspace;
     a.s = SortedTokens{(uint32_t*)(w + l.key), (uint32_t*)(w + l.pos), (uint32_t*)(w + l.seg_start),
-                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info)};
+                       (uint32_t*)(w + l.span_rank), (uint32_t*)(w + l.info), tokens->error};
     a.partials = (float*)(w + l.partials);
     a.partial_stride = l.partial_stride;
     a.large = (uint4*)(w + l.large);

@@ -17,7 +17,7 @@ namespace tensair {
 struct TokenIds {
     const void* ids;
     int64_t padding;      // an id equal to this stands for "no token"
-    uint32_t* err;        // nullable: receives kErrBadToken
+    uint32_t* err;        // nullable: receives kErrBadToken (checked build: and kErrBounds)
     uint32_t n, V;
     bool wide;            // 64-bit ids
 };
@@ -127,6 +127,7 @@ struct SortedTokens {
     uint32_t* seg_start;   // [min(n, V) + 1] first sorted position of each distinct token, then n_valid
     uint32_t* span_rank;   // [spans] distinct tokens that begin before the span
     uint32_t* info;        // [0] n_valid, [1] distinct tokens, [2], [3] set to zero: entries of SumArgs::large
+    uint32_t* err;         // nullable: the caller's error word (checked build)
 };
 constexpr uint32_t kSpan = 64;         // sorted positions
 // Sorted positions; a token with more is added up in pieces.  Whole table bf16 (16,384 tokens of 512), rows, AdamW rows (65,536 of 300):

@@ -55,6 +55,8 @@ __device__ void clear_part(const ClearRows& c, uint64_t part, uint64_t parts) {
     }
 }
 
+__device__ __forceinline__ uint32_t most_tokens(uint32_t n, uint32_t V) { return n < V ? n : V; }   // distinct ones; seg_start has one place more
+
 struct ClusterShared {
     uint32_t warp_sums[kSortBlockWarps];
     uint32_t heads[kMaxCluster], valid[kMaxCluster];   // of every block of the cluster, written by that block
@@ -100,7 +102,7 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
         if (tid < bins) sh.digit_base[tid] = digit_start + before;
         __syncthreads();
         const uint32_t to = sh.digit_base[digit] + place;
-        cluster.map_shared_rank(sh.items, to / kSortBlock)[to % kSortBlock] = item;
+        if (in_bounds(t.err, to, blocks * kSortBlock)) cluster.map_shared_rank(sh.items, to / kSortBlock)[to % kSortBlock] = item;
         cluster.sync();
         item = sh.items[tid];
     }
@@ -123,17 +125,18 @@ k_cluster_sort(TokenIds t, SortedTokens s, uint32_t key_bits, uint32_t digit_bit
         all_heads += sh.heads[b];
         all_valid += sh.valid[b];
     }
+    const uint32_t most = most_tokens(t.n, t.V);
     if (at < t.n) {
         s.key[at] = item.x;
         s.pos[at] = item.y;
-        if (head) s.seg_start[before] = at;
+        if (head && in_bounds(t.err, before, most)) s.seg_start[before] = at;
         if (at % kSpan == 0) s.span_rank[at / kSpan] = before;
     }
     if (at == 0) {
         s.info[0] = all_valid;
         s.info[1] = all_heads;
         s.info[2] = s.info[3] = 0;
-        s.seg_start[all_heads] = all_valid;
+        if (in_bounds(t.err, all_heads, most + 1)) s.seg_start[all_heads] = all_valid;
     }
     after_previous_launch();     // the launch that clears the table, if there is one, has run beside this one and ends with it
 }
@@ -203,6 +206,7 @@ k_tile_scatter(uint32_t n, const uint2* items, uint2* out, const uint16_t* place
     __syncthreads();
     if (at >= n) return;
     const uint32_t to = base[item.x >> shift & (bins - 1)] + rank;     // below n: the places past the batch come last
+    if (!in_bounds(s.err, to, n)) return;
     if (kLast) {
         s.key[to] = item.x;
         s.pos[to] = item.y;
@@ -230,7 +234,7 @@ k_list_tokens(uint32_t n, uint32_t V, uint32_t tiles, SortedTokens s, ClearShare
     const uint32_t key = at < n ? s.key[at] : 0xFFFFFFFFu;
     const bool head = key < V && (at == 0 || s.key[at - 1] != key);
     const uint32_t h = run + block_exclusive(head, warp_sums, &heads);
-    if (at >= n) return;
+    if (at >= n || !in_bounds(s.err, h + head, most_tokens(n, V) + 1)) return;
     if (head) s.seg_start[h] = at;
     if (at % kSpan == 0) s.span_rank[at / kSpan] = h;
     const bool ends = at + 1 == n || s.key[at + 1] >= V;
@@ -364,7 +368,7 @@ k_write_tokens(const item_t* __restrict__ items, uint32_t n, uint32_t V, const u
         const bool head = in && begins_token(items, i, V);
         uint32_t heads;
         const uint32_t h = run + block_exclusive(head, warp_sums, &heads);
-        if (in) {
+        if (in && in_bounds(s.err, h + head, most_tokens(n, V) + 1)) {
             const uint32_t key = item_key(items[i]);
             s.key[i] = key;
             s.pos[i] = item_payload(items[i]);
@@ -435,7 +439,7 @@ cudaError_t launch_token_sort(cudaStream_t stream, const TokenIds& t, const Sort
     }
     uint64_t launches = 0;
     Launcher L{stream, &launches, 0, nullptr};
-    L.lim.err = s.info;    // only read by the checked build's scatter, whose positions are below n by construction
+    L.lim.err = s.err;     // of the checked build's scatter
     k_token_items<<<(t.n + kTileThreads - 1) / kTileThreads, kTileThreads, 0, stream>>>(t, w.a);
     item_t* sorted = nullptr;
     e = launch_sort(L, w.a, w.b, t.n, key_bits, w.hist, &sorted);

@@ -535,3 +535,24 @@ def test_every_code_of_8_bit_moments_is_that_of_separately_rounded_operations(sp
             assert torch.isnan(code[~finite].float()).all() and finite.float().mean() > 0.99
         m = (opt.m[0].float().view(-1, 256) * opt.m_scale[0][:, None]).view(-1)
         v = (opt.v[0].float().view(-1, 256) * opt.v_scale[0][:, None]).view(-1)
+
+
+# ---------------------------------------------------------------- the checked build
+@gpu
+@pytest.mark.parametrize("n", [1, 200, 256, 257, 1024, 1025, 9000, 16_384, 16_385, 100_000, 131_073, 300_000])
+def test_no_index_of_a_call_leaves_its_array(n):
+    """With the checked build (TENSAIR_CHECKED=1) every index that is computed from data is compared with its bound; the error word
+    stays clean over all lengths and forms, over vocabularies below and above the batch."""
+    d = 5
+    for V in (1, 300, 700_000):
+        ids, grad = _batch(n, V, n, d)
+        e = _ops().Embedding(V, d, max_tokens=n, padding_id=2)
+        held = ids != 2
+        _same_rows(e.gradient_rows(grad, ids), ids[held], grad[held])
+        want = torch.zeros(V, d, device="cuda").index_add_(0, ids[held], grad[held])
+        table = e.gradient(grad, ids)
+        assert torch.equal(table, want)
+        assert torch.equal(e.gradient(grad, ids, out=table, accumulate=True), 2 * want)
+        e.adamw(grad, ids, table, torch.zeros_like(want), torch.zeros_like(want), step=1)
+        e.lookup(table, ids)
+        e.check()
