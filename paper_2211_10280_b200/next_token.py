@@ -7,7 +7,8 @@
    window, two linear layers, softmax over the vocabulary.
 3. Each step looks rows up (`Embedding.lookup`), takes gradients, clips them by their global norm on the device, and
    updates the layers with `AdamW` (one launch for all of them) and the table with `Embedding.adamw`, which reads the
-   batch's gradient rows and touches only the rows of its tokens.  With --dense the table's whole gradient is made
+   batch's gradient rows and touches only the rows of its tokens; the table's share of the norm is that of its touched rows
+   (`Embedding.gradient_rows`, the form that a message has).  With --dense the table's whole gradient is made
    (autograd through `Embedding.__call__`) and the table is one more tensor of the AdamW step.
 Nothing in a step waits for the device; the loss is read every `report` steps.
 """
@@ -53,6 +54,18 @@ def clip_factor(grads, max_norm: float) -> torch.Tensor:
     return torch.where(torch.isfinite(norm), (max_norm / (norm + 1e-6)).clamp(max=1.0), norm)
 
 
+def rows_slot(most: int, d: int):
+    """Room for the touched rows of a batch of up to `most` tokens, as `Embedding.gradient_rows` fills it."""
+    return (torch.empty(most, dtype=torch.int32, device="cuda"), torch.zeros(most, d, device="cuda"),
+            torch.empty(1, dtype=torch.int32, device="cuda"))
+
+
+def touched_rows(embedding, grad, ids, slot) -> torch.Tensor:
+    """The rows of the table's gradient that are not zero, with zeros behind them: their number stays on the device."""
+    _, rows, count = embedding.gradient_rows(grad, ids, out=slot)
+    return torch.where(torch.arange(rows.shape[0], device="cuda")[:, None] < count, rows, 0.0)
+
+
 def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows: int = 1024, window: int = 4, state_bits: int = 8,
           dense: bool = False, lr: float = 3e-3, max_norm: float = 1.0, report: int = 50, quiet: bool = True):
     """Trains the model; returns the table before and after, the ids that occurred, and the reported losses."""
@@ -66,7 +79,7 @@ def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows:
         c.copy_(w.detach())
     params, decay = [w.detach() for w in layers], [1.0, 0.0, 1.0, 0.0]
     embedding = operators.Embedding(V, d, max_tokens=rows * window, scale=math.sqrt(d))
-    m, v = torch.zeros_like(table), torch.zeros_like(table)
+    m, v, slot = torch.zeros_like(table), torch.zeros_like(table), rows_slot(min(V, rows * window), d)
     if dense:
         params, copies, decay = params + [table], copies + [None], decay + [0.0]
     optimizer = operators.AdamW(params, lr=lr, weight_decay=0.01, state_bits=state_bits, copies=copies, decay_factors=decay)
@@ -87,7 +100,7 @@ def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows:
         loss = torch.nn.functional.cross_entropy((h @ w[2].t() + w[3]).float(), target)
         grads = list(torch.autograd.grad(loss, w + [table if dense else x]))
         table.requires_grad_(False)
-        clip = clip_factor(grads, max_norm)
+        clip = clip_factor(grads if dense else grads[:4] + [touched_rows(embedding, grads[4], ids, slot)], max_norm)
         optimizer.step(grads if dense else grads[:4], grad_scale=clip)
         if not dense:
             embedding.adamw(grads[4], ids, table, m, v, step=step, lr=lr, weight_decay=0.0, grad_scale=clip)

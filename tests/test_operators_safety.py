@@ -351,6 +351,21 @@ def test_a_step_whose_gradient_norm_is_not_finite_is_left_out(bad):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
+@gpu
+def test_the_table_has_the_same_norm_in_both_forms_of_the_example(n=700):
+    """A token that occurs several times counts with the sum of its gradient rows, whichever form the gradient has."""
+    from paper_2211_10280_b200 import next_token
+
+    V, d = 90, 6
+    e = _ops().Embedding(V, d, max_tokens=n, scale=2.0)
+    slot = next_token.rows_slot(V, d)
+    for k in (n, 3):                   # the second batch leaves rows of the first in the slot
+        ids, grad = _batch(k, V, k, d)
+        rows = next_token.touched_rows(e, grad, ids, slot)
+        assert rows.square().sum().item() == e.gradient(grad, ids).square().sum().item()
+        assert k < n or rows.square().sum().item() != (2 * grad).square().sum().item()
+
+
 # ---------------------------------------------------------------- captured steps
 @gpu
 def test_a_captured_step_is_the_same_step_at_every_replay():
