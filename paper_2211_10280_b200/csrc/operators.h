@@ -100,14 +100,6 @@ struct FastDiv {
     __device__ __forceinline__ uint32_t div(uint32_t x) const { return (__umulhi(x, mul) + x) >> shift; }
 };
 
-// The same for x < 2^16 and divisors below 2^16, made on the device: floor((x + 1/2) / divisor) in fp32 is exact there (the half keeps the
-// quotient at least 1 / (2 divisor) away from an integer; the two roundings move it by less than 2^-7 / divisor).
-struct FastDivSmall {
-    float inverse;
-    __device__ __forceinline__ explicit FastDivSmall(uint32_t divisor) : inverse(1.0f / (float)divisor) {}
-    __device__ __forceinline__ uint32_t div(uint32_t x) const { return (uint32_t)(((float)x + 0.5f) * inverse); }
-};
-
 // The constants of one AdamW step (see adamw.cuh for the formulas).
 struct AdamwConsts {
     float beta1, rest1;        // beta1, 1 - beta1
