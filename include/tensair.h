@@ -495,7 +495,8 @@ typedef struct tensair_tokens {
     const void* ids;          /* [n], of `type` */
     uint64_t n;               /* 0 .. 2^30 */
     uint64_t V;               /* rows of the table, 1 .. 2^30 */
-    int64_t padding_id;       /* an id that stands for "no token": its position reads as a zero row and has no gradient */
+    int64_t padding_id;       /* an id that stands for "no token": its position reads as a zero row and has no gradient;
+                                 INT64_MIN: no id does */
     uint32_t* error;          /* nullable: a sticky error word of the caller's; bit 0 is set when an id is neither in [0,V)
                                  nor padding_id (tensair_error_of_flags decodes it); such a position is treated as
                                  one without a token */

@@ -45,8 +45,8 @@ k_lookup(TokenIds t, uint32_t row0, const TT* __restrict__ table, uint64_t table
             const uint32_t r = vecs.div(w), col = (w - r * vecs.divisor) * E;
             const int64_t id = t.wide ? __ldg(reinterpret_cast<const long long*>(t.ids) + row0 + r)
                                       : __ldg(reinterpret_cast<const int32_t*>(t.ids) + row0 + r);
-            if (id != t.padding && (uint64_t)id < t.V) from[u] = table + (uint64_t)id * table_stride + col;
-            else if (id != t.padding && t.err) atomicOr(t.err, kErrBadToken);
+            if (t.is_token(id)) from[u] = table + (uint64_t)id * table_stride + col;
+            else t.report(id);
         }
     }
 #pragma unroll

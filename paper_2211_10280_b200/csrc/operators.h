@@ -13,13 +13,20 @@
 
 namespace tensair {
 
+constexpr int64_t kNoPadding = INT64_MIN;
 // How the token ids of a batch are read.
 struct TokenIds {
     const void* ids;
-    int64_t padding;      // an id equal to this stands for "no token"
+    int64_t padding;      // an id equal to this stands for "no token"; kNoPadding: none does
     uint32_t* err;        // nullable: receives kErrBadToken (checked build: and kErrBounds)
     uint32_t n, V;
     bool wide;            // 64-bit ids
+
+    __device__ __forceinline__ bool is_token(int64_t id) const { return (uint64_t)id < V && id != padding; }
+    // for an id that is no token
+    __device__ __forceinline__ void report(int64_t id) const {
+        if (err && (id != padding || padding == kNoPadding)) atomicOr(err, kErrBadToken);
+    }
 };
 
 // ---- element types: everything is computed in fp32 and rounded to nearest once, when it is stored

@@ -10,9 +10,8 @@ constexpr int kMaxDigitBits = 10;
 
 __device__ __forceinline__ uint32_t token_key(const TokenIds& t, uint32_t i) {
     const int64_t id = t.wide ? reinterpret_cast<const int64_t*>(t.ids)[i] : reinterpret_cast<const int32_t*>(t.ids)[i];
-    if (id == t.padding) return t.V;
-    if ((uint64_t)id < t.V) return (uint32_t)id;
-    if (t.err) atomicOr(t.err, kErrBadToken);
+    if (t.is_token(id)) return (uint32_t)id;
+    t.report(id);
     return t.V;
 }
 

@@ -552,6 +552,26 @@ def test_every_code_of_8_bit_moments_is_that_of_separately_rounded_operations(sp
         v = (opt.v[0].float().view(-1, 256) * opt.v_scale[0][:, None]).view(-1)
 
 
+# ---------------------------------------------------------------- ids
+@gpu
+def test_without_a_padding_id_every_id_outside_the_vocabulary_is_reported():
+    V, d, low = 10, 4, -(1 << 63)
+    table, grad = torch.ones(V, d, device="cuda"), torch.ones(3, d, device="cuda")
+    for padding, bad in ((None, (low, -1, V)), (low, (low,)), (low + 1, (low, -1)), (-1, (low, V)), (3, (-1, low))):
+        e = _ops().Embedding(V, d, max_tokens=3, padding_id=padding)
+        for x in bad:
+            ids = torch.tensor([1, x, 2], device="cuda")
+            for call in (lambda: e.lookup(table, ids), lambda: e.gradient(grad, ids)):
+                out = call()
+                with pytest.raises(B.TensairError):
+                    e.check()
+                assert out.sum().item() == 2 * d
+        if padding not in (None, low):
+            ids = torch.tensor([1, padding, 2], device="cuda")
+            assert e.lookup(table, ids).sum().item() == e.gradient(grad, ids).sum().item() == 2 * d
+            e.check()
+
+
 # ---------------------------------------------------------------- the checked build
 @gpu
 @pytest.mark.parametrize("n", [1, 200, 256, 257, 1024, 1025, 9000, 16_384, 16_385, 100_000, 131_073, 300_000])
