@@ -338,7 +338,7 @@ class AdamW:
         self._hyper = B.Adamw()
         self._at = C.byref(self._hyper)
         self._said, self._left_out = [None, None, None, None], []
-        self._numel = [p.numel() for p in params]
+        self._numel, self._shapes = [p.numel() for p in params], [p.shape for p in params]
         self._written = self._all_written(())
 
     def _all_written(self, left_out):
@@ -371,7 +371,8 @@ class AdamW:
               f"{name}: a contiguous tensor of {n} elements on {self.device}, of {', '.join(str(d) for d in dtypes)}")
 
     def step(self, grads=None, grad_scale=None):
-        """One step with `grads` (default: the parameters' .grad; a parameter whose gradient is None is left alone).
+        """One step with `grads` (default: the parameters' .grad; a parameter whose gradient is None is left alone), each of its
+        parameter's shape, or flat.
 
         grad_scale: a float32 on the device that multiplies every gradient; if it is not finite the parameters and moments
         stay as they are (the step still counts).
@@ -388,11 +389,13 @@ class AdamW:
             for i in left_out:
                 grads[i] = self.params[i]          # stands in for the checks
         index, a, said = self.index, self._np, self._said     # what the descriptors say is written again only where it changed
-        kinds = [g.dtype for g in grads]
-        if (list(map(_T.numel, grads)) != self._numel or (kinds != said[2] and not _FLOATS.keys() >= set(kinds))
+        kinds, shapes = [g.dtype for g in grads], [g.shape for g in grads]
+        if (shapes != self._shapes or (kinds != said[2] and not _FLOATS.keys() >= set(kinds))
                 or False in map(_T.is_contiguous, grads) or list(map(_T.get_device, grads)) != [index] * len(grads)):
-            for i, g in enumerate(grads):
+            for i, (g, p) in enumerate(zip(grads, self.params)):
                 self._fits(g, self._numel[i], _FLOATS, f"grads[{i}]")
+                _need(g.shape == p.shape or g.dim() == 1, f"grads[{i}]: shape {tuple(g.shape)} for a parameter of shape {tuple(p.shape)}")
+            self._shapes = shapes
         ptrs = list(map(_T.data_ptr, grads))
         if ptrs != said[0]:
             a["grad"] = said[0] = ptrs

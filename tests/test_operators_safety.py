@@ -157,6 +157,22 @@ def test_a_step_refuses_parameters_that_no_longer_fit(recorder, change):
     assert recorder.asked[0] == recorder.asked[1]
 
 
+def test_a_gradient_of_another_shape_is_refused(recorder):
+    p, q = torch.nn.Parameter(torch.ones(8, 6)), torch.ones(5)
+    opt = _ops().AdamW([p, q])
+    for bad in (torch.ones(6, 8), torch.ones(48, 1), torch.ones(2, 4, 6)):
+        for _ in range(2):
+            with pytest.raises(ValueError, match="shape"):
+                opt.step([bad, torch.ones(5)])
+    for good in (torch.ones(8, 6), torch.ones(48), torch.ones(8, 6), None):
+        opt.step([good, torch.ones(5)])
+    with pytest.raises(ValueError):
+        opt.step([torch.ones(47), torch.ones(5)])
+    p.data = torch.ones(6, 8)
+    opt.step([torch.ones(6, 8), torch.ones(5)])
+    assert len(recorder.asked) == 5
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_moments_and_copies_cannot_be_replaced_unseen(recorder, bits):
     p = torch.ones(300)
