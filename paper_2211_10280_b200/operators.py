@@ -383,15 +383,18 @@ class AdamW:
             grads = [p.grad for p in self.params]
         _need(len(grads) == len(self.params), "grads: one for each parameter, or None")
         # one list per property, each made in one go: a fifth of the time of a loop with its checks
-        left_out = [i for i, g in enumerate(grads) if g is None]
-        if left_out:
+        try:
+            kinds, left_out = [g.dtype for g in grads], []
+        except AttributeError:                     # there is a None
+            left_out = [i for i, g in enumerate(grads) if g is None]
             grads = list(grads)
             for i in left_out:
                 grads[i] = self.params[i]          # stands in for the checks
+            kinds = [g.dtype for g in grads]
+        shapes = [g.shape for g in grads]
         index, a, said = self.index, self._np, self._said     # what the descriptors say is written again only where it changed
-        kinds, shapes = [g.dtype for g in grads], [g.shape for g in grads]
         if (shapes != self._shapes or (kinds != said[2] and not _FLOATS.keys() >= set(kinds))
-                or False in map(_T.is_contiguous, grads) or list(map(_T.get_device, grads)) != [index] * len(grads)):
+                or False in map(_T.is_contiguous, grads) or set(map(_T.get_device, grads)) != {index}):
             for i, (g, p) in enumerate(zip(grads, self.params)):
                 self._fits(g, self._numel[i], _FLOATS, f"grads[{i}]")
                 _need(g.shape == p.shape or g.dim() == 1, f"grads[{i}]: shape {tuple(g.shape)} for a parameter of shape {tuple(p.shape)}")
