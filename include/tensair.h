@@ -485,6 +485,7 @@ TENSAIR_API int tensair_raise_error_flags(tensair_ctx* ctx, uint32_t flags);
  * refuses to be captured with 8-bit moments, whose rounding would repeat its random bits).  All pointers inside the argument blocks are device pointers that must stay valid until
  * the stream has passed the call; the argument blocks themselves are read during the call.  Arguments are checked
  * before anything is enqueued; tensair_last_error(NULL) says what the calling thread's last refused call was refused for.
+ * What a call writes may not overlap what it reads, but for the tensors that it updates in place.
  * Everything is computed in fp32 whatever the tensors' types are, and rounded to nearest once, when it is stored.
  * No sum depends on timing: the same inputs give the same bits.
  */

@@ -17,8 +17,8 @@
 // block's scale alone, so they stay where they are, as in 32 bits.
 //
 // With 8-bit moments an element moves 14 bytes (fp32, bf16 gradients) and takes some 60 instructions, 26 of them integer (Philox,
-// the roundings, addresses), so the kernel is bound by both: 128 M elements take 325 us, 5.5 TB/s (0.84 of the copy rate).
-// What made it so (547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate quotients in the
+// the roundings, addresses), so the kernel is bound by both: 128 M elements take 360 us a step in a run of steps, 5.0 TB/s (0.76 of the copy
+// rate), and 325 us where only a few follow one another.  What made it so (short runs; 547 us at first): packed fp32 arithmetic, roots by one Newton step two at a time, approximate quotients in the
 // update, Philox with its round keys in the arguments, one vote per block for the rare cases, 64 registers for four blocks per
 // multiprocessor (401 us), and the next turn's reads prefetched into the level-2 cache.  Copying them ahead through shared memory
 // instead made it slower (443 us).
@@ -296,48 +296,48 @@ template <int kCount>
 __device__ __forceinline__ void step8(const Batch<kCount>& b, const Entry& t, uint64_t block, uint32_t lane, float grad_scale,
                                       float (&p)[kLaneElems], Two (&g)[4], Two m_scale, Two v_scale, uint2& mc, uint2& vc) {
     Two m[4], v[4];
-                const uint64_t group = (t.block0 + block) * 32 + lane;
-                const Philox4 r = philox4x32_10(Philox4{(uint32_t)group, (uint32_t)(group >> 32), b.step_lo, kTagRounding | b.step_hi}, b.keys);
-                const uint32_t words[4] = {r.x, r.y, r.z, r.w};
-                uint32_t bits20[kLaneElems];
-    #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    bits20[2 * h] = words[h] << 4 & 0xFFFF0u;
-                    bits20[2 * h + 1] = words[h] >> 12 & 0xFFFF0u;
-                }
-    #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    // every product and sum rounded by itself, as a program of separate operations has them: what is
-                    // stored then does not depend on which of them a compiler contracts
-                    m[h] = decode8((uint16_t)((h < 2 ? mc.x : mc.y) >> (16 * (h & 1))), m_scale);
-                    v[h] = decode8((uint16_t)((h < 2 ? vc.x : vc.y) >> (16 * (h & 1))), v_scale);
-                    g[h] = g[h] * Two(grad_scale);
-                    m[h] = sum_of(m[h] * Two(b.c.beta1), g[h] * Two(b.c.rest1));
-                    v[h] = sum_of(v[h] * v[h] * Two(b.c.beta2), g[h] * g[h] * Two(b.c.rest2));
-                }
-                uint32_t m_low, m_top, v_low, v_top;
-                range8<false>(m, &m_low, &m_top);
-                range8<true>(v, &v_low, &v_top);
-                // from here on v is its square root
-                if (__all_sync(0xFFFFFFFFu, v_low >= 0x0F800000u && v_top < kInfBits)) {      // 2^-96
-    #pragma unroll
-                    for (int h = 0; h < 4; ++h) v[h] = roots(v[h]);
-                } else {
-    #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const float2 f = v[h].floats();
-                        v[h] = Two(__fsqrt_rn(f.x), __fsqrt_rn(f.y));
-                    }
-                }
-                range8<true>(v, &v_low, &v_top);
-    #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const float2 low = fma2(v[h], Two(b.c.inv_root2), Two(b.c.eps)).floats();
-                    const Two change = m[h] * Two(approximate_reciprocal(low.x), approximate_reciprocal(low.y));
-                    const float2 y = fma2(change, Two(-t.step_size), Two(p[2 * h], p[2 * h + 1]) * Two(t.keep)).floats();
-                    p[2 * h] = y.x;
-                    p[2 * h + 1] = y.y;
-                }
+    const uint64_t group = (t.block0 + block) * 32 + lane;
+    const Philox4 r = philox4x32_10(Philox4{(uint32_t)group, (uint32_t)(group >> 32), b.step_lo, kTagRounding | b.step_hi}, b.keys);
+    const uint32_t words[4] = {r.x, r.y, r.z, r.w};
+    uint32_t bits20[kLaneElems];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        bits20[2 * h] = words[h] << 4 & 0xFFFF0u;
+        bits20[2 * h + 1] = words[h] >> 12 & 0xFFFF0u;
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        // every product and sum rounded by itself, as a program of separate operations has them: what is
+        // stored then does not depend on which of them a compiler contracts
+        m[h] = decode8((uint16_t)((h < 2 ? mc.x : mc.y) >> (16 * (h & 1))), m_scale);
+        v[h] = decode8((uint16_t)((h < 2 ? vc.x : vc.y) >> (16 * (h & 1))), v_scale);
+        g[h] = g[h] * Two(grad_scale);
+        m[h] = sum_of(m[h] * Two(b.c.beta1), g[h] * Two(b.c.rest1));
+        v[h] = sum_of(v[h] * v[h] * Two(b.c.beta2), g[h] * g[h] * Two(b.c.rest2));
+    }
+    uint32_t m_low, m_top, v_low, v_top;
+    range8<false>(m, &m_low, &m_top);
+    range8<true>(v, &v_low, &v_top);
+    // from here on v is its square root
+    if (__all_sync(0xFFFFFFFFu, v_low >= 0x0F800000u && v_top < kInfBits)) {      // 2^-96
+#pragma unroll
+        for (int h = 0; h < 4; ++h) v[h] = roots(v[h]);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const float2 f = v[h].floats();
+            v[h] = Two(__fsqrt_rn(f.x), __fsqrt_rn(f.y));
+        }
+    }
+    range8<true>(v, &v_low, &v_top);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const float2 low = fma2(v[h], Two(b.c.inv_root2), Two(b.c.eps)).floats();
+        const Two change = m[h] * Two(approximate_reciprocal(low.x), approximate_reciprocal(low.y));
+        const float2 y = fma2(change, Two(-t.step_size), Two(p[2 * h], p[2 * h + 1]) * Two(t.keep)).floats();
+        p[2 * h] = y.x;
+        p[2 * h + 1] = y.y;
+    }
     mc = store8<false>(m, m_low, m_top, bits20, t.m_scale + block, lane);
     vc = store8<true>(v, v_low, v_top, bits20, t.v_scale + block, lane);
 }
@@ -478,7 +478,7 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
             for (uint32_t i = 0; i < count; ++i)
                 if (tensors[i].param_type == pt && tensors[i].grad_type == gt) total += tensors[i].n;
             if (!total) continue;
-// A block finds its tensor once per chunk.  With 32-bit moments short chunks are best (96 M elements: 395 us with 2,048,
+            // A block finds its tensor once per chunk.  With 32-bit moments short chunks are best (96 M elements: 395 us with 2,048,
             // 403 with 4,096, 410 with 8,192: the blocks that run together stay close together in memory); with 8-bit ones the search
             // is worth sharing (128 M: 442 us with 4,096, 401 with 16,384), as long as all multiprocessors have chunks.
             b.chunk = bits == 8 ? 16384 : 2048;
@@ -491,8 +491,10 @@ cudaError_t launch_all(cudaStream_t stream, const AdamwTensor* tensors, uint32_t
     return cudaSuccess;
 }
 
-// Tensors that a launch's arguments hold: every launch copies them all, so there are four sizes (1.6, 3, 6 and 30 KB;
-// a launch takes some 0.6 us per KB).
+// Tensors that a launch's arguments hold: the host copies them all with every launch, so there are four sizes (1.6, 3, 6 and 32 KB).  The
+// kernel's own time is the same with all of them (4.2 us for 13 to 336 tensors of 1,000 elements); the call takes the host 4.7 us with 16
+// tensors, 6.4 with 64, 9.4 with 65, 17 with 336.  Launches of 64 instead of the last size: 9.6 us with 65, 11.2 with 128 (11.6 in one
+// launch), 14.4 with 129 (11.3), 30 with 336, and 4.1 us more on the device for each.
 constexpr int kFew = 16, kSome = 32, kMore = 64, kMany = 336;
 
 }  // namespace

@@ -7,11 +7,11 @@
 //   up to 2^14 positions   one launch of one thread-block cluster.  The items stay in the cluster's shared memory; every pass
 //                          exchanges the digit totals through distributed shared memory and writes the items straight into
 //                          the shared memory of the block that owns their place.  Bound by the latency of its barriers:
-//                          2,048 tokens 8.5 us, 4,096 9 us, 16,384 12.3 us (V = 100,000).
+//                          2,048 tokens 8.8 us, 4,096 9.3 us, 16,384 12.5 us (V = 100,000).
 //   up to 2^17             two launches per pass, rank and scatter, and one that lists the tokens; items and totals go through
 //                          the level-2 cache, and every block adds up the totals it needs itself.  Each launch begins
-//                          while the one before it ends.  32,768 tokens 17.6 us, 65,536 22.5 us, 131,072 40 us (V = 1 M); in one
-//                          cluster, with 4 items per thread, 65,536 took 27 us; 16,384 take 14 us this way.
+//                          while the one before it runs.  32,768 tokens 17.7 us, 65,536 22.2 us, 131,072 31.8 us (V = 1 M); in one
+//                          cluster, with 4 items per thread, 65,536 took 27 us; 16,384 took 14 us this way.
 //   beyond                 the library's multi-launch radix sort (262,144 tokens 78 us), whose totals are scanned by a launch of their
 //                          own.
 #include <cooperative_groups.h>
@@ -249,7 +249,8 @@ k_list_tokens(uint32_t n, uint32_t V, uint32_t tiles, SortedTokens s, ClearShare
     }
 }
 
-// A few blocks per multiprocessor clear all: they start at once, so the launch that follows can run beside them.
+// One block per multiprocessor: all start at once, so the launch that follows can run beside them.  102 MB take 18.5 us, 5.5 TB/s, alone
+// (a memset 16.6), 26 with the sort of 16,384 tokens beside them.
 constexpr int kClearThreads = 512;
 __global__ void __launch_bounds__(kClearThreads) k_clear(ClearRows c) {
     let_next_launch_begin();

@@ -2,7 +2,7 @@
 
     Embedding   rows of a table looked up for a batch of tokens, times a scale; the gradient of the table by sorted
                 tokens (the whole table, added to it, or the touched rows alone); the AdamW step of the touched rows.
-    AdamW       one AdamW step over many tensors at once, with moments in 32 or in 8 bits.
+    AdamW       an AdamW step over many tensors at once, with moments in 32 or in 8 bits.
 
 Every call enqueues its kernels on the current stream of the tensors' device and returns without waiting; tensors
 that another stream is still writing are ordered by the caller, as for torch's own operators.  There is no fallback:
@@ -274,7 +274,8 @@ _DESCRIPTOR = np.dtype({"names": [f[0] for f in B.AdamwTensor._fields_],
 
 
 class AdamW:
-    """AdamW over a list of contiguous parameters, all of them in one launch:
+    """AdamW over a list of contiguous parameters, in one launch for each combination of parameter and gradient types (and for every
+    336 parameters):
 
         m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
         p <- p (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
