@@ -340,7 +340,13 @@ class AdamW:
         self._at = C.byref(self._hyper)
         self._said, self._left_out = [None, None, None, None], []
         self._numel, self._shapes = [p.numel() for p in params], [p.shape for p in params]
-        self._written = self._all_written(())
+        self._describe_params([p.data_ptr() for p in params], [p.dtype for p in params])      # as they were checked above
+
+    def _describe_params(self, places, kinds):
+        self._np["param_type"] = [_FLOATS[k] for k in kinds]
+        self._np["param"] = places
+        self._said[1], self._said[3] = places, kinds
+        self._written = self._all_written(self._left_out)
 
     def _all_written(self, left_out):
         """What a step writes that may be part of a graph: parameters and copies, but for those that are left out."""
@@ -408,10 +414,7 @@ class AdamW:
         if ptrs != said[1] or param_kinds != said[3]:
             for i, p in enumerate(self.params):
                 self._fits(p, self._numel[i], _FLOATS, f"params[{i}]")
-            a["param_type"] = [_FLOATS[k] for k in param_kinds]
-            a["param"] = ptrs
-            said[1], said[3] = ptrs, param_kinds
-            self._written = self._all_written(self._left_out)
+            self._describe_params(ptrs, param_kinds)
         if kinds != said[2]:
             said[2] = kinds
             a["grad_type"] = [_FLOATS[k] for k in kinds]
