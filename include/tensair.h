@@ -587,6 +587,125 @@ typedef struct tensair_adamw_tensor {
 TENSAIR_API int tensair_adamw_step(const tensair_adamw_tensor* tensors, uint64_t count, uint32_t state_bits,
                                    const tensair_adamw* adamw, void* stream);
 
+/*
+ * ---- operators of a recurrent language model ----
+ *
+ * What a model that goes on along the stream needs between the embedding and the next token: layer norm, dropout, a gated linear
+ * recurrence with a state of fixed size per stream, and the draw of the next token.  As above: no context, the caller's tensors and
+ * stream, arithmetic in fp32 (the draw: 64 bits), one rounding when a value is stored, no result that depends on timing.
+ */
+
+/* Layer norm of n rows x of d elements: out = (x - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps). */
+typedef struct tensair_norm {
+    const void* weight;       /* [d], of param_type */
+    const void* bias;         /* [d], of param_type; nullable */
+    float* mean;              /* [n]: written by the forward call (nullable there, with rstd), read by the gradient */
+    float* rstd;              /* [n] */
+    uint64_t n;               /* 0 .. 2^30 */
+    uint32_t param_type;
+    float eps;                /* finite, not negative */
+} tensair_norm;
+
+/* x and out: n rows; out of x's type, or of 16 bits where x is TENSAIR_FLOAT32.  bias and (mean, rstd) may be NULL. */
+TENSAIR_API int tensair_layer_norm(const tensair_norm* norm, const tensair_rows* x, const tensair_rows* out, void* stream);
+
+/*
+ * Its gradient.  With c = (x - mean) rstd and g = grad weight:
+ *     dx = rstd (g - mean(g) - c mean(g c)),    dweight = sum over rows of grad c,    dbias = sum over rows of grad
+ * grad is of the type of what the forward call wrote, dx of x's type, dweight and dbias ([d], param_type) nullable; norm->bias is not
+ * looked at.  The sums over rows are taken in an order that n, d and the types fix.  dx may be grad (of the same type).
+ * workspace: needed where dweight or dbias is; tensair_norm_workspace_bytes(n, d) bytes, 256-byte aligned; it
+ * holds nothing between calls, and calls that share one must be ordered by their streams.
+ */
+TENSAIR_API int tensair_norm_workspace_bytes(uint64_t n, uint32_t d, uint64_t* bytes);
+TENSAIR_API int tensair_layer_norm_gradient(const tensair_norm* norm, const tensair_rows* grad, const tensair_rows* x,
+                                            const tensair_rows* dx, void* dweight, void* dbias, void* workspace,
+                                            uint64_t workspace_bytes, void* stream);
+
+/*
+ * Dropout of n contiguous elements, with a mask that is never stored:
+ *     out[e] = (word(e) >= floor(p 2^32) ? x[e] / (1 - p) : 0) + residual[e]
+ * word(e) is word e % 4 of Philox4x32-10 of the counter (e / 4 low, high, call low, 6 << 24 | call high) and the key `seed`; call counts modulo 2^56.
+ * The gradient with respect to x is the same call on the incoming gradient, without the residual.  out may be x, or residual.
+ */
+typedef struct tensair_dropout_call {
+    const void* x;
+    const void* residual;     /* nullable = 0 */
+    void* out;
+    uint64_t n;               /* 0 .. 2^40 - 1 */
+    double p;                 /* 0 .. 1; 1: nothing is kept */
+    uint64_t seed;
+    uint64_t call;            /* below 2^56: a number for every mask that is to differ */
+    const uint64_t* call_at;  /* nullable: device; its value when the stream reaches the call is added to `call`, so that the replays of
+                                 a graph draw masks of their own.  NULL: EINVAL when the stream is being captured */
+    uint32_t type;            /* of x, residual and out */
+    uint32_t reserved;
+} tensair_dropout_call;
+TENSAIR_API int tensair_dropout(const tensair_dropout_call* dropout, void* stream);
+
+/*
+ * A gated linear recurrence over B sequences of T steps of d channels, with f = sigmoid(gate):
+ *     h_t = f_t h_{t-1} + (1 - f_t) value_t        out_t = h_t
+ * A tensair_steps holds rows of d elements: `step` elements between the steps of a sequence, `batch` between sequences.
+ * lengths: steps of each sequence, clamped to 0 .. T; the steps from there on are padding: what is there is not
+ * used, out is zero there and the state stays.  state: what h begins with (NULL = 0); last: h after the last step.
+ * marks: h before every eighth step, float[B][ceil(T / 8)][d], for the gradient.  state and last may be one (not in the gradient).
+ * A value, gate or state that is not finite makes its channel NaN or infinite from that step of its sequence on.
+ */
+typedef struct tensair_steps {
+    void* data;
+    uint64_t batch, step;     /* step: 0 or at least d where it is written; both below 2^40 */
+} tensair_steps;
+typedef struct tensair_sequences {
+    tensair_steps gate, value;
+    const int32_t* lengths;   /* [B], device; nullable = T */
+    uint64_t B, T;            /* 0 .. 2^30 each; B * ceil(d / 2) at most 2^30 */
+    uint32_t d;               /* 1 .. 2^20 */
+    uint32_t type;            /* of gate, value and all that is of their shape */
+} tensair_sequences;
+TENSAIR_API int tensair_recurrence(const tensair_sequences* seq, const float* state, const tensair_steps* out, float* last,
+                                   float* marks, void* stream);
+
+/*
+ * Its gradient.  grad: with respect to out; grad_last: with respect to `last` (nullable = 0); marks: what the forward call left.
+ * With e = grad_last behind the last step, backwards:
+ *     D_t = grad_t + e_{t+1}    e_t = f_t D_t    dvalue_t = (1 - f_t) D_t    dgate_t = f_t (1 - f_t) (h_{t-1} - value_t) D_t
+ * dstate (nullable) = e of the first step.  Padding has gradients of zero, and grad is not used there.
+ */
+TENSAIR_API int tensair_recurrence_gradient(const tensair_sequences* seq, const tensair_steps* grad, const float* grad_last,
+                                            const float* marks, const tensair_steps* dgate, const tensair_steps* dvalue,
+                                            float* dstate, void* stream);
+
+/* One step (seq->T == 1, no lengths): state [B][d] is updated in place. */
+TENSAIR_API int tensair_recurrence_step(const tensair_sequences* seq, float* state, const tensair_steps* out, void* stream);
+
+/*
+ * The draw of the next token from n rows of V logits, with one given random number u for each row.
+ * A row's tokens are ordered by (logit descending, id ascending); NaN counts as minus infinity.  A weight is exp((logit - largest) /
+ * temperature) in 64 bits, rounded to a multiple of 2^-b, b = min(46, 62 - bits of V - 1), so that sums are exact.  Kept are
+ *     the first top_k tokens (top_k <= 0 or >= V: all);
+ *     of those the tokens with less than top_p * (their weight) before them, one at least (top_p >= 1: all);
+ *     of those the ones with logit - largest >= temperature * ln(min_p) (min_p <= 0: all).
+ * token = the lowest id whose running kept weight, ids ascending, exceeds floor(u * kept weight), u clamped to [0, 1); logprob =
+ * ln(its share of the kept weight).  temperature <= 0 (or NaN): the lowest id of the largest logit, logprob 0.  A row
+ * without a logit above minus infinity has token -1 and logprob minus infinity.  Where the largest logit is plus infinity only such tokens have weight.
+ * A setting is an array of n on the device or, where that is NULL, one value for all rows.
+ */
+typedef struct tensair_draw {
+    const float* uniform;     /* [n] */
+    int64_t* token;           /* [n] */
+    float* logprob;           /* [n], nullable */
+    const float* temperatures;
+    const float* top_ps;
+    const float* min_ps;
+    const int32_t* top_ks;
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    uint64_t n;               /* 0 .. 2^24 */
+} tensair_draw;
+/* logits: n rows of d = V elements, V <= 2^20. */
+TENSAIR_API int tensair_sample(const tensair_draw* draw, const tensair_rows* logits, void* stream);
+
 /* ---- host-only pieces, usable without a GPU ---- */
 
 /* Walker/Vose alias table over weights count^0.75 (counts NULL = all 1): host in, host out. */

@@ -84,6 +84,31 @@ class AdamwTensor(C.Structure):
                 ("copy_type", C.c_uint32), ("skip", C.c_uint32)]
 
 
+class Norm(C.Structure):
+    _fields_ = [("weight", C.c_void_p), ("bias", C.c_void_p), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("n", C.c_uint64),
+                ("param_type", C.c_uint32), ("eps", C.c_float)]
+
+
+class DropoutCall(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("p", C.c_double),
+                ("seed", C.c_uint64), ("call", C.c_uint64), ("call_at", C.c_void_p), ("type", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class Steps(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_uint64), ("step", C.c_uint64)]
+
+
+class Sequences(C.Structure):
+    _fields_ = [("gate", Steps), ("value", Steps), ("lengths", C.c_void_p), ("B", C.c_uint64), ("T", C.c_uint64),
+                ("d", C.c_uint32), ("type", C.c_uint32)]
+
+
+class Draw(C.Structure):
+    _fields_ = [("uniform", C.c_void_p), ("token", C.c_void_p), ("logprob", C.c_void_p), ("temperatures", C.c_void_p),
+                ("top_ps", C.c_void_p), ("min_ps", C.c_void_p), ("top_ks", C.c_void_p), ("temperature", C.c_float),
+                ("top_p", C.c_float), ("min_p", C.c_float), ("top_k", C.c_int32), ("n", C.c_uint64)]
+
+
 class TensairError(RuntimeError):
     def __init__(self, code: int, what: str, detail: str = ""):
         self.code = code
@@ -153,10 +178,20 @@ SYMBOLS = {
     "tensair_embedding_gradient_rows": (_int, [_P(Tokens), _P(Rows), C.c_float, _vp, _P(Rows), _vp, _vp, _u64, _vp]),
     "tensair_embedding_adamw": (_int, [_P(Tokens), _P(Rows), C.c_float, _P(Rows), _P(Rows), _P(Rows), _P(Adamw), _vp, _u64, _vp]),
     "tensair_adamw_step": (_int, [_P(AdamwTensor), _u64, _u32, _P(Adamw), _vp]),
+    "tensair_layer_norm": (_int, [_P(Norm), _P(Rows), _P(Rows), _vp]),
+    "tensair_norm_workspace_bytes": (_int, [_u64, _u32, _P(_u64)]),
+    "tensair_layer_norm_gradient": (_int, [_P(Norm), _P(Rows), _P(Rows), _P(Rows), _vp, _vp, _vp, _u64, _vp]),
+    "tensair_dropout": (_int, [_P(DropoutCall), _vp]),
+    "tensair_recurrence": (_int, [_P(Sequences), _vp, _P(Steps), _vp, _vp, _vp]),
+    "tensair_recurrence_gradient": (_int, [_P(Sequences), _P(Steps), _vp, _vp, _P(Steps), _P(Steps), _vp, _vp]),
+    "tensair_recurrence_step": (_int, [_P(Sequences), _vp, _P(Steps), _vp]),
+    "tensair_sample": (_int, [_P(Draw), _P(Rows), _vp]),
 }
 
 _OPERATORS = {"tensair_embedding_lookup", "tensair_embedding_workspace_bytes", "tensair_embedding_gradient",
-              "tensair_embedding_gradient_rows", "tensair_embedding_adamw", "tensair_adamw_step"}
+              "tensair_embedding_gradient_rows", "tensair_embedding_adamw", "tensair_adamw_step", "tensair_layer_norm",
+              "tensair_norm_workspace_bytes", "tensair_layer_norm_gradient", "tensair_dropout", "tensair_recurrence",
+              "tensair_recurrence_gradient", "tensair_recurrence_step", "tensair_sample"}
 _lib = None
 
 

@@ -23,7 +23,8 @@ LIB_CHECKED = HERE / "libtensair_checked.so"
 OBJ = HERE / "_build"
 
 SOURCES = ["tensair.cu", "schedule.cu", "sampler.cu", "radix_sort.cu", "forward.cu", "message.cu", "apply.cu",
-           "static_scratch.cu", "merge.cu", "topk.cu", "alias_build.cu", "operators.cu", "token_sort.cu", "embedding.cu", "embedding_short.cu", "adamw.cu"]
+           "static_scratch.cu", "merge.cu", "topk.cu", "alias_build.cu", "operators.cu", "token_sort.cu", "embedding.cu", "embedding_short.cu", "adamw.cu",
+           "layers.cu", "layer_norm.cu", "dropout.cu", "recurrence.cu", "sample.cu"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

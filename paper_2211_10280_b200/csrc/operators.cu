@@ -8,29 +8,18 @@
 #include <vector>
 
 #include "context.h"
+#include "operator_checks.h"
 #include "operators.h"
 
 using namespace tensair;
 
 namespace {
 
-constexpr uint64_t kMaxTokens = 1ull << 30, kMaxVocabulary = 1ull << 30, kMaxWidth = 1ull << 20, kMaxStride = (1ull << 31) - 1;
+constexpr uint64_t kMaxTokens = 1ull << 30, kMaxVocabulary = 1ull << 30;
 
 // What the last refused or failed operator call of this thread said (these calls have no context to keep it in).
 // A fixed array: setting it can neither allocate nor throw.
 thread_local char last_refusal[160] = "";
-
-int refuse(int code, const char* why) {
-    std::snprintf(last_refusal, sizeof(last_refusal), "%s", why);
-    return code;
-}
-int launched(cudaError_t e) {
-    if (e == cudaSuccess) return TENSAIR_OK;
-    return refuse(TENSAIR_ECUDA, cudaGetErrorString(e));
-}
-#define TENSAIR_REQUIRE(cond, why) do { if (!(cond)) return refuse(TENSAIR_EINVAL, why); } while (0)
-
-bool is_float_type(uint32_t type) { return type <= TENSAIR_FLOAT16; }
 
 int check_tokens(const tensair_tokens* t) {
     TENSAIR_REQUIRE(t, "tokens: NULL");
@@ -43,6 +32,19 @@ int check_tokens(const tensair_tokens* t) {
     return TENSAIR_OK;
 }
 
+}  // namespace
+
+namespace tensair {
+
+int refuse(int code, const char* why) {
+    std::snprintf(last_refusal, sizeof(last_refusal), "%s", why);
+    return code;
+}
+int launched(cudaError_t e) {
+    if (e == cudaSuccess) return TENSAIR_OK;
+    return refuse(TENSAIR_ECUDA, cudaGetErrorString(e));
+}
+
 int check_rows(const tensair_rows* r, uint32_t d, bool empty, const char* null, const char* bad) {
     TENSAIR_REQUIRE(r && (empty || r->data), null);
     TENSAIR_REQUIRE(is_float_type(r->type) && r->d == d && (empty || (r->stride >= d && r->stride <= kMaxStride)) &&
@@ -50,10 +52,25 @@ int check_rows(const tensair_rows* r, uint32_t d, bool empty, const char* null, 
     return TENSAIR_OK;
 }
 
+int multiprocessors() {
+    static std::atomic<int> known[kMaxDevices];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) return 0;
+    int sms = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (!sms) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+        if (device < kMaxDevices) known[device].store(sms, std::memory_order_relaxed);
+    }
+    return sms;
+}
+
+}  // namespace tensair
+
+namespace {
+
 TokenIds tokens_of(const tensair_tokens& t) {
     return TokenIds{t.ids, t.padding_id, t.error, (uint32_t)t.n, (uint32_t)t.V, t.type == TENSAIR_INT64};
 }
-RowsView view_of(const tensair_rows& r) { return RowsView{r.data, (uint32_t)r.stride, r.type}; }
 
 // The workspace of the gradient calls for a batch of n tokens.
 struct Layout {
@@ -84,18 +101,6 @@ Layout layout_of(uint32_t n, uint32_t V, uint32_t d) {
     l.tile_counts = take(s.tile_counts);
     l.total = off;
     return l;
-}
-
-int multiprocessors() {
-    static std::atomic<int> known[kMaxDevices];
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess) return 0;
-    int sms = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
-    if (!sms) {
-        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
-        if (device < kMaxDevices) known[device].store(sms, std::memory_order_relaxed);
-    }
-    return sms;
 }
 
 // The part all gradient calls share: checks, workspace, sort, sums.

@@ -7,6 +7,7 @@
 //   init       counter = (e/4 low, e/4 high, 0, 3<<24) for table element e = row*d + col; word e%4
 //   rounding   counter = (group of 8 elements low, high, step low, 5<<24 | step high); element e of the group takes the
 //              low (e even) or high (e odd) half of word e/2
+//   dropout    counter = (group of 4 elements low, high, call low, 6<<24 | call high); element e of the group takes word e
 #pragma once
 #include <stdint.h>
 
@@ -22,6 +23,7 @@ constexpr uint32_t kTagDelay = 2u << 24;
 constexpr uint32_t kTagInit = 3u << 24;
 constexpr uint32_t kTagRoute = 4u << 24;
 constexpr uint32_t kTagRounding = 5u << 24;
+constexpr uint32_t kTagDropout = 6u << 24;
 
 struct Philox4 {
     uint32_t x, y, z, w;
