@@ -687,7 +687,7 @@ TENSAIR_API int tensair_recurrence_step(const tensair_sequences* seq, float* sta
  *     of those the tokens with less than top_p * (their weight) before them, one at least (top_p >= 1: all);
  *     of those the ones with logit - largest >= temperature * ln(min_p) (min_p <= 0: all).
  * token = the lowest id whose running kept weight, ids ascending, exceeds floor(u * kept weight), u clamped to [0, 1); logprob =
- * ln(its share of the kept weight).  temperature <= 0 (or NaN): the lowest id of the largest logit, logprob 0.  A row
+ * ln(its share of the kept weight).  A temperature above 1e30 counts as 1e30.  temperature <= 0 (or NaN): the lowest id of the largest logit, logprob 0.  A row
  * without a logit above minus infinity has token -1 and logprob minus infinity.  Where the largest logit is plus infinity only such tokens have weight.
  * A setting is an array of n on the device or, where that is NULL, one value for all rows.
  */

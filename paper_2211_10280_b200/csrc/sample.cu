@@ -28,58 +28,107 @@ constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMostCluster = 16;
 constexpr uint32_t kBuckets = 1024;          // two to a thread
 constexpr float kPerLogit = 48.0f;           // buckets of the first turn
-constexpr uint32_t kNothing = 0x007FFFFFu;   // the key of minus infinity
 typedef unsigned long long mass_t;
 
-// Keys order as logits do; NaN counts as minus infinity, minus zero as zero.
-__device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x + 0.0f);
-    const uint32_t k = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return x != x ? kNothing : k;
-}
-__device__ __forceinline__ float logit_of(uint32_t key) {
-    return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
-}
-
-// Weights relative to that of the largest logit.
-struct Weights {
-    double largest, per_logit;       // log2(e) / temperature
-    const double* roots;             // 2^(j/16), j < 16
-    double magic;                    // 2^(52 - bits)
-    uint32_t largest_key;
-    // exp by table and polynomial (after Tang, ACM TOMS 15, 1989): 2^z = 2^(n/16) 2^r with |r| <= 1/32, the
-    // latter by its series up to r^6 (what is left out is below 5e-16 of it)
-    __device__ __forceinline__ mass_t of(uint32_t key) const {
-        if (key == largest_key) return (mass_t)(__double_as_longlong(1.0 + magic) - __double_as_longlong(magic));
-        const double z = ((double)logit_of(key) - largest) * per_logit;
-        if (!(z > -64.0)) return 0;      // rounds to nothing: bits is at most 46
-        const double shifted = z * 16.0 + 0x1.8p52;
-        const int n = (int)__double_as_longlong(shifted);
-        const double r = fma(shifted - 0x1.8p52, -0.0625, z) * 0.69314718055994530942;
-        double y = 1.0 / 720.0;
-        y = fma(y, r, 1.0 / 120.0);
-        y = fma(y, r, 1.0 / 24.0);
-        y = fma(y, r, 1.0 / 6.0);
-        y = fma(y, r, 0.5);
-        y = fma(y, r, 1.0);
-        y = fma(y, r, 1.0) * roots[n & 15];
-        y = __longlong_as_double(__double_as_longlong(y) + ((long long)(n >> 4) << 52));
-        return (mass_t)(__double_as_longlong(y + magic) - __double_as_longlong(magic));
+// Keys order as logits do, 16-bit logits in 16 bits; NaN counts as minus infinity, minus zero as zero.
+template <typename T>
+struct Keys {
+    static constexpr int kBits = sizeof(T) * 8;
+    static constexpr uint32_t kSign = 1u << (kBits - 1), kAll = kSign | (kSign - 1);
+    static __device__ __forceinline__ uint32_t bits_of(T x) {
+        if constexpr (sizeof(T) == 4) return __float_as_uint(x);
+        else return *reinterpret_cast<const unsigned short*>(&x);
     }
+    static __device__ __forceinline__ uint32_t of(T x) {
+        const uint32_t b = bits_of(x);
+        const uint32_t k = b & kSign ? (b == kSign ? kSign : ~b & kAll) : b | kSign;
+        return to_float(x) == to_float(x) ? k : nothing();
+    }
+    static __device__ __forceinline__ float logit(uint32_t key) {
+        const uint32_t b = key & kSign ? key & ~kSign : ~key & kAll;
+        if constexpr (sizeof(T) == 4) return __uint_as_float(b);
+        else {
+            const unsigned short h = (unsigned short)b;
+            return to_float(*reinterpret_cast<const T*>(&h));
+        }
+    }
+    // of minus infinity, the lowest key
+    static __device__ __forceinline__ uint32_t nothing() { return ~bits_of(from_float<T>(-INFINITY)) & kAll; }
 };
 
-// The tokens kept: keys above `key`, and the first `ties` ids of those that have it.
+// (ln 2 / 32)^k / k!: in constant memory, from where the multiply-adds take them as operands (as literals they cost two moves each, for
+// every logit: 75 instructions a logit instead of 45).
+__constant__ double kSeries[6] = {1.0, 0.02166084939249829, 0.00023459619820224677, 1.6938509724371819e-06,
+                                    9.172562701824643e-09, 3.9737099845494154e-11};
+constexpr double kLog2e = 1.44269504088896340736;
+
+// Weights relative to that of the largest logit.  Logits up to `least` have none.
+struct Weights {
+    double largest, step;            // 32 log2(e) / temperature
+    const double* roots;             // 2^(j/32), j < 32
+    double magic;                    // 2^(52 - bits)
+    float top, least;
+    bool alone;                      // only the largest logit has weight: it is infinite, or the next smaller number is too far below
+    uint32_t bits;
+
+    __device__ __forceinline__ double gap(float x) const { return x == top ? 0.0 : (double)x - largest; }
+    __device__ void set(float largest_logit, float temperature, uint32_t weight_bits, const double* table) {
+        top = largest_logit;
+        largest = (double)top;
+        step = 32.0 * kLog2e / (double)temperature;
+        roots = table;
+        bits = weight_bits;
+        magic = __longlong_as_double((long long)(1023 + 52 - (int)bits) << 52);
+        const double none = -32.0 * (bits + 2);
+        least = (float)(largest - (double)temperature * ((bits + 2) / kLog2e));
+        if (!(least < top)) least = top;
+        // the next number further down, a few times at most: the first one below has rounded to here
+        while (gap(least) * step > none && least != -INFINITY) least = __uint_as_float(least > 0.0f ? __float_as_uint(least) - 1 : least < 0.0f ? __float_as_uint(least) + 1 : 0x80000001u);
+        alone = !(gap(least) * step > -32000.0);
+    }
+    // As raw bits: the sum of n of them less n times none() is the sum of the weights, as whole numbers.
+    // exp by table and polynomial (after Tang, ACM TOMS 15, 1989): 2^(s/32) = 2^(n/32) 2^((s-n)/32) with |s - n| <= 1/2, the
+    // latter by its series up to the fifth power (what is left out is below 2.3e-15 of it).
+    template <bool kAlone>
+    __device__ __forceinline__ mass_t raw(float x) const {
+        if (kAlone) return (mass_t)__double_as_longlong((x == top ? 1.0 : 0.0) + magic);
+        const double g = (double)fmaxf(x, least) - largest;
+        const double shifted = fma(g, step, 0x1.8p52);
+        const int n = (int)__double_as_longlong(shifted);
+        const double r = fma(g, step, 0x1.8p52 - shifted);
+        double y = kSeries[5];
+        y = fma(y, r, kSeries[4]);
+        y = fma(y, r, kSeries[3]);
+        y = fma(y, r, kSeries[2]);
+        y = fma(y, r, kSeries[1]);
+        y = fma(y, r, 1.0) * roots[n & 31];
+        y = __hiloint2double(__double2hiint(y) + ((n >> 5) << 20), __double2loint(y));
+        return (mass_t)__double_as_longlong(y + magic);
+    }
+    __device__ __forceinline__ mass_t none() const { return (mass_t)__double_as_longlong(magic); }
+    __device__ __forceinline__ mass_t of(float x) const { return (alone ? raw<true>(x) : raw<false>(x)) - none(); }
+};
+
+// The tokens kept: keys above `key`, and the first `ties` ids of those that have it (kAllTies: all).
+constexpr uint32_t kAllTies = 0xFFFFFFFFu;
 struct Border {
     uint32_t key, ties;
     __device__ __forceinline__ bool operator<(const Border& o) const { return key > o.key || (key == o.key && ties < o.ties); }   // keeps less
 };
 
+constexpr uint32_t kList = 4096;             // tokens that are taken out of the row, at most
 struct Shared {
-    uint32_t count[2][kBuckets], low[2][kBuckets], high[2][kBuckets];    // of two turns; a mass is high 2^32 + low
-    double roots[16];
+    // logits (of any type) and ids of tokens that are taken out
+    alignas(16) unsigned char listed[kList * 4];
+    alignas(16) uint32_t ids[kList];
+    // of two turns; a mass is high 2^32 + low.  Read two at a time.
+    alignas(16) uint32_t count[2][kBuckets];
+    alignas(16) uint32_t low[2][kBuckets];
+    alignas(16) uint32_t high[2][kBuckets];
+    double roots[32];
     // what each block of the cluster tells the others
-    uint32_t largest[kMostCluster], first[kMostCluster], ties[kMostCluster];
     mass_t mass[kMostCluster];
+    uint32_t largest[kMostCluster], first[kMostCluster], ties[kMostCluster], tokens[kMostCluster];
     mass_t warp_mass[kWarps];
     uint32_t warp_count[kWarps];
     // the bucket that holds the border
@@ -87,6 +136,8 @@ struct Shared {
     uint32_t bucket, count_before, count_in;
     uint32_t edge[2];
 };
+constexpr uint32_t kShort = kList;           // rows whose border is looked for among all their tokens
+constexpr uint32_t kSharedBytes = (sizeof(Shared) + 15) / 16 * 16;
 
 // A row's slice, cut into kWarps runs of `steps` accesses of a warp.
 template <typename T>
@@ -99,26 +150,22 @@ struct Slice {
     __device__ __forceinline__ uint32_t place(uint32_t step) const {
         return ((threadIdx.x / 32 * steps + step) * 32 + (threadIdx.x & 31)) * E;
     }
-    // E keys from `at` on; behind the slice: minus infinity
-    __device__ __forceinline__ void keys(uint32_t at, uint32_t (&key)[E]) const {
-        if (whole && at + E <= length) {
-            const Pack<T, E> x = load_pack<T, E>(logits + at);
+    // E logits from `at` on; behind the slice: minus infinity
+    __device__ __forceinline__ Pack<T, E> load(uint32_t at) const {
+        if (whole && at + E <= length) return load_pack<T, E>(logits + at);
+        Pack<T, E> x;
 #pragma unroll
-            for (int e = 0; e < E; ++e) key[e] = key_of(to_float(x.v[e]));
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) key[e] = at + e < length ? key_of(to_float(logits[at + e])) : kNothing;
-        }
+        for (int e = 0; e < E; ++e) x.v[e] = at + e < length ? logits[at + e] : from_float<T>(-INFINITY);
+        return x;
     }
     template <typename F>
     __device__ __forceinline__ void each(F&& f) const {
         for (uint32_t s = 0; s < steps; ++s) {
             const uint32_t at = place(s);
             if (at - (threadIdx.x & 31) * E >= length) break;
-            uint32_t key[E];
-            keys(at, key);
+            const Pack<T, E> x = load(at);
 #pragma unroll
-            for (int e = 0; e < E; ++e) f(key[e]);
+            for (int e = 0; e < E; ++e) f(x.v[e]);
         }
     }
 };
@@ -136,70 +183,66 @@ struct Team {                  // the cluster
         if (size > 1) cg::this_cluster().sync();
         else __syncthreads();
     }
+    // No block writes into another's memory before that one has started: it says so first thing, and asks before it writes.
+    __device__ __forceinline__ void started() const {
+        if (size > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    }
+    __device__ __forceinline__ void all_started() const {
+        if (size > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
     template <typename T>
     __device__ __forceinline__ T* of(T* p, uint32_t r) const { return size > 1 ? cg::this_cluster().map_shared_rank(p, r) : p; }
 };
 
 // The bucket, of equal width in logits below the largest.
-__device__ __forceinline__ uint32_t linear_bucket(uint32_t key, uint32_t largest_key, float largest) {
-    if (key == largest_key) return 0;
-    const float gap = (largest - logit_of(key)) * kPerLogit;
-    return gap < (float)(kBuckets - 1) ? (uint32_t)gap : kBuckets - 1;
+__device__ __forceinline__ uint32_t linear_bucket(float x, float largest) {
+    const float gap = fminf((largest - x) * kPerLogit, (float)(kBuckets - 1));      // NaN: the last one
+    return x == largest ? 0 : (uint32_t)gap;
 }
 
-// The largest key in [kNothing, largest_key] whose linear bucket is at least b (0: there is none), by one warp.
-__device__ __forceinline__ uint32_t key_at(uint32_t b, uint32_t largest_key, float largest) {
-    uint32_t lo = kNothing, hi = largest_key;      // buckets fall as keys rise
+// The largest key up to `top` whose linear bucket is at least b (there is one for any b < kBuckets), by one warp.
+template <typename T>
+__device__ __forceinline__ uint32_t key_at(uint32_t b, uint32_t top, float largest) {
+    uint32_t lo = Keys<T>::nothing(), hi = top;      // buckets fall as keys rise
     const uint32_t lane = threadIdx.x & 31;
-    if (linear_bucket(lo, largest_key, largest) < b) return 0;
     while (lo < hi) {      // 32 probes between lo, which has it, and hi
         const uint32_t step = (hi - lo + 31) / 32, probe = lo + (lane + 1) * step;
-        const bool has = probe <= hi && probe >= lo && linear_bucket(probe, largest_key, largest) >= b;
+        const bool has = probe <= hi && linear_bucket(Keys<T>::logit(probe), largest) >= b;
         const uint32_t n = __popc(__ballot_sync(0xFFFFFFFFu, has));
-        const uint32_t next = lo + n * step;
-        const uint32_t end = next + step - 1;      // the next probe does not have it, or lies behind hi
-        lo = next;
+        lo += n * step;
+        const uint32_t end = lo + step - 1;      // the next probe does not have it, or lies behind hi
         if (end < hi) hi = end;
     }
     return lo;
 }
 
-// The border by rank (k tokens are kept) or by mass (tokens are kept as long as the mass before them is below share * the whole).
-// `limit`: tokens beyond it do not count.  Buckets are numbered from the largest logit down.
-template <bool kByMass, typename T>
-__device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& team, const Weights& weights, uint32_t& turn, uint32_t k, double share,
-                              const Border& limit) {
-    const float largest = logit_of(weights.largest_key);
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-    uint32_t lo = 0, hi = 0xFFFFFFFFu, shift = 0, count_before = 0, count_in = 0;
-    mass_t mass_before = 0;
-    double target = 0.0;
-    bool linear = true;
-    // ranges of 32 bits shrink by 10 bits a turn: five turns at most
-    for (int turns = 0; turns < 6; ++turns, linear = false) {
-        const uint32_t which = turn & 1;
-        ++turn;
-        auto add = [&](uint32_t key, uint32_t times) {
-            if (key < lo || key > hi) return;
-            const uint32_t b = linear ? linear_bucket(key, weights.largest_key, largest) : (hi - key) >> shift;
-            if (kByMass) {
-                const mass_t m = weights.of(key) * times;
-                if (!m) return;
-                const uint32_t low = (uint32_t)m, old = atomicAdd(&sh.low[which][b], low);
-                const uint32_t carry = old + low < old;
-                if ((uint32_t)(m >> 32) + carry) atomicAdd(&sh.high[which][b], (uint32_t)(m >> 32) + carry);
-            }
-            atomicAdd(&sh.count[which][b], times);
-        };
-        slice.each([&](uint32_t key) {
-            if (!kByMass || key > limit.key) add(key, 1);
-        });
-        if (kByMass && limit.ties && team.rank == 0 && tid == 0) add(limit.key, limit.ties);
-        team.sync();
-        // every block adds up the cluster's buckets and looks for the border: two buckets to a thread
-        uint32_t count[2] = {0, 0};
-        mass_t mass[2] = {0, 0};
-        for (uint32_t r = 0; r < team.size; ++r) {
+// What every thread of the cluster has added up.
+__device__ __forceinline__ mass_t team_sum(Shared& sh, const Team& team, mass_t x) {
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+    x = warp_sum(x);
+    __syncthreads();
+    if (lane == 0) sh.warp_mass[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        x = warp_sum(lane < kWarps ? sh.warp_mass[lane] : 0);
+        if (lane < team.size) *team.of(&sh.mass[team.rank], lane) = x;
+    }
+    team.sync();
+    x = 0;
+    for (uint32_t r = 0; r < team.size; ++r) x += sh.mass[r];
+    return x;
+}
+
+// The thread's two buckets, added up over the cluster, and what is in the buckets before them; `whole`: what is in all.
+template <bool kByMass>
+struct Pair {
+    uint32_t count[2], before;
+    mass_t mass[2], mass_before, whole;
+    __device__ __forceinline__ Pair(Shared& sh, const Team& team, uint32_t which) : count{0, 0}, before(0), mass{0, 0}, mass_before(0), whole(0) {
+        const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+#pragma unroll 4
+        for (uint32_t i = 0; i < team.size; ++i) {
+            const uint32_t r = (team.rank + i) & (team.size - 1);      // each its own first: no block is read by all others at once
             const uint2 c = *(const uint2*)team.of(&sh.count[which][tid * 2], r);
             count[0] += c.x;
             count[1] += c.y;
@@ -222,27 +265,276 @@ __device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& tea
         }
         if (lane == 31) {
             sh.warp_count[warp] = upto;
-            sh.warp_mass[warp] = mass_upto;
+            if (kByMass) sh.warp_mass[warp] = mass_upto;
         }
         // the other turn's buckets are read by nobody any more
         for (uint32_t b = tid; b < kBuckets; b += kThreads) sh.count[which ^ 1][b] = sh.low[which ^ 1][b] = sh.high[which ^ 1][b] = 0;
         __syncthreads();
-        uint32_t count_base = count_before;
-        mass_t mass_base = mass_before, whole = mass_before;
+        before = upto - count[0] - count[1];
+        mass_before = mass_upto - mass[0] - mass[1];
         for (int w = 0; w < kWarps; ++w) {
             if (w < (int)warp) {
-                count_base += sh.warp_count[w];
-                mass_base += sh.warp_mass[w];
+                before += sh.warp_count[w];
+                if (kByMass) mass_before += sh.warp_mass[w];
             }
-            whole += sh.warp_mass[w];
+            if (kByMass) whole += sh.warp_mass[w];
         }
-        if (kByMass && linear) target = share * (double)whole;
-        count_base += upto - count[0] - count[1];
-        mass_base += mass_upto - mass[0] - mass[1];
+    }
+};
+
+// The place that the random number u has in the kept weight.
+__device__ __forceinline__ mass_t target_of(float u, mass_t total) {
+    const mass_t target = u > 0.0f ? u < 1.0f ? (mass_t)((double)u * (double)total) : total - 1 : 0;
+    return target < total ? target : total - 1;
+}
+__device__ __forceinline__ float logprob_of(const Weights& weights, float logit, float temperature, mass_t total) {
+    return (float)(weights.gap(logit) / (double)temperature - log((double)total * exp2(-(double)weights.bits)));
+}
+
+// A front of the order that the border is in: the logits from `from` on, `tokens` of them.
+struct Front {
+    float from;
+    uint32_t tokens;
+    mass_t whole;      // weight of all tokens; by mass alone
+};
+// By rank: the buckets up to the one with the k-th token.  By mass: the counts in the buckets bound the masses there, from below and
+// from above, which gives a bucket that the border cannot be behind.
+template <bool kByMass, typename T>
+__device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team, const Weights& weights, uint32_t top, uint32_t& turn, uint32_t k, double share) {
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32, which = turn & 1;
+    const float largest = weights.top;
+    ++turn;
+    mass_t sum = 0;
+    uint32_t n = 0;
+    if (kByMass && !weights.alone)
+        slice.each([&](T x) {
+            const float f = to_float(x);
+            atomicAdd(&sh.count[which][linear_bucket(f, largest)], 1);
+            sum += weights.template raw<false>(f);
+            ++n;
+        });
+    else
+        slice.each([&](T x) {
+            const float f = to_float(x);
+            atomicAdd(&sh.count[which][linear_bucket(f, largest)], 1);
+            if (kByMass) {
+                sum += weights.template raw<true>(f);
+                ++n;
+            }
+        });
+    Front front{-INFINITY, kList + 1, 0};
+    if (kByMass) front.whole = team_sum(sh, team, sum - n * weights.none());
+    else team.sync();
+    const Pair<false> mine(sh, team, which);
+    const uint32_t upto[2] = {mine.before + mine.count[0], mine.before + mine.count[0] + mine.count[1]};
+    bool reached[2];
+    if (kByMass) {
+        // a token of bucket b weighs between 2^(-(b + 1) fall) and 2^(-b fall)
+        const float fall = (float)(weights.step / (32.0 * (double)kPerLogit)), once = exp2f(-fall);
+        float low[2], high[2], w = exp2f(-fall * (float)(tid * 2));
+        if (weights.alone) w = 0.0f;
+        high[0] = (float)mine.count[0] * w;
+        low[0] = high[0] * once;
+        high[1] = (float)mine.count[1] * (w * once);
+        low[1] = tid * 2 + 1 < kBuckets - 1 ? high[1] * once : 0.0f;
+        high[1] += high[0];
+        low[1] += low[0];
+        float low_upto = low[1], high_upto = high[1];
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const float x = __shfl_up_sync(0xFFFFFFFFu, low_upto, o), y = __shfl_up_sync(0xFFFFFFFFu, high_upto, o);
+            if (lane >= (uint32_t)o) {
+                low_upto += x;
+                high_upto += y;
+            }
+        }
+        __syncthreads();
+        if (lane == 31) {
+            sh.warp_count[warp] = __float_as_uint(low_upto);
+            sh.warp_mass[warp] = __float_as_uint(high_upto);
+        }
+        __syncthreads();
+        float low_before = low_upto - low[1], high_before = high_upto - high[1], high_all = 0.0f;
+        for (uint32_t v = 0; v < kWarps; ++v) {
+            const float h = __uint_as_float((uint32_t)sh.warp_mass[v]);
+            if (v < warp) {
+                low_before += __uint_as_float(sh.warp_count[v]);
+                high_before += h;
+            }
+            high_all += h;
+        }
+        // an eighth of a percent, and 2^-16 of all that was added, for what is rounded
+        const double scale = exp2(-(double)weights.bits);
+        const float target = (float)(share * (double)front.whole * scale) * 1.00125f, rest = (float)((1.0 - share) * (double)front.whole * scale);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            reached[i] = upto[i] > 0 && !weights.alone &&
+                         (low_before + low[i] >= target || (high_all - (high_before + high[i])) * 1.00125f + high_all * 0x1p-16f <= rest);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) reached[i] = upto[i] >= k;
+    }
+    // the first bucket that reaches it
+    if (tid == 0) sh.bucket = kBuckets;
+    __syncthreads();
+    if (reached[0] || reached[1]) atomicMin(&sh.bucket, tid * 2 + (reached[0] ? 0 : 1));
+    __syncthreads();
+    const uint32_t bucket = sh.bucket;
+    if (bucket / 2 == tid) sh.count_in = upto[bucket & 1];
+    if (bucket < kBuckets - 1 && warp == 0) {
+        const uint32_t key = key_at<T>(bucket + 1, top, largest);
+        if (lane == 0) sh.edge[0] = key + 1;      // the lowest of the bucket
+    }
+    __syncthreads();
+    if (bucket < kBuckets - 1) {
+        front.from = Keys<T>::logit(sh.edge[0]);
+        front.tokens = sh.count_in;
+    }
+    return front;
+}
+
+// Takes the tokens of a front out of the row, in order of their ids, into the cluster's first block, which goes on alone: its list is a slice
+// like any other.  False: the block is not the first.
+template <typename T>
+__device__ bool take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
+    constexpr int E = Slice<T>::E;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    T* logits = (T*)sh.listed;
+    uint32_t here = 0;
+    slice.each([&](T x) { here += to_float(x) >= from; });
+    here = __reduce_add_sync(0xFFFFFFFFu, here);
+    __syncthreads();
+    if (lane == 0) sh.warp_count[warp] = here;
+    __syncthreads();
+    uint32_t at = 0, count = 0;
+    for (uint32_t w = 0; w < kWarps; ++w) {
+        if (w < warp) at += sh.warp_count[w];
+        count += sh.warp_count[w];
+    }
+    if (here)
+        for (uint32_t s = 0; s < slice.steps; ++s) {
+            const uint32_t place = slice.place(s);
+            const Pack<T, E> x = slice.load(place);
+            uint32_t mine = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) mine += to_float(x.v[e]) >= from;
+            if (!__any_sync(0xFFFFFFFFu, mine)) continue;
+            uint32_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t c = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= (uint32_t)o) upto += c;
+            }
+            uint32_t to = at + upto - mine;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (to_float(x.v[e]) >= from) {
+                    if (to < kList) {
+                        logits[to] = x.v[e];
+                        sh.ids[to] = slice.begin + place + e;
+                    }
+                    ++to;
+                }
+            at += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+    if (team.size > 1) {
+        if (tid < team.size) *team.of(&sh.tokens[team.rank], tid) = count;
+        team.sync();
+        if (team.rank == 0) {
+            // the others' lists behind its own: a warp to a block at a time
+            for (uint32_t r = 1 + warp; r < team.size; r += kWarps) {
+                uint32_t to = 0;
+                for (uint32_t q = 0; q < r; ++q) to += sh.tokens[q];
+                const uint32_t n = sh.tokens[r];
+                const T* theirs = team.of(logits, r);
+                const uint32_t* their_ids = team.of(&sh.ids[0], r);
+#pragma unroll 4
+                for (uint32_t i = lane; i < n; i += 32)
+                    if (to + i < kList) {
+                        logits[to + i] = theirs[i];
+                        sh.ids[to + i] = their_ids[i];
+                    }
+            }
+            count = 0;
+            for (uint32_t r = 0; r < team.size; ++r) count += sh.tokens[r];
+        }
+        team.sync();      // the others' lists have been read
+        if (team.rank != 0) return false;
+    } else __syncthreads();
+    team = Team{1, 0};
+    slice.logits = logits;
+    slice.begin = 0;
+    slice.length = count < kList ? count : kList;
+    slice.steps = (slice.length + kWarps * 32 * E - 1) / (kWarps * 32 * E);
+    slice.whole = true;
+    return true;
+}
+
+// The border by rank (k tokens are kept) or by mass (tokens are kept as long as the mass before them is below share * the whole).
+// `limit`: tokens beyond it do not count; `whole`: the weight of all others, 0: of what there is here.  Buckets are numbered from the largest logit down.
+template <bool kByMass, typename T>
+__device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& team, const Weights& weights, uint32_t top, uint32_t& turn, uint32_t k,
+                              double share, mass_t whole, const Border& limit) {
+    using K = Keys<T>;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    const float largest = weights.top;
+    uint32_t lo = K::nothing(), hi = top, shift = 0, count_before = 0, count_in = 0;
+    mass_t mass_before = 0;
+    double target = share * (double)whole;
+    bool whole_known = whole != 0;
+    const float limit_logit = K::logit(limit.key);
+    const bool ties_too = limit.ties == kAllTies;
+    bool linear = true;
+    // ranges of 32 bits shrink by 10 bits a turn: five turns at most
+    for (int turns = 0; turns < 6; ++turns, linear = false) {
+        const uint32_t which = turn & 1;
+        ++turn;
+        auto add = [&](float x, uint32_t b, uint32_t times) {
+            if (kByMass) {
+                const mass_t m = weights.of(x) * times;
+                if (!m) return;
+                const uint32_t low = (uint32_t)m, old = atomicAdd(&sh.low[which][b], low);
+                const uint32_t carry = old + low < old;
+                if ((uint32_t)(m >> 32) + carry) atomicAdd(&sh.high[which][b], (uint32_t)(m >> 32) + carry);
+            }
+            atomicAdd(&sh.count[which][b], times);
+        };
+        if (linear) {
+            if (kByMass) {
+                slice.each([&](T x) {
+                    const float f = to_float(x);
+                    if (f > limit_logit || (ties_too && f == limit_logit)) add(f, linear_bucket(f, largest), 1);
+                });
+                if (!ties_too && limit.ties && team.rank == 0 && tid == 0) add(limit_logit, linear_bucket(limit_logit, largest), limit.ties);
+            } else {
+                slice.each([&](T x) { add(0.0f, linear_bucket(to_float(x), largest), 1); });
+            }
+        } else {
+            const float low = K::logit(lo), high = K::logit(hi);
+            slice.each([&](T x) {
+                const float f = to_float(x);
+                if (f >= low && f <= high) {
+                    if (kByMass && !(f > limit_logit || (ties_too && f == limit_logit))) return;
+                    add(f, (hi - K::of(x)) >> shift, 1);
+                } else if (!kByMass && lo == K::nothing() && f != f) add(0.0f, (hi - lo) >> shift, 1);
+            });
+            if (kByMass && !ties_too && limit.ties && team.rank == 0 && tid == 0 && limit.key >= lo && limit.key <= hi)
+                add(limit_logit, (hi - limit.key) >> shift, limit.ties);
+        }
+        team.sync();
+        if (tid == 0) sh.bucket = kBuckets;
+        // every block adds up the cluster's buckets and looks for the border: two buckets to a thread
+        const Pair<kByMass> mine(sh, team, which);
+        if (kByMass && !whole_known) {
+            target = share * (double)mine.whole;
+            whole_known = true;
+        }
+        uint32_t count_base = count_before + mine.before;
+        mass_t mass_base = mass_before + mine.mass_before;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t c = count_base + count[i];
-            const mass_t m = mass_base + mass[i];
+            const uint32_t c = count_base + mine.count[i];
+            const mass_t m = mass_base + mine.mass[i];
             // the first bucket that reaches the border
             const bool before = kByMass ? count_base > 0 && (double)mass_base >= target : count_base >= k;
             const bool reached = kByMass ? c > 0 && (double)m >= target : c >= k;
@@ -250,37 +542,38 @@ __device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& tea
                 sh.bucket = tid * 2 + i;
                 sh.count_before = count_base;
                 sh.mass_before = mass_base;
-                sh.count_in = count[i];
+                sh.count_in = mine.count[i];
             }
             count_base = c;
             mass_base = m;
         }
         __syncthreads();
         const uint32_t bucket = sh.bucket;
+        if (bucket == kBuckets) return Border{K::nothing(), kAllTies};      // the border is behind all that is here
         count_before = sh.count_before;
         mass_before = sh.mass_before;
         count_in = sh.count_in;
         if (linear) {
-            if (warp < 2) {
-                const uint32_t key = key_at(bucket + warp, weights.largest_key, largest);
+            if (warp < 2 && bucket + warp < kBuckets) {
+                const uint32_t key = key_at<T>(bucket + warp, top, largest);
                 if (lane == 0) sh.edge[warp] = key;
             }
             __syncthreads();
             hi = sh.edge[0];
-            lo = bucket + 1 < kBuckets ? sh.edge[1] + 1 : kNothing;
+            lo = bucket + 1 < kBuckets ? sh.edge[1] + 1 : K::nothing();
         } else {
             hi -= bucket << shift;
             const uint32_t width = (1u << shift) - 1;
             if (hi - lo > width) lo = hi - width;
         }
-        if (kByMass ? count_in == 1 : k - count_before == count_in) return Border{lo - 1, 0};     // all of the bucket
+        if (kByMass ? count_in == 1 : k - count_before == count_in) return Border{lo, kAllTies};     // all of the bucket
         if (lo == hi) break;
         shift = 0;
         while ((hi - lo) >> shift >= kBuckets) ++shift;
     }
     if (!kByMass) return Border{lo, k - count_before};
     // the ties of one key: as many as begin below the target
-    const mass_t each = weights.of(lo);
+    const mass_t each = weights.of(K::logit(lo));
     uint32_t ties = 1;
     if (each) {
         const double want = (target - (double)mass_before) / (double)each;
@@ -292,13 +585,16 @@ __device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& tea
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps, bool staged, bool whole) {
     constexpr int E = Slice<T>::E;
-    extern __shared__ __align__(16) unsigned char stage[];
-    __shared__ Shared sh;
+    using K = Keys<T>;
+    extern __shared__ __align__(16) unsigned char memory[];
+    Shared& sh = *reinterpret_cast<Shared*>(memory);
+    unsigned char* stage = memory + kSharedBytes;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-    const Team team{cluster, blockIdx.x % cluster};
+    Team team{cluster, blockIdx.x % cluster};
+    team.started();
     const uint32_t row = blockIdx.x / cluster;
     const uint32_t slice_length = kWarps * steps * 32 * E;
     const T* logits = (const T*)a.logits.data + (uint64_t)row * a.logits.stride;
@@ -310,43 +606,36 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     slice.logits = logits + (slice.length ? slice.begin : 0);
     for (uint32_t b = tid; b < kBuckets; b += kThreads)
         for (int w = 0; w < 2; ++w) sh.count[w][b] = sh.low[w][b] = sh.high[w][b] = 0;
-    if (tid < 16) sh.roots[tid] = exp2(tid / 16.0);
-    // the slice, into shared memory, and its largest key
-    uint32_t top = kNothing;
+    if (tid < 32) sh.roots[tid] = exp2(tid / 32.0);
+    // the slice, into shared memory, and its largest logit
+    float largest = -INFINITY;
     for (uint32_t s = 0; s < steps; ++s) {
         const uint32_t at = slice.place(s);
         if (at - lane * E >= slice.length) break;
-        uint32_t key[E];
-        if (staged) {
-            T* to = (T*)stage + at;
-            Pack<T, E> x;
-            if (whole && at + E <= slice.length) x = load_pack<T, E>(slice.logits + at);
-            else
+        const Pack<T, E> x = slice.load(at);
+        if (staged) *(Pack<T, E>*)((T*)stage + at) = x;
 #pragma unroll
-                for (int e = 0; e < E; ++e) x.v[e] = at + e < slice.length ? slice.logits[at + e] : from_float<T>(-INFINITY);
-            *(Pack<T, E>*)to = x;
-#pragma unroll
-            for (int e = 0; e < E; ++e) key[e] = key_of(to_float(x.v[e]));
-        } else slice.keys(at, key);
-#pragma unroll
-        for (int e = 0; e < E; ++e) top = top > key[e] ? top : key[e];
+        for (int e = 0; e < E; ++e) largest = fmaxf(largest, to_float(x.v[e]));      // of NaN and a number: the number
     }
     if (staged) {
         slice.logits = (const T*)stage;
         slice.whole = true;
     }
-    top = warp_max(top);
+    // as keys from here on: minus zero and zero are one
+    uint32_t top = warp_max(K::of(from_float<T>(largest)));
     if (lane == 0) sh.warp_count[warp] = top;
-    team.sync();          // no block writes into another's memory before that one has started
+    __syncthreads();
+    team.all_started();
     if (warp == 0) {
         top = warp_max(lane < kWarps ? sh.warp_count[lane] : 0);
         if (lane < team.size) *team.of(&sh.largest[team.rank], lane) = top;
     }
     team.sync();
-    top = kNothing;
+    top = K::nothing();
     for (uint32_t r = 0; r < team.size; ++r) top = top > sh.largest[r] ? top : sh.largest[r];
-    const float temperature = a.temperature.of(row);
-    if (top == kNothing) {      // there is no token to draw
+    largest = K::logit(top);
+    const float given = a.temperature.of(row), temperature = given < 1e30f ? given : given >= 1e30f ? 1e30f : 0.0f;      // NaN: the largest logit
+    if (top == K::nothing()) {      // there is no token to draw
         if (team.rank == 0 && tid == 0) {
             a.token[row] = -1;
             if (a.logprob) a.logprob[row] = -INFINITY;
@@ -358,11 +647,10 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         for (uint32_t s = 0; s < steps; ++s) {
             const uint32_t at = slice.place(s);
             if (at - lane * E >= slice.length) break;
-            uint32_t key[E];
-            slice.keys(at, key);
+            const Pack<T, E> x = slice.load(at);
 #pragma unroll
             for (int e = E - 1; e >= 0; --e)
-                if (key[e] == top && slice.begin + at + e < first) first = slice.begin + at + e;
+                if (to_float(x.v[e]) == largest && slice.begin + at + e < first) first = slice.begin + at + e;
         }
         first = __reduce_min_sync(0xFFFFFFFFu, first);
         if (lane == 0) sh.warp_count[warp] = first;
@@ -380,40 +668,60 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         return;
     }
     Weights weights;
-    weights.largest = logit_of(top);
-    weights.largest_key = top;
-    weights.per_logit = 1.44269504088896340736 / (double)temperature;
-    weights.roots = sh.roots;
-    weights.magic = __longlong_as_double((long long)(1023 + 52 - (int)a.bits) << 52);
+    weights.set(largest, temperature, a.bits, sh.roots);
     uint32_t turn = 0;
-    Border border{0, 0};
-    const int32_t k = a.top_k.of(row);
-    if (k > 0 && (uint32_t)k < a.V) border = find_border<false>(sh, slice, team, weights, turn, (uint32_t)k, 0.0, border);
-    const float p = a.top_p.of(row);
-    if (p < 1.0f) {
-        const Border b = find_border<true>(sh, slice, team, weights, turn, 0, (double)p, border);
-        if (b < border) border = b;
-    }
-    const float min_p = a.min_p.of(row);
+    Border border{K::nothing(), kAllTies};
+    const int32_t first_k = a.top_k.of(row);
+    const uint32_t k = first_k > 0 && (uint32_t)first_k < a.V ? (uint32_t)first_k : 0;
+    const float p = a.top_p.of(row), min_p = a.min_p.of(row), u = a.uniform[row];
     if (min_p > 0.0f) {
         // the smallest logit that is close enough to the largest
         const double least = min_p < 1.0f ? (double)temperature * log((double)min_p) : 0.0;
-        uint32_t key = key_of((float)(weights.largest + least));
+        auto close = [&](uint32_t x) { return x == top || weights.gap(K::logit(x)) >= least; };
+        uint32_t key = K::of(from_float<T>((float)((double)largest + least)));
         if (key > top) key = top;
-        auto close = [&](uint32_t x) { return x == top || (double)logit_of(x) - weights.largest >= least; };
-        while (key > kNothing && close(key - 1)) --key;
+        while (key > K::nothing() && close(key - 1)) --key;
         while (!close(key)) ++key;
-        const Border b{key - 1, 0};
+        border.key = key;
+    }
+    bool taken_out = false;
+    if (k || p < 1.0f) {
+        mass_t whole = 0;
+        if (a.V > kShort) {
+            const Front front = k ? find_front<false>(sh, slice, team, weights, top, turn, k, 0.0)
+                                  : find_front<true>(sh, slice, team, weights, top, turn, 0, (double)p);
+            whole = front.whole;
+            if (front.tokens <= kList) {
+                taken_out = true;
+                if (!take_out(sh, slice, team, front.from)) return;
+            }
+        }
+        Border b{K::nothing(), kAllTies};
+        if (k) b = find_border<false>(sh, slice, team, weights, top, turn, k, 0.0, 0, b);
         if (b < border) border = b;
+        if (p < 1.0f) {
+            b = find_border<true>(sh, slice, team, weights, top, turn, 0, (double)p, whole, b);
+            if (b < border) border = b;
+        }
     }
     // kept weights in order of ids: of each warp's run, of the blocks, of the row
+    const float edge = K::logit(border.key);
     mass_t mass = 0;
-    uint32_t ties = 0;
-    slice.each([&](uint32_t key) {
-        if (key > border.key) mass += weights.of(key);
-        ties += key == border.key;
-    });
-    mass = warp_sum(mass);
+    uint32_t ties = 0, n = 0;
+    if (edge == -INFINITY && !weights.alone)      // all of them
+        slice.each([&](T x) {
+            mass += weights.template raw<false>(to_float(x));
+            ++n;
+        });
+    else
+        slice.each([&](T x) {
+            const float f = to_float(x);
+            if (f > edge) {
+                mass += weights.of(f);
+            }
+            ties += f == edge;
+        });
+    mass = warp_sum(mass - n * weights.none());
     ties = __reduce_add_sync(0xFFFFFFFFu, ties);
     __syncthreads();      // the arrays were read by the search
     if (lane == 0) {
@@ -430,7 +738,7 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         }
     }
     team.sync();
-    const mass_t each = border.ties ? weights.of(border.key) : 0;
+    const mass_t each = weights.of(edge);
     // with `seen` ties before it, a run with `here` ties has so many that are kept
     auto kept_ties = [&](uint32_t seen, uint32_t here) { return seen >= border.ties ? 0u : border.ties - seen < here ? border.ties - seen : here; };
     mass_t total = 0, before = 0;
@@ -443,9 +751,7 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         total += sh.mass[r] + kept_ties(seen, sh.ties[r]) * each;
         seen += sh.ties[r];
     }
-    const float u = a.uniform[row];
-    mass_t target = u > 0.0f ? u < 1.0f ? (mass_t)((double)u * (double)total) : total - 1 : 0;
-    if (target >= total) target = total - 1;
+    const mass_t target = target_of(u, total);
     for (uint32_t w = 0; w < warp; ++w) {
         before += sh.warp_mass[w] + kept_ties(seen_before, sh.warp_count[w]) * each;
         seen_before += sh.warp_count[w];
@@ -453,12 +759,12 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     const mass_t mine = sh.warp_mass[warp] + kept_ties(seen_before, sh.warp_count[warp]) * each;
     if (target < before || target >= before + mine) return;
     // the warp that has the token goes through its run
-    for (uint32_t s = 0; s < steps; ++s) {
+    for (uint32_t s = 0; s < slice.steps; ++s) {
         const uint32_t at = slice.place(s);
-        uint32_t key[E], here = 0;
-        slice.keys(at, key);
+        const Pack<T, E> x = slice.load(at);
+        uint32_t here = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) here += key[e] == border.key;
+        for (int e = 0; e < E; ++e) here += to_float(x.v[e]) == edge;
         uint32_t upto = here;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -469,8 +775,9 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         mass_t m[E], sum = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            m[e] = key[e] > border.key ? weights.of(key[e]) : key[e] == border.key && tie < border.ties ? each : 0;
-            tie += key[e] == border.key;
+            const float f = to_float(x.v[e]);
+            m[e] = f > edge ? weights.of(f) : f == edge && tie < border.ties ? each : 0;
+            tie += f == edge;
             sum += m[e];
         }
         mass_t running = sum;
@@ -482,16 +789,17 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         mass_t from = before + running - sum;
         if (target >= from && target < from + sum) {
             int found = -1;
+            float logit = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 from += m[e];
-                if (found < 0 && target < from) found = e;
+                if (found < 0 && target < from) {
+                    found = e;
+                    logit = to_float(x.v[e]);
+                }
             }
-            a.token[row] = slice.begin + at + found;
-            if (a.logprob) {
-                const double gap = key[found] == top ? 0.0 : (double)logit_of(key[found]) - weights.largest;
-                a.logprob[row] = (float)(gap / (double)temperature - log((double)total * exp2(-(double)a.bits)));
-            }
+            a.token[row] = taken_out ? sh.ids[at + found] : slice.begin + at + found;
+            if (a.logprob) a.logprob[row] = logprob_of(weights, logit, temperature, total);
         }
         before += __shfl_sync(0xFFFFFFFFu, running, 31);
         seen_before += __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -516,13 +824,13 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
         const bool staged = bytes <= kStage;
         const bool whole = (uintptr_t)a.logits.data % 16 == 0 && (a.n < 2 || a.logits.stride % E == 0);
         auto* kernel = k_sample<T>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStage);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
         if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(a.n * cluster);
         cfg.blockDim = dim3(kThreads);
-        cfg.dynamicSmemBytes = staged ? bytes : 0;
+        cfg.dynamicSmemBytes = kSharedBytes + (staged ? bytes : 0);
         cfg.stream = stream;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
