@@ -72,10 +72,10 @@ struct Weights {
     uint32_t bits;
 
     __device__ __forceinline__ double gap(float x) const { return x == top ? 0.0 : (double)x - largest; }
-    __device__ void set(float largest_logit, float temperature, uint32_t weight_bits, const double* table) {
+    __device__ void set(float largest_logit, float temperature, double log2e_32_by_temperature, uint32_t weight_bits, const double* table) {
         top = largest_logit;
         largest = (double)top;
-        step = 32.0 * kLog2e / (double)temperature;
+        step = log2e_32_by_temperature;
         roots = table;
         bits = weight_bits;
         magic = __longlong_as_double((long long)(1023 + 52 - (int)bits) << 52);
@@ -381,25 +381,23 @@ __device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team,
     __syncthreads();
     const uint32_t bucket = sh.bucket;
     if (bucket / 2 == tid) sh.count_in = upto[bucket & 1];
-    if (bucket < kBuckets - 1 && warp == 0) {
-        const uint32_t key = key_at<T>(bucket + 1, top, largest);
-        if (lane == 0) sh.edge[0] = key + 1;      // the lowest of the bucket
-    }
     __syncthreads();
     if (bucket < kBuckets - 1) {
-        front.from = Keys<T>::logit(sh.edge[0]);
+        // below every logit of the bucket, by what the subtraction and the product there may have rounded
+        const float edge = largest - (float)(bucket + 1) * ((1.0f + 0x1p-20f) / kPerLogit);
+        front.from = fmaxf(edge - fabsf(edge) * 0x1p-21f - fabsf(largest) * 0x1p-22f, -3.4028234e38f);
         front.tokens = sh.count_in;
     }
     return front;
 }
 
-// Takes the tokens of a front out of the row, in order of their ids, into the cluster's first block, which goes on alone: its list is a slice
-// like any other.  False: the block is not the first.
+enum Taken { kTooMany, kByOther, kHere };
+// Takes the logits from `from` on out of the row, in order of their ids, into the cluster's first block, which goes on alone: its list is a
+// slice like any other.
 template <typename T>
-__device__ bool take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
+__device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
     constexpr int E = Slice<T>::E;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-    T* logits = (T*)sh.listed;
     uint32_t here = 0;
     slice.each([&](T x) { here += to_float(x) >= from; });
     here = __reduce_add_sync(0xFFFFFFFFu, here);
@@ -408,83 +406,76 @@ __device__ bool take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
     __syncthreads();
     uint32_t at = 0, count = 0;
     for (uint32_t w = 0; w < kWarps; ++w) {
-        if (w < warp) at += sh.warp_count[w];
-        count += sh.warp_count[w];
+        const uint32_t n = sh.warp_count[w];
+        if (w < warp) at += n;
+        count += n;
     }
+    if (tid < team.size) *team.of(&sh.tokens[team.rank], tid) = count;
+    team.sync();
+    count = 0;
+    for (uint32_t r = 0; r < team.size; ++r) {
+        const uint32_t n = sh.tokens[r];
+        if (r < team.rank) at += n;
+        count += n;
+    }
+    if (count > kList) return kTooMany;
+    T* logits = team.of((T*)sh.listed, 0);
+    uint32_t* ids = team.of(&sh.ids[0], 0);
     if (here)
         for (uint32_t s = 0; s < slice.steps; ++s) {
             const uint32_t place = slice.place(s);
             const Pack<T, E> x = slice.load(place);
-            uint32_t mine = 0;
+            uint32_t mine = 0;      // one bit for each that goes
 #pragma unroll
-            for (int e = 0; e < E; ++e) mine += to_float(x.v[e]) >= from;
+            for (int e = 0; e < E; ++e) mine |= (to_float(x.v[e]) >= from ? 1u : 0u) << e;
             if (!__any_sync(0xFFFFFFFFu, mine)) continue;
-            uint32_t upto = mine;
+            uint32_t upto = __popc(mine);
+            const uint32_t own = upto;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const uint32_t c = __shfl_up_sync(0xFFFFFFFFu, upto, o);
                 if (lane >= (uint32_t)o) upto += c;
             }
-            uint32_t to = at + upto - mine;
+            uint32_t to = at + upto - own;
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (to_float(x.v[e]) >= from) {
+                if (mine >> e & 1) {
                     if (to < kList) {
                         logits[to] = x.v[e];
-                        sh.ids[to] = slice.begin + place + e;
+                        ids[to] = slice.begin + place + e;
                     }
                     ++to;
                 }
             at += __shfl_sync(0xFFFFFFFFu, upto, 31);
         }
-    if (team.size > 1) {
-        if (tid < team.size) *team.of(&sh.tokens[team.rank], tid) = count;
-        team.sync();
-        if (team.rank == 0) {
-            // the others' lists behind its own: a warp to a block at a time
-            for (uint32_t r = 1 + warp; r < team.size; r += kWarps) {
-                uint32_t to = 0;
-                for (uint32_t q = 0; q < r; ++q) to += sh.tokens[q];
-                const uint32_t n = sh.tokens[r];
-                const T* theirs = team.of(logits, r);
-                const uint32_t* their_ids = team.of(&sh.ids[0], r);
-#pragma unroll 4
-                for (uint32_t i = lane; i < n; i += 32)
-                    if (to + i < kList) {
-                        logits[to + i] = theirs[i];
-                        sh.ids[to + i] = their_ids[i];
-                    }
-            }
-            count = 0;
-            for (uint32_t r = 0; r < team.size; ++r) count += sh.tokens[r];
-        }
-        team.sync();      // the others' lists have been read
-        if (team.rank != 0) return false;
-    } else __syncthreads();
+    team.sync();      // all is there
+    if (team.rank != 0) return kByOther;
     team = Team{1, 0};
-    slice.logits = logits;
+    slice.logits = (const T*)sh.listed;
     slice.begin = 0;
-    slice.length = count < kList ? count : kList;
-    slice.steps = (slice.length + kWarps * 32 * E - 1) / (kWarps * 32 * E);
+    slice.length = count;
+    slice.steps = (count + kWarps * 32 * E - 1) / (kWarps * 32 * E);
     slice.whole = true;
-    return true;
+    return kHere;
 }
 
 // The border by rank (k tokens are kept) or by mass (tokens are kept as long as the mass before them is below share * the whole).
-// `limit`: tokens beyond it do not count; `whole`: the weight of all others, 0: of what there is here.  Buckets are numbered from the largest logit down.
+// `limit`: tokens beyond it do not count; `whole`: the weight of all others, 0: of what there is here.  `lowest`: the key that no logit here
+// is below; minus infinity's: the first turn has buckets of equal width.  Buckets are numbered from the largest logit down.
 template <bool kByMass, typename T>
 __device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& team, const Weights& weights, uint32_t top, uint32_t& turn, uint32_t k,
-                              double share, mass_t whole, const Border& limit) {
+                              double share, mass_t whole, const Border& limit, uint32_t lowest) {
     using K = Keys<T>;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
     const float largest = weights.top;
-    uint32_t lo = K::nothing(), hi = top, shift = 0, count_before = 0, count_in = 0;
+    uint32_t lo = lowest, hi = top, shift = 0, count_before = 0, count_in = 0;
     mass_t mass_before = 0;
     double target = share * (double)whole;
     bool whole_known = whole != 0;
     const float limit_logit = K::logit(limit.key);
     const bool ties_too = limit.ties == kAllTies;
-    bool linear = true;
+    bool linear = lowest == K::nothing();
+    while ((hi - lo) >> shift >= kBuckets) ++shift;
     // ranges of 32 bits shrink by 10 bits a turn: five turns at most
     for (int turns = 0; turns < 6; ++turns, linear = false) {
         const uint32_t which = turn & 1;
@@ -607,6 +598,8 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     for (uint32_t b = tid; b < kBuckets; b += kThreads)
         for (int w = 0; w < 2; ++w) sh.count[w][b] = sh.low[w][b] = sh.high[w][b] = 0;
     if (tid < 32) sh.roots[tid] = exp2(tid / 32.0);
+    const float given = a.temperature.of(row), temperature = given < 1e30f ? given : given >= 1e30f ? 1e30f : 0.0f;      // NaN: the largest logit
+    const double step = 32.0 * kLog2e / (double)temperature;
     // the slice, into shared memory, and its largest logit
     float largest = -INFINITY;
     for (uint32_t s = 0; s < steps; ++s) {
@@ -634,7 +627,6 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     top = K::nothing();
     for (uint32_t r = 0; r < team.size; ++r) top = top > sh.largest[r] ? top : sh.largest[r];
     largest = K::logit(top);
-    const float given = a.temperature.of(row), temperature = given < 1e30f ? given : given >= 1e30f ? 1e30f : 0.0f;      // NaN: the largest logit
     if (top == K::nothing()) {      // there is no token to draw
         if (team.rank == 0 && tid == 0) {
             a.token[row] = -1;
@@ -668,7 +660,7 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         return;
     }
     Weights weights;
-    weights.set(largest, temperature, a.bits, sh.roots);
+    weights.set(largest, temperature, step, a.bits, sh.roots);
     uint32_t turn = 0;
     Border border{K::nothing(), kAllTies};
     const int32_t first_k = a.top_k.of(row);
@@ -687,20 +679,26 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     bool taken_out = false;
     if (k || p < 1.0f) {
         mass_t whole = 0;
+        uint32_t lowest = K::nothing();
         if (a.V > kShort) {
             const Front front = k ? find_front<false>(sh, slice, team, weights, top, turn, k, 0.0)
                                   : find_front<true>(sh, slice, team, weights, top, turn, 0, (double)p);
             whole = front.whole;
             if (front.tokens <= kList) {
-                taken_out = true;
-                if (!take_out(sh, slice, team, front.from)) return;
+                const Taken taken = take_out(sh, slice, team, front.from);
+                if (taken == kByOther) return;
+                if (taken == kHere) {
+                    taken_out = true;
+                    lowest = K::of(from_float<T>(front.from));
+                    lowest -= lowest > K::nothing();      // rounded up, maybe
+                }
             }
         }
         Border b{K::nothing(), kAllTies};
-        if (k) b = find_border<false>(sh, slice, team, weights, top, turn, k, 0.0, 0, b);
+        if (k) b = find_border<false>(sh, slice, team, weights, top, turn, k, 0.0, 0, b, lowest);
         if (b < border) border = b;
         if (p < 1.0f) {
-            b = find_border<true>(sh, slice, team, weights, top, turn, 0, (double)p, whole, b);
+            b = find_border<true>(sh, slice, team, weights, top, turn, 0, (double)p, whole, b, lowest);
             if (b < border) border = b;
         }
     }
