@@ -14,6 +14,8 @@
 // asked for.  (Slices that do not fit are read again, out of the level-2 cache.)
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "columns.cuh"
 #include "layers.h"
 
@@ -89,12 +91,17 @@ struct Weights {
     // As raw bits: the sum of n of them less n times none() is the sum of the weights, as whole numbers.
     // exp by table and polynomial (after Tang, ACM TOMS 15, 1989): 2^(s/32) = 2^(n/32) 2^((s-n)/32) with |s - n| <= 1/2, the
     // latter by its series up to the fifth power (what is left out is below 2.3e-15 of it).
+    // fall: how many 32nds of an octave it is below the largest (rounded).
     template <bool kAlone>
-    __device__ __forceinline__ mass_t raw(float x) const {
-        if (kAlone) return (mass_t)__double_as_longlong((x == top ? 1.0 : 0.0) + magic);
+    __device__ __forceinline__ mass_t raw(float x, int& fall) const {
+        if (kAlone) {
+            fall = x == top ? 0 : kBuckets;
+            return (mass_t)__double_as_longlong((x == top ? 1.0 : 0.0) + magic);
+        }
         const double g = (double)fmaxf(x, least) - largest;
         const double shifted = fma(g, step, 0x1.8p52);
         const int n = (int)__double_as_longlong(shifted);
+        fall = -n;
         const double r = fma(g, step, 0x1.8p52 - shifted);
         double y = kSeries[5];
         y = fma(y, r, kSeries[4]);
@@ -104,6 +111,11 @@ struct Weights {
         y = fma(y, r, 1.0) * roots[n & 31];
         y = __hiloint2double(__double2hiint(y) + ((n >> 5) << 20), __double2loint(y));
         return (mass_t)__double_as_longlong(y + magic);
+    }
+    template <bool kAlone>
+    __device__ __forceinline__ mass_t raw(float x) const {
+        int fall;
+        return raw<kAlone>(x, fall);
     }
     __device__ __forceinline__ mass_t none() const { return (mass_t)__double_as_longlong(magic); }
     __device__ __forceinline__ mass_t of(float x) const { return (alone ? raw<true>(x) : raw<false>(x)) - none(); }
@@ -147,9 +159,8 @@ struct Slice {
     uint32_t begin, length;    // in the row
     uint32_t steps;
     bool whole;                // accesses of 16 bytes
-    __device__ __forceinline__ uint32_t place(uint32_t step) const {
-        return ((threadIdx.x / 32 * steps + step) * 32 + (threadIdx.x & 31)) * E;
-    }
+    __device__ __forceinline__ uint32_t place(uint32_t run, uint32_t step) const { return ((run * steps + step) * 32 + (threadIdx.x & 31)) * E; }
+    __device__ __forceinline__ uint32_t place(uint32_t step) const { return place(threadIdx.x / 32, step); }
     // E logits from `at` on; behind the slice: minus infinity
     __device__ __forceinline__ Pack<T, E> load(uint32_t at) const {
         if (whole && at + E <= length) return load_pack<T, E>(logits + at);
@@ -158,15 +169,42 @@ struct Slice {
         for (int e = 0; e < E; ++e) x.v[e] = at + e < length ? logits[at + e] : from_float<T>(-INFINITY);
         return x;
     }
+    // One bit for each logit from `from` on.
+    static __device__ __forceinline__ uint32_t from_on(const Pack<T, E>& x, T from) {
+        uint32_t mask = 0;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) mask |= (x.v[e] >= from ? 1u : 0u) << e;
+        } else {
+            // two comparisons in one; of four results' bytes a bit each
+            using Two = std::conditional_t<std::is_same_v<T, __half>, __half2, __nv_bfloat162>;
+            const Two* two = reinterpret_cast<const Two*>(x.v);
+            Two edge;
+            edge.x = edge.y = from;
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                const uint32_t bytes = __byte_perm(__hge2_mask(two[e / 2], edge), __hge2_mask(two[e / 2 + 1], edge), 0x6420);
+                mask |= ((bytes & 0x08040201u) * 0x01010101u >> 24) << e;
+            }
+        }
+        return mask;
+    }
+    // f(place, logits) for the accesses of the thread.  (Several read before the first is used: no faster for 32-bit logits, and a fifth slower
+    // for 16-bit ones, for want of registers.)
     template <typename F>
-    __device__ __forceinline__ void each(F&& f) const {
+    __device__ __forceinline__ void accesses(F&& f) const {
         for (uint32_t s = 0; s < steps; ++s) {
             const uint32_t at = place(s);
-            if (at - (threadIdx.x & 31) * E >= length) break;
-            const Pack<T, E> x = load(at);
+            if (at - (threadIdx.x & 31) * E >= length) break;      // the same for a warp
+            f(at, load(at));
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F&& f) const {
+        accesses([&](uint32_t, const Pack<T, E>& x) {
 #pragma unroll
             for (int e = 0; e < E; ++e) f(x.v[e]);
-        }
+        });
     }
 };
 
@@ -308,20 +346,14 @@ __device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team,
     uint32_t n = 0;
     if (kByMass && !weights.alone)
         slice.each([&](T x) {
-            const float f = to_float(x);
-            atomicAdd(&sh.count[which][linear_bucket(f, largest)], 1);
-            sum += weights.template raw<false>(f);
+            int fall;
+            sum += weights.template raw<false>(to_float(x), fall);
+            atomicAdd(&sh.count[which][fall < (int)kBuckets ? fall : kBuckets - 1], 1);
             ++n;
         });
-    else
-        slice.each([&](T x) {
-            const float f = to_float(x);
-            atomicAdd(&sh.count[which][linear_bucket(f, largest)], 1);
-            if (kByMass) {
-                sum += weights.template raw<true>(f);
-                ++n;
-            }
-        });
+    else if (!kByMass)
+        slice.each([&](T x) { atomicAdd(&sh.count[which][linear_bucket(to_float(x), largest)], 1); });
+    else return Front{-INFINITY, kList + 1, 0};      // few have weight, and who knows how many: the search among all finds them
     Front front{-INFINITY, kList + 1, 0};
     if (kByMass) front.whole = team_sum(sh, team, sum - n * weights.none());
     else team.sync();
@@ -329,10 +361,9 @@ __device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team,
     const uint32_t upto[2] = {mine.before + mine.count[0], mine.before + mine.count[0] + mine.count[1]};
     bool reached[2];
     if (kByMass) {
-        // a token of bucket b weighs between 2^(-(b + 1) fall) and 2^(-b fall)
-        const float fall = (float)(weights.step / (32.0 * (double)kPerLogit)), once = exp2f(-fall);
-        float low[2], high[2], w = exp2f(-fall * (float)(tid * 2));
-        if (weights.alone) w = 0.0f;
+        // a token of bucket b weighs between 2^(-(b + 1/2) / 32) and 2^(-(b - 1/2) / 32)
+        const float once = exp2f(-1.0f / 32.0f), w = exp2f((0.5f - (float)(tid * 2)) / 32.0f);
+        float low[2], high[2];
         high[0] = (float)mine.count[0] * w;
         low[0] = high[0] * once;
         high[1] = (float)mine.count[1] * (w * once);
@@ -368,7 +399,7 @@ __device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team,
         const float target = (float)(share * (double)front.whole * scale) * 1.00125f, rest = (float)((1.0 - share) * (double)front.whole * scale);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            reached[i] = upto[i] > 0 && !weights.alone &&
+            reached[i] = upto[i] > 0 &&
                          (low_before + low[i] >= target || (high_all - (high_before + high[i])) * 1.00125f + high_all * 0x1p-16f <= rest);
     } else {
 #pragma unroll
@@ -383,8 +414,9 @@ __device__ Front find_front(Shared& sh, const Slice<T>& slice, const Team& team,
     if (bucket / 2 == tid) sh.count_in = upto[bucket & 1];
     __syncthreads();
     if (bucket < kBuckets - 1) {
-        // below every logit of the bucket, by what the subtraction and the product there may have rounded
-        const float edge = largest - (float)(bucket + 1) * ((1.0f + 0x1p-20f) / kPerLogit);
+        // below every logit of the bucket, by what the arithmetic there and here may have rounded
+        const float width = kByMass ? (float)(1.0 / weights.step) : 1.0f / kPerLogit;
+        const float edge = largest - ((float)bucket + (kByMass ? 0.5f : 1.0f)) * width * (1.0f + 0x1p-20f);
         front.from = fmaxf(edge - fabsf(edge) * 0x1p-21f - fabsf(largest) * 0x1p-22f, -3.4028234e38f);
         front.tokens = sh.count_in;
     }
@@ -395,11 +427,11 @@ enum Taken { kTooMany, kByOther, kHere };
 // Takes the logits from `from` on out of the row, in order of their ids, into the cluster's first block, which goes on alone: its list is a
 // slice like any other.
 template <typename T>
-__device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
+__device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
     constexpr int E = Slice<T>::E;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
     uint32_t here = 0;
-    slice.each([&](T x) { here += to_float(x) >= from; });
+    slice.accesses([&](uint32_t, const Pack<T, E>& x) { here += __popc(slice.from_on(x, from)); });
     here = __reduce_add_sync(0xFFFFFFFFu, here);
     __syncthreads();
     if (lane == 0) sh.warp_count[warp] = here;
@@ -422,32 +454,24 @@ __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, float from) {
     T* logits = team.of((T*)sh.listed, 0);
     uint32_t* ids = team.of(&sh.ids[0], 0);
     if (here)
-        for (uint32_t s = 0; s < slice.steps; ++s) {
-            const uint32_t place = slice.place(s);
-            const Pack<T, E> x = slice.load(place);
-            uint32_t mine = 0;      // one bit for each that goes
-#pragma unroll
-            for (int e = 0; e < E; ++e) mine |= (to_float(x.v[e]) >= from ? 1u : 0u) << e;
-            if (!__any_sync(0xFFFFFFFFu, mine)) continue;
-            uint32_t upto = __popc(mine);
-            const uint32_t own = upto;
+        slice.accesses([&](uint32_t place, const Pack<T, E>& x) {
+            uint32_t mine = slice.from_on(x, from);
+            if (!__any_sync(0xFFFFFFFFu, mine)) return;
+            const uint32_t own = __popc(mine);
+            uint32_t upto = own;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const uint32_t c = __shfl_up_sync(0xFFFFFFFFu, upto, o);
                 if (lane >= (uint32_t)o) upto += c;
             }
-            uint32_t to = at + upto - own;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (mine >> e & 1) {
-                    if (to < kList) {
-                        logits[to] = x.v[e];
-                        ids[to] = slice.begin + place + e;
-                    }
-                    ++to;
-                }
+            // few lanes have any, and few of them more than one: read again rather than picked from registers
+            for (uint32_t to = at + upto - own; mine; mine &= mine - 1, ++to) {
+                const uint32_t id = place + __ffs(mine) - 1;
+                logits[to] = slice.logits[id];
+                ids[to] = slice.begin + id;
+            }
             at += __shfl_sync(0xFFFFFFFFu, upto, 31);
-        }
+        });
     team.sync();      // all is there
     if (team.rank != 0) return kByOther;
     team = Team{1, 0};
@@ -602,14 +626,11 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     const double step = 32.0 * kLog2e / (double)temperature;
     // the slice, into shared memory, and its largest logit
     float largest = -INFINITY;
-    for (uint32_t s = 0; s < steps; ++s) {
-        const uint32_t at = slice.place(s);
-        if (at - lane * E >= slice.length) break;
-        const Pack<T, E> x = slice.load(at);
+    slice.accesses([&](uint32_t at, const Pack<T, E>& x) {
         if (staged) *(Pack<T, E>*)((T*)stage + at) = x;
 #pragma unroll
         for (int e = 0; e < E; ++e) largest = fmaxf(largest, to_float(x.v[e]));      // of NaN and a number: the number
-    }
+    });
     if (staged) {
         slice.logits = (const T*)stage;
         slice.whole = true;
@@ -636,14 +657,11 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     }
     if (!(temperature > 0.0f)) {      // the largest logit, its lowest id
         uint32_t first = 0xFFFFFFFFu;
-        for (uint32_t s = 0; s < steps; ++s) {
-            const uint32_t at = slice.place(s);
-            if (at - lane * E >= slice.length) break;
-            const Pack<T, E> x = slice.load(at);
+        slice.accesses([&](uint32_t at, const Pack<T, E>& x) {
 #pragma unroll
             for (int e = E - 1; e >= 0; --e)
                 if (to_float(x.v[e]) == largest && slice.begin + at + e < first) first = slice.begin + at + e;
-        }
+        });
         first = __reduce_min_sync(0xFFFFFFFFu, first);
         if (lane == 0) sh.warp_count[warp] = first;
         __syncthreads();
@@ -685,12 +703,13 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
                                   : find_front<true>(sh, slice, team, weights, top, turn, 0, (double)p);
             whole = front.whole;
             if (front.tokens <= kList) {
-                const Taken taken = take_out(sh, slice, team, front.from);
+                T from = from_float<T>(front.from);
+                if (to_float(from) > front.from) from = from_float<T>(K::logit(K::of(from) - 1));      // rounded up
+                const Taken taken = take_out(sh, slice, team, from);
                 if (taken == kByOther) return;
                 if (taken == kHere) {
                     taken_out = true;
-                    lowest = K::of(from_float<T>(front.from));
-                    lowest -= lowest > K::nothing();      // rounded up, maybe
+                    lowest = K::of(from);
                 }
             }
         }
@@ -714,9 +733,7 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     else
         slice.each([&](T x) {
             const float f = to_float(x);
-            if (f > edge) {
-                mass += weights.of(f);
-            }
+            if (f > edge) mass += weights.of(f);
             ties += f == edge;
         });
     mass = warp_sum(mass - n * weights.none());
@@ -750,34 +767,70 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         seen += sh.ties[r];
     }
     const mass_t target = target_of(u, total);
-    for (uint32_t w = 0; w < warp; ++w) {
-        before += sh.warp_mass[w] + kept_ties(seen_before, sh.warp_count[w]) * each;
+    // the warp's run that has the token: all threads find the same
+    bool here = false;
+    uint32_t run = 0;
+    for (uint32_t w = 0; w < kWarps; ++w) {
+        const mass_t m = sh.warp_mass[w] + kept_ties(seen_before, sh.warp_count[w]) * each;
+        if (target >= before && target < before + m) {
+            here = true;
+            run = w;
+            break;
+        }
+        before += m;
         seen_before += sh.warp_count[w];
     }
-    const mass_t mine = sh.warp_mass[warp] + kept_ties(seen_before, sh.warp_count[warp]) * each;
-    if (target < before || target >= before + mine) return;
-    // the warp that has the token goes through its run
-    for (uint32_t s = 0; s < slice.steps; ++s) {
-        const uint32_t at = slice.place(s);
-        const Pack<T, E> x = slice.load(at);
-        uint32_t here = 0;
+    if (!here) return;
+    // the access of that run that has it: an access to a warp, kWarps at a time
+    for (uint32_t s0 = 0; s0 < slice.steps; s0 += kWarps) {
+        const uint32_t at = slice.place(run, s0 + warp);
+        const Pack<T, E> x = s0 + warp < slice.steps ? slice.load(at) : slice.load(slice.length);
+        mass_t m[E], sum = 0;
+        uint32_t equal = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) here += to_float(x.v[e]) == edge;
-        uint32_t upto = here;
+        for (int e = 0; e < E; ++e) {
+            const float f = to_float(x.v[e]);
+            m[e] = f > edge ? weights.of(f) : 0;
+            equal += f == edge;
+            sum += m[e];
+        }
+        const mass_t all = warp_sum(sum);
+        const uint32_t all_equal = __reduce_add_sync(0xFFFFFFFFu, equal);
+        __syncthreads();
+        if (lane == 0) {
+            sh.warp_mass[warp] = all;
+            sh.warp_count[warp] = all_equal;
+        }
+        __syncthreads();
+        bool mine = false, found = false;
+        for (uint32_t w = 0; w < kWarps && !found; ++w) {
+            const mass_t k = sh.warp_mass[w] + kept_ties(seen_before, sh.warp_count[w]) * each;
+            found = target < before + k;
+            mine = found && w == warp;
+            if (!found) {
+                before += k;
+                seen_before += sh.warp_count[w];
+            }
+        }
+        if (!found) continue;
+        if (!mine) return;
+        // of that access, the lane and the logit
+        uint32_t upto = equal;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
             const uint32_t c = __shfl_up_sync(0xFFFFFFFFu, upto, o);
             if (lane >= (uint32_t)o) upto += c;
         }
-        uint32_t tie = seen_before + upto - here;
-        mass_t m[E], sum = 0;
+        uint32_t tie = seen_before + upto - equal;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float f = to_float(x.v[e]);
-            m[e] = f > edge ? weights.of(f) : f == edge && tie < border.ties ? each : 0;
-            tie += f == edge;
-            sum += m[e];
-        }
+        for (int e = 0; e < E; ++e)
+            if (to_float(x.v[e]) == edge) {
+                if (tie < border.ties) {
+                    m[e] = each;
+                    sum += each;
+                }
+                ++tie;
+            }
         mass_t running = sum;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -786,22 +839,20 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
         }
         mass_t from = before + running - sum;
         if (target >= from && target < from + sum) {
-            int found = -1;
+            int place = -1;
             float logit = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 from += m[e];
-                if (found < 0 && target < from) {
-                    found = e;
+                if (place < 0 && target < from) {
+                    place = e;
                     logit = to_float(x.v[e]);
                 }
             }
-            a.token[row] = taken_out ? sh.ids[at + found] : slice.begin + at + found;
+            a.token[row] = taken_out ? sh.ids[at + place] : slice.begin + at + place;
             if (a.logprob) a.logprob[row] = logprob_of(weights, logit, temperature, total);
         }
-        before += __shfl_sync(0xFFFFFFFFu, running, 31);
-        seen_before += __shfl_sync(0xFFFFFFFFu, upto, 31);
-        if (target < before) return;
+        return;
     }
 }
 
@@ -813,16 +864,18 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
     return with_type(a.logits.type, [&](auto t) {
         using T = decltype(t);
         constexpr uint32_t E = Slice<T>::E, unit = kWarps * 32 * E;      // tokens of one access of a block
-        // blocks enough for the device, and for a slice to fit
+        // Blocks enough for the device, two to a multiprocessor, as long as a slice is worth the cluster's barriers.  us, one block to
+        // a row against more (a power of two each): 256 rows of 100,000 0.9 of the mass: 174, 167, 192; first 50: 66, 86, 109; 64 rows of 10,000: 27, 27,
+        // 31, 48; one row of 100,000: 69, 47, 34, 29, 26
         uint32_t cluster = 1;
-        while (cluster < kMostCluster && cluster * unit < a.V &&
-               ((uint64_t)a.n * cluster < (uint64_t)sms * 2 || (uint64_t)a.V * sizeof(T) > (uint64_t)cluster * 56 * 1024)) cluster *= 2;
+        while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 5000) cluster *= 2;
         const uint32_t steps = (uint32_t)(((uint64_t)a.V + (uint64_t)cluster * unit - 1) / ((uint64_t)cluster * unit));
         const uint64_t bytes = (uint64_t)steps * unit * sizeof(T);
         const bool staged = bytes <= kStage;
         const bool whole = (uintptr_t)a.logits.data % 16 == 0 && (a.n < 2 || a.logits.stride % E == 0);
         auto* kernel = k_sample<T>;
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
