@@ -24,6 +24,7 @@
 // instead made it slower (443 us).
 #include "adamw.cuh"
 #include "operators.h"
+#include "packed.cuh"
 #include "philox.cuh"
 
 namespace tensair {
@@ -148,29 +149,6 @@ k_adamw(const __grid_constant__ Batch<kCount> b) {
 
 // ------------------------------------------------------------------ moments in 8 bits
 constexpr int kLaneElems = kBlock / 32;  // 8
-
-// Two floats in one register pair: the packed instructions do both in one issue slot, each rounded as the single ones.
-struct Two {
-    unsigned long long bits;
-    __device__ __forceinline__ Two() {}
-    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(a), "f"(b)); }
-    __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
-    __device__ __forceinline__ float2 floats() const {
-        float2 f;
-        asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(bits));
-        return f;
-    }
-};
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-    Two r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-    return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-    Two r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
-    return r;
-}
 
 // A sum of products that are rounded first, and then the sum: by single additions, since the assembler contracts a packed
 // product and a packed sum into one operation, whatever their rounding modifiers say.

@@ -8,16 +8,24 @@
 //
 // Both are first-order linear recurrences x <- (1 - r) x + b.  Steps compose: (r, b) then (r', b') is (r + r' - r r', (1 - r') b + b').  A thread takes
 // 8 steps of a few channels and holds them in registers; the threads of a block cover more steps one after the other, the blocks of
-// a cluster still more, and a block goes on with its cluster's next stretch until the sequence ends.  Every level passes on the
-// composition of what it holds, gets the state that it begins with, and only then makes its outputs: the inputs are read once.
-// Compositions are joined in step order, so no result depends on timing.
+// a cluster still more, and a block goes on with its cluster's next stretch until the sequence ends, and then with other channels.  Every
+// level passes on the composition of what it holds, gets the state that it begins with, and only then makes its outputs: the inputs are
+// read once.  Compositions are joined in step order, so no result depends on timing.
 //
 // The gradient needs h_{t-1} again: the forward call leaves the state before every eighth step in fp32 (half a byte per element),
 // and a thread of the backward call replays its own 8 steps from there.
+//
+// Kept of a gate is n = f - 1 = -sigmoid(-gate), not f: x + n x in one fused step has the relative accuracy of n, so a gate near 1
+// remembers for as long as it should (1 - 6e-8 would be the f next to 1) and a gate of minus infinity forgets all.  Compositions keep
+// f - 1 of their product for the same reason (the product itself, rounded near 1 step after step, drifts: 20,000 steps of 1 - 8e-7
+// were off by 6e-5).  Two channels go through each instruction (packed fp32).
+//
+// The next stretch's inputs are on their way into shared memory (asynchronous copies, each thread its own) while this one's are worked on.
 #include <cooperative_groups.h>
 
 #include "columns.cuh"
 #include "layers.h"
+#include "packed.cuh"
 
 namespace tensair {
 
@@ -28,62 +36,189 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256;
 constexpr int kSteps = kMark;            // of a thread
 constexpr uint32_t kMostCluster = 16;
+constexpr uint32_t kClusterChannels = 64;      // of a block that is part of a cluster, at most
 
-// r = 1 - f = sigmoid(-gate) and e = exp(gate).  What is kept of f is r: f x = x - r x in one fused step has the relative accuracy of
-// r, so a gate near 1 remembers for as long as it should (1 - 6e-8 would be the f next to 1) and a gate of -inf forgets all.
-__device__ __forceinline__ float complement(float gate, float& e) {
-    e = expf(gate);
-    return __fdividef(1.0f, 1.0f + e);
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float decay(float rest, float x) { return fmaf(-rest, x, x); }
-// The complement of a product of two factors, from theirs.  (The product itself, rounded near 1 step after step, drifts: 20,000 steps
-// of 1 - 8e-7 were off by 6e-5.)
-__device__ __forceinline__ float join_rest(float a, float b) { return fmaf(b, 1.0f - a, a); }
+__device__ __forceinline__ float reciprocal_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float least_or_nan(float x, float y) {
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+// exp(gate), at most 2^127.9 (whose 1 - f is zero all the same).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by
+// (1.5 |gate| + 2) 2^-24 of it; half a unit of the gate's own last place is 10^4 times as much.  Gates of 32 bits: expf.
+template <typename T>
+__device__ __forceinline__ Two exp_of(Two gate) {
+    if constexpr (sizeof(T) == 2) {
+        const float2 x = (gate * Two(1.44269504f)).floats();
+        return Two(exp2_approx(least_or_nan(x.x, 127.9f)), exp2_approx(least_or_nan(x.y, 127.9f)));
+    } else {
+        const float2 x = gate.floats();
+        return Two(expf(least_or_nan(x.x, 88.6f)), expf(least_or_nan(x.y, 88.6f)));
+    }
+}
+// n = f - 1 from e = exp(gate): -1 / (1 + e)
+__device__ __forceinline__ Two complement(Two e) {
+    const float2 x = fma2(e, Two(-1.0f), Two(-1.0f)).floats();
+    return Two(reciprocal_approx(x.x), reciprocal_approx(x.y));
+}
+__device__ __forceinline__ Two decay(Two n, Two x) { return fma2(n, x, x); }
+__device__ __forceinline__ float decay(float n, float x) { return fmaf(n, x, x); }
+// f - 1 of the product of two factors, from theirs.
+__device__ __forceinline__ Two join_rest(Two a, Two b) { return fma2(b, a + Two(1.0f), a); }
+__device__ __forceinline__ float join_rest(float a, float b) { return fmaf(b, a + 1.0f, a); }
 
-// What the threads of a block pass one another: for each of its channels, the compositions of its stretches of steps.
-// [stretch][channel]; kThreads * E of each.
-template <int E>
-struct Joint {
-    float r[kThreads * E], b[kThreads * E];
-    float carry[kThreads * E], start[kThreads * E];
-    float2 ranks[2][kMostCluster][64];       // the cluster's compositions, of two turns (channels of a block that is part of a cluster: 64 at most)
-};
-
-// The state that every stretch of the block begins with, from the stretches' compositions (kBack: from the last one to the first).
-// On return `joint.r, b` hold the composition of what comes before each stretch inside the block, joint.start the state the block
-// begins with, and joint.carry the state after the cluster's whole turn.
-template <bool kBack, int E>
-__device__ __forceinline__ void join_block(Joint<E>& joint, uint32_t channels, uint32_t stretches, uint32_t cluster, uint32_t rank, uint32_t turn) {
-    __syncthreads();
-    for (uint32_t c = threadIdx.x; c < channels; c += kThreads) {
-        float rest = 0.0f, b = 0.0f;
-#pragma unroll 4
-        for (uint32_t s = 0; s < stretches; ++s) {
-            const uint32_t at = (kBack ? stretches - 1 - s : s) * channels + c;
-            const float r = joint.r[at], add = joint.b[at];
-            joint.r[at] = rest;
-            joint.b[at] = b;
-            b = decay(r, b) + add;
-            rest = join_rest(rest, r);
-        }
-        if (cluster == 1) {
-            const float carry = joint.carry[c];
-            joint.start[c] = carry;
-            joint.carry[c] = decay(rest, carry) + b;
-        } else {
-            cg::cluster_group all = cg::this_cluster();
-            for (uint32_t r = 0; r < cluster; ++r)
-                *all.map_shared_rank(&joint.ranks[turn & 1][rank][c], r) = make_float2(rest, b);
+// 8 bytes of raw elements as pairs of floats, and back.  kNegative: with their signs changed.
+template <typename T, bool kNegative>
+__device__ __forceinline__ void unpack(uint2 raw, Two (&x)[8 / sizeof(T) / 2]) {
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t sign = kNegative ? 0x80000000u : 0;
+        x[0] = Two(__uint_as_float(raw.x ^ sign), __uint_as_float(raw.y ^ sign));
+    } else {
+        const uint32_t sign = kNegative ? 0x80008000u : 0, words[2] = {raw.x ^ sign, raw.y ^ sign};
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            if constexpr (std::is_same_v<T, __nv_bfloat16>) x[p] = Two(__uint_as_float(words[p] << 16), __uint_as_float(words[p] & 0xFFFF0000u));
+            else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&words[p]));
+                x[p] = Two(f.x, f.y);
+            }
         }
     }
-    if (cluster > 1) {
+}
+template <typename T>
+__device__ __forceinline__ uint2 pack(const Two (&x)[8 / sizeof(T) / 2]) {
+    if constexpr (sizeof(T) == 4) {
+        const float2 f = x[0].floats();
+        return make_uint2(__float_as_uint(f.x), __float_as_uint(f.y));
+    } else {
+        uint32_t words[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const float2 f = x[p].floats();
+            if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+                const __nv_bfloat162 y = __floats2bfloat162_rn(f.x, f.y);
+                words[p] = *reinterpret_cast<const uint32_t*>(&y);
+            } else {
+                const __half2 y = __floats2half2_rn(f.x, f.y);
+                words[p] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+        }
+        return make_uint2(words[0], words[1]);
+    }
+}
+template <typename T, typename C>
+__device__ __forceinline__ void store_raw(T* to, uint2 raw, uint32_t left) {
+    if constexpr (!C::kRagged) *reinterpret_cast<uint2*>(to) = raw;
+    else {
+        const T* x = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+        for (int e = 0; e < C::E; ++e)
+            if (e < (int)left) to[e] = x[e];
+    }
+}
+// Into shared memory: asynchronously, where the rows allow it.
+template <typename T, typename C>
+__device__ __forceinline__ void fetch(void* to, const T* from, uint32_t left) {
+    if constexpr (!C::kRagged)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "n"(sizeof(T) * C::E) : "memory");
+    else *reinterpret_cast<Pack<T, C::E>*>(to) = load_columns<C>(from, left);
+}
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <typename T>
+__device__ __forceinline__ uint2 infinite() {      // gates that keep everything
+    if constexpr (sizeof(T) == 4) return make_uint2(0x7F800000u, 0x7F800000u);
+    else if constexpr (std::is_same_v<T, __half>) return make_uint2(0x7C007C00u, 0x7C007C00u);
+    else return make_uint2(0x7F807F80u, 0x7F807F80u);
+}
+
+// What the threads of a block pass one another: for each of its channels, the compositions of its stretches of steps, in the order
+// of the recurrence ([stretch][channel]).
+template <int E>
+struct Joint {
+    alignas(16) float n[kThreads * E];
+    alignas(16) float b[kThreads * E];
+    float carry[kThreads * E], start[kThreads * E];
+    float2 parts[kThreads];
+    float2 ranks[2][kMostCluster][kClusterChannels];       // the cluster's compositions, of two turns
+};
+
+// How a launch cuts its work: a block covers `units` pieces of channels (of all sequences, one after the other) and kThreads /
+// units stretches of kSteps steps at a time.
+struct Cut {
+    FastDiv vecs;          // pieces of channels of a sequence
+    uint32_t total;        // of all sequences
+    uint32_t units;        // power of two
+    uint32_t cluster, turns;
+    uint32_t groups;       // of `units` pieces
+};
+
+// The state that every stretch of the block begins with, from the stretches' compositions.  `place`: of the block in its cluster, in the order
+// of the recurrence.  On return joint.n, b hold the composition of what comes before each stretch inside the block, joint.start the state the block
+// begins with, and joint.carry the state after the cluster's whole turn.
+template <int E>
+__device__ __forceinline__ void join_block(Joint<E>& joint, const Cut& cut, uint32_t stretches, uint32_t place, bool odd) {
+    const uint32_t channels = cut.units * E, parts = channels < kThreads ? kThreads / channels : 1, each = stretches / parts;
+    __syncthreads();
+    // a channel's stretches are cut into parts of E (or are one part, where there are few)
+    for (uint32_t i = threadIdx.x; i < channels * parts; i += kThreads) {
+        const uint32_t c = i & (channels - 1), from = i / channels * each;
+        float n = 0.0f, b = 0.0f;
+#pragma unroll 4
+        for (uint32_t s = from; s < from + each; ++s) {
+            const float then = joint.n[s * channels + c];
+            b = decay(then, b) + joint.b[s * channels + c];
+            n = join_rest(n, then);
+        }
+        if (parts > 1) joint.parts[i] = make_float2(n, b);
+    }
+    if (parts > 1) __syncthreads();
+    for (uint32_t i = threadIdx.x; i < channels * parts; i += kThreads) {
+        const uint32_t c = i & (channels - 1), part = i / channels;
+        float n = 0.0f, b = 0.0f;
+#pragma unroll 4
+        for (uint32_t q = 0; q < part; ++q) {
+            const float2 x = joint.parts[q * channels + c];
+            b = decay(x.x, b) + x.y;
+            n = join_rest(n, x.x);
+        }
+#pragma unroll 4
+        for (uint32_t s = part * each; s < (part + 1) * each; ++s) {
+            const float then = joint.n[s * channels + c], add = joint.b[s * channels + c];
+            joint.n[s * channels + c] = n;
+            joint.b[s * channels + c] = b;
+            b = decay(then, b) + add;
+            n = join_rest(n, then);
+        }
+        if (part + 1 < parts) continue;
+        if (cut.cluster == 1) {
+            const float carry = joint.carry[c];
+            joint.start[c] = carry;
+            joint.carry[c] = decay(n, carry) + b;
+        } else {
+            cg::cluster_group all = cg::this_cluster();
+#pragma unroll 4
+            for (uint32_t r = 0; r < cut.cluster; ++r)
+                *all.map_shared_rank(&joint.ranks[odd][place][c], r) = make_float2(n, b);
+        }
+    }
+    if (cut.cluster > 1) {
         cg::this_cluster().sync();
-        for (uint32_t c = threadIdx.x; c < channels; c += kThreads) {
+        if (threadIdx.x < channels) {
+            const uint32_t c = threadIdx.x;
             float carry = joint.carry[c], start = 0.0f;
-            for (uint32_t q = 0; q < cluster; ++q) {
-                const uint32_t r = kBack ? cluster - 1 - q : q;
-                if (r == rank) start = carry;
-                const float2 x = joint.ranks[turn & 1][r][c];
+#pragma unroll 4
+            for (uint32_t q = 0; q < cut.cluster; ++q) {
+                if (q == place) start = carry;
+                const float2 x = joint.ranks[odd][q][c];
                 carry = decay(x.x, carry) + x.y;
             }
             joint.start[c] = start;
@@ -93,188 +228,219 @@ __device__ __forceinline__ void join_block(Joint<E>& joint, uint32_t channels, u
     __syncthreads();
 }
 
-// How a launch cuts its work: a block covers `units` pieces of channels (of all sequences, one after the other) and kThreads /
-// units stretches of kSteps steps.
-struct Cut {
-    FastDiv vecs;          // pieces of channels of a sequence
-    uint32_t total;        // of all sequences
-    uint32_t units;        // power of two
-    uint32_t cluster;
-    uint32_t turns;
+// A thread's place in a group of channels.
+struct Piece {
+    uint32_t s, col, left, length;      // sequence, first channel, channels from there on, steps that count
+    bool mine;
 };
-
-template <typename T, typename C>
-__global__ void __launch_bounds__(kThreads)
-k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ Cut cut) {
-    constexpr int E = C::E;
-    __shared__ Joint<E> joint;
-    const uint32_t u = threadIdx.x & (cut.units - 1), stretch = threadIdx.x / cut.units, stretches = kThreads / cut.units;
-    const uint32_t rank = blockIdx.x % cut.cluster, unit = blockIdx.x / cut.cluster * cut.units + u;
-    const uint32_t channels = cut.units * E;
-    const bool mine = unit < cut.total;
-    const uint32_t s = mine ? cut.vecs.div(unit) : 0, col = mine ? (unit - s * cut.vecs.divisor) * E : 0, left = a.d - col;
-    uint32_t length = mine ? a.T : 0;
-    if (mine && a.lengths) {
-        const int32_t n = a.lengths[s];
-        length = n < 0 ? 0 : (uint32_t)n < a.T ? (uint32_t)n : a.T;
+template <int E>
+__device__ __forceinline__ Piece piece_of(const RecurrenceArgs& a, const Cut& cut, uint32_t group) {
+    Piece p;
+    const uint32_t unit = group * cut.units + (threadIdx.x & (cut.units - 1));
+    p.mine = group < cut.groups && unit < cut.total;
+    p.s = p.mine ? cut.vecs.div(unit) : 0;
+    p.col = p.mine ? (unit - p.s * cut.vecs.divisor) * E : 0;
+    p.left = a.d - p.col;
+    p.length = p.mine ? a.T : 0;
+    if (p.mine && a.lengths) {
+        const int32_t n = a.lengths[p.s];
+        p.length = n < 0 ? 0 : (uint32_t)n < a.T ? (uint32_t)n : a.T;
     }
-    const T* gate = (const T*)a.gate.data + s * a.gate.batch + col;
-    const T* value = (const T*)a.value.data + s * a.value.batch + col;
-    T* out = (T*)a.out.data + s * a.out.batch + col;
-    const uint64_t row = (uint64_t)s * a.d + col;
-    if (stretch == 0) {
-        Pack<float, E> first = {};
-#pragma unroll
-        for (int e = 0; e < E; ++e) joint.carry[u * E + e] = mine && a.state && (!C::kRagged || e < (int)left) ? a.state[row + e] : 0.0f;
-    }
-    if (cut.cluster > 1) cg::this_cluster().sync();      // no block writes into another's memory before that one has started
-    const uint32_t marks = (a.T + kMark - 1) / kMark;
-    for (uint32_t turn = 0; turn < cut.turns; ++turn) {
-        const uint64_t t64 = ((uint64_t)(turn * cut.cluster + rank) * stretches + stretch) * kSteps;
-        const uint32_t t0 = t64 < a.T ? (uint32_t)t64 : a.T;
-        Pack<T, E> rg[kSteps] = {}, rv[kSteps] = {};
-#pragma unroll
-        for (int l = 0; l < kSteps; ++l)
-            if (t0 + l < length) {
-                rg[l] = load_columns<C>(gate + (t0 + l) * a.gate.step, left);
-                rv[l] = load_columns<C>(value + (t0 + l) * a.value.step, left);
-            }
-        // the stretch's composition: h <- (1 - r) h + b
-        float rest[kSteps][E], r[E], b[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) r[e] = b[e] = 0.0f;
-#pragma unroll
-        for (int l = 0; l < kSteps; ++l)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                float exp_gate;
-                rest[l][e] = t0 + l < length ? complement(to_float(rg[l].v[e]), exp_gate) : 0.0f;     // padding: h stays
-                r[e] = join_rest(r[e], rest[l][e]);
-                b[e] = fmaf(rest[l][e], to_float(rv[l].v[e]), decay(rest[l][e], b[e]));
-            }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            joint.r[stretch * channels + u * E + e] = r[e];
-            joint.b[stretch * channels + u * E + e] = b[e];
-        }
-        join_block<false, E>(joint, channels, stretches, cut.cluster, rank, turn);
-        float h[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            h[e] = decay(joint.r[stretch * channels + u * E + e], joint.start[u * E + e]) + joint.b[stretch * channels + u * E + e];
-        __syncthreads();
-        if (!mine || t0 >= a.T) continue;
-        if (a.marks) store_columns<C>(a.marks + ((uint64_t)s * marks + t0 / kMark) * a.d + col, h, left);
-#pragma unroll
-        for (int l = 0; l < kSteps; ++l) {
-            if (t0 + l >= a.T) break;
-            float y[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                h[e] = fmaf(rest[l][e], to_float(rv[l].v[e]), decay(rest[l][e], h[e]));
-                y[e] = t0 + l < length ? h[e] : 0.0f;
-            }
-            store_columns<C>(out + (t0 + l) * a.out.step, y, left);
-        }
-    }
-    if (a.last && mine && rank == 0 && stretch == 0)
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (!C::kRagged || e < (int)left) a.last[row + e] = joint.carry[u * E + e];
+    return p;
+}
+// The first of the thread's steps in a turn.
+__device__ __forceinline__ uint32_t first_step(const RecurrenceArgs& a, const Cut& cut, uint32_t turn, uint32_t rank) {
+    const uint64_t t = ((uint64_t)(turn * cut.cluster + rank) * (kThreads / cut.units) + threadIdx.x / cut.units) * kSteps;
+    return t < a.T ? (uint32_t)t : a.T;
 }
 
-template <typename T, typename C>
-__global__ void __launch_bounds__(kThreads)
-k_recurrence_gradient(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ Cut cut) {
-    constexpr int E = C::E;
-    __shared__ Joint<E> joint;
+// kBack: the gradient, from the last step to the first.  The data of a thread's steps in shared memory: [gate, value, (gradient)][step][thread].
+template <typename T, typename C, bool kBack>
+__global__ void __launch_bounds__(kThreads, 2)
+k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ Cut cut) {
+    constexpr int E = C::E, P = E / 2, kRows = (kBack ? 3 : 2) * kSteps;
+    extern __shared__ __align__(16) unsigned char memory[];
+    Joint<E>& joint = *reinterpret_cast<Joint<E>*>(memory);
+    uint2* rows = reinterpret_cast<uint2*>(memory + (sizeof(Joint<E>) + 15) / 16 * 16) + threadIdx.x;
+    float* mark = reinterpret_cast<float*>(memory + (sizeof(Joint<E>) + 15) / 16 * 16 + kRows * kThreads * 8) + threadIdx.x * E;
     const uint32_t u = threadIdx.x & (cut.units - 1), stretch = threadIdx.x / cut.units, stretches = kThreads / cut.units;
-    const uint32_t rank = blockIdx.x % cut.cluster, unit = blockIdx.x / cut.cluster * cut.units + u;
-    const uint32_t channels = cut.units * E;
-    const bool mine = unit < cut.total;
-    const uint32_t s = mine ? cut.vecs.div(unit) : 0, col = mine ? (unit - s * cut.vecs.divisor) * E : 0, left = a.d - col;
-    uint32_t length = mine ? a.T : 0;
-    if (mine && a.lengths) {
-        const int32_t n = a.lengths[s];
-        length = n < 0 ? 0 : (uint32_t)n < a.T ? (uint32_t)n : a.T;
-    }
-    const T* gate = (const T*)a.gate.data + s * a.gate.batch + col;
-    const T* value = (const T*)a.value.data + s * a.value.batch + col;
-    const T* grad = (const T*)a.out.data + s * a.out.batch + col;
-    T* dgate = (T*)a.dgate.data + s * a.dgate.batch + col;
-    T* dvalue = (T*)a.dvalue.data + s * a.dvalue.batch + col;
-    const uint64_t row = (uint64_t)s * a.d + col;
-    if (stretch == 0) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) joint.carry[u * E + e] = mine && a.state && (!C::kRagged || e < (int)left) ? a.state[row + e] : 0.0f;
-    }
-    if (cut.cluster > 1) cg::this_cluster().sync();
+    const uint32_t channels = cut.units * E, rank = blockIdx.x % cut.cluster;
+    const uint32_t at = (kBack ? stretches - 1 - stretch : stretch) * channels + u * E;      // in joint.n and b
     const uint32_t marks = (a.T + kMark - 1) / kMark;
-    for (uint32_t turn = cut.turns; turn-- > 0;) {
-        const uint64_t t64 = ((uint64_t)(turn * cut.cluster + rank) * stretches + stretch) * kSteps;
-        const uint32_t t0 = t64 < a.T ? (uint32_t)t64 : a.T;
-        Pack<T, E> rg[kSteps] = {}, rv[kSteps] = {}, rd[kSteps] = {};
-        Pack<float, E> mark = {};
-        if (t0 < length) mark = load_columns<C>(a.marks + ((uint64_t)s * marks + t0 / kMark) * a.d + col, left);
+
+    // asks for a turn's data
+    auto ask = [&](const Piece& p, uint32_t turn) {
+        const uint32_t t0 = first_step(a, cut, turn, rank);
+        const uint32_t live = t0 < p.length ? p.length - t0 : 0;
+        const T* gate = (const T*)a.gate.data + p.s * a.gate.batch + t0 * a.gate.step + p.col;
+        const T* value = (const T*)a.value.data + p.s * a.value.batch + t0 * a.value.step + p.col;
+        const T* grad = kBack ? (const T*)a.out.data + p.s * a.out.batch + t0 * a.out.step + p.col : nullptr;
 #pragma unroll
-        for (int l = 0; l < kSteps; ++l)
-            if (t0 + l < length) {
-                rg[l] = load_columns<C>(gate + (t0 + l) * a.gate.step, left);
-                rv[l] = load_columns<C>(value + (t0 + l) * a.value.step, left);
-                rd[l] = load_columns<C>(grad + (t0 + l) * a.out.step, left);
+        for (int l = 0; l < kSteps; ++l) {
+            if (l < live) {
+                fetch<T, C>(rows + l * kThreads, gate + l * a.gate.step, p.left);
+                fetch<T, C>(rows + (kSteps + l) * kThreads, value + l * a.value.step, p.left);
+                if (kBack) fetch<T, C>(rows + (2 * kSteps + l) * kThreads, grad + l * a.out.step, p.left);
+            } else {
+                rows[l * kThreads] = infinite<T>();
+                rows[(kSteps + l) * kThreads] = make_uint2(0, 0);
+                if (kBack) rows[(2 * kSteps + l) * kThreads] = make_uint2(0, 0);
             }
-        // r = 1 - f and f r (h_{t-1} - v_t) of every step, h from the mark on
-        float rest[kSteps][E], slope[kSteps][E], h[E], r[E], b[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) h[e] = mark.v[e], r[e] = b[e] = 0.0f;
-#pragma unroll
-        for (int l = 0; l < kSteps; ++l)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float g = to_float(rg[l].v[e]), v = to_float(rv[l].v[e]);
-                float exp_gate;
-                const float now = complement(g, exp_gate), f = g < 0.0f ? exp_gate * now : 1.0f - now;
-                rest[l][e] = t0 + l < length ? now : 0.0f;
-                slope[l][e] = t0 + l < length ? f * now * (h[e] - v) : 0.0f;
-                h[e] = fmaf(now, v, decay(now, h[e]));
-            }
-#pragma unroll
-        for (int l = kSteps - 1; l >= 0; --l)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                r[e] = join_rest(r[e], rest[l][e]);
-                b[e] = decay(rest[l][e], b[e] + to_float(rd[l].v[e]));      // padding: the gradient passes, none is added
-            }
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            joint.r[stretch * channels + u * E + e] = r[e];
-            joint.b[stretch * channels + u * E + e] = b[e];
         }
-        join_block<true, E>(joint, channels, stretches, cut.cluster, rank, turn);
+        if (kBack) {
+            const float* from = a.marks + ((uint64_t)p.s * marks + t0 / kMark) * a.d + p.col;
+            if (live) fetch<float, C>(mark, from, p.left);
+            else
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            b[e] = decay(joint.r[stretch * channels + u * E + e], joint.start[u * E + e]) + joint.b[stretch * channels + u * E + e];
+                for (int e = 0; e < E; ++e) mark[e] = 0.0f;
+        }
+    };
+    // the state that a group begins with, by the threads of the first stretch
+    auto first_state = [&](const Piece& p) {
+        Pack<float, E> x = {};
+        if (stretch == 0 && p.mine && a.state) x = load_columns<Columns<E, true>>(a.state + (uint64_t)p.s * a.d + p.col, p.left);
+        return x;
+    };
+
+    uint32_t group = blockIdx.x / cut.cluster;
+    const uint32_t clusters = gridDim.x / cut.cluster;
+    Piece piece = piece_of<E>(a, cut, group);
+    Pack<float, E> first = first_state(piece);
+    ask(piece, kBack ? cut.turns - 1 : 0);
+    if (cut.cluster > 1) cg::this_cluster().sync();      // no block writes into another's memory before that one has started
+    bool odd = false;
+    for (uint32_t done = 0; group < cut.groups; odd = !odd) {
+        const uint32_t turn = kBack ? cut.turns - 1 - done : done;
+        const Piece now = piece;
+        if (done == 0 && stretch == 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) joint.carry[u * E + e] = first.v[e];
+        }
+        fetched();
+        Two n[kSteps][P], slope[kBack ? kSteps : 1][P], all_n[P], all_b[P];
+        uint2 other[kSteps];      // values; backward: gradients
+#pragma unroll
+        for (int p = 0; p < P; ++p) all_n[p] = all_b[p] = Two(0.0f);
+        if constexpr (!kBack) {
+#pragma unroll
+            for (int l = 0; l < kSteps; ++l) {
+                Two gate[P], v[P];
+                unpack<T, false>(rows[l * kThreads], gate);
+                other[l] = rows[(kSteps + l) * kThreads];
+                unpack<T, true>(other[l], v);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    n[l][p] = complement(exp_of<T>(gate[p]));
+                    all_n[p] = join_rest(all_n[p], n[l][p]);
+                    all_b[p] = fma2(n[l][p], v[p], decay(n[l][p], all_b[p]));
+                }
+            }
+        } else {
+            Two h[P];
+#pragma unroll
+            for (int p = 0; p < P; ++p) h[p] = Two(mark[2 * p], mark[2 * p + 1]);
+#pragma unroll
+            for (int l = 0; l < kSteps; ++l) {
+                Two gate[P], v[P];
+                unpack<T, false>(rows[l * kThreads], gate);
+                unpack<T, true>(rows[(kSteps + l) * kThreads], v);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const Two e = exp_of<T>(gate[p]);
+                    n[l][p] = complement(e);
+                    slope[l][p] = (e * n[l][p]) * n[l][p] * (h[p] + v[p]);      // (-f) (-(1 - f)) (h - v)
+                    h[p] = fma2(n[l][p], v[p], decay(n[l][p], h[p]));
+                }
+                other[l] = rows[(2 * kSteps + l) * kThreads];
+            }
+#pragma unroll
+            for (int l = kSteps - 1; l >= 0; --l) {
+                Two dh[P];
+                unpack<T, false>(other[l], dh);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    all_n[p] = join_rest(all_n[p], n[l][p]);
+                    all_b[p] = decay(n[l][p], all_b[p] + dh[p]);      // padding: the gradient passes, none is added
+                }
+            }
+        }
+        // the next turn's data, of this group or of the next
+        if (++done == cut.turns) {
+            done = 0;
+            group += clusters;
+            piece = piece_of<E>(a, cut, group);
+            first = first_state(piece);
+        }
+        if (group < cut.groups) ask(piece, kBack ? cut.turns - 1 - done : done);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            *reinterpret_cast<float2*>(&joint.n[at + 2 * p]) = all_n[p].floats();
+            *reinterpret_cast<float2*>(&joint.b[at + 2 * p]) = all_b[p].floats();
+        }
+        join_block<E>(joint, cut, stretches, kBack ? cut.cluster - 1 - rank : rank, odd);
+        Two x[P];      // the state before the thread's steps; backward: its gradient behind them
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const float2 then_n = *reinterpret_cast<const float2*>(&joint.n[at + 2 * p]), then_b = *reinterpret_cast<const float2*>(&joint.b[at + 2 * p]);
+            x[p] = decay(Two(then_n.x, then_n.y), Two(joint.start[u * E + 2 * p], joint.start[u * E + 2 * p + 1])) + Two(then_b.x, then_b.y);
+        }
         __syncthreads();
-        if (!mine || t0 >= a.T) continue;
+        const uint32_t t0 = first_step(a, cut, turn, rank);
+        if (now.mine && t0 < a.T) {
+            if constexpr (!kBack) {
+                T* out = (T*)a.out.data + now.s * a.out.batch + t0 * a.out.step + now.col;
+                if (a.marks) {
+                    float y[E];
 #pragma unroll
-        for (int l = kSteps - 1; l >= 0; --l) {
-            if (t0 + l >= a.T) continue;
-            float dg[E], dv[E];
+                    for (int p = 0; p < P; ++p) {
+                        const float2 f = x[p].floats();
+                        y[2 * p] = f.x;
+                        y[2 * p + 1] = f.y;
+                    }
+                    store_columns<C>(a.marks + ((uint64_t)now.s * marks + t0 / kMark) * a.d + now.col, y, now.left);
+                }
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float D = to_float(rd[l].v[e]) + b[e];
-                b[e] = decay(rest[l][e], D);
-                dg[e] = slope[l][e] * D;
-                dv[e] = rest[l][e] * D;
+                for (int l = 0; l < kSteps; ++l) {
+                    Two v[P];
+                    unpack<T, true>(other[l], v);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) x[p] = fma2(n[l][p], v[p], decay(n[l][p], x[p]));
+                    uint2 raw = pack<T>(x);
+                    if (t0 + l >= now.length) raw = make_uint2(0, 0);
+                    if (t0 + l < a.T) store_raw<T, C>(out + l * a.out.step, raw, now.left);
+                }
+            } else {
+                T* dgate = (T*)a.dgate.data + now.s * a.dgate.batch + t0 * a.dgate.step + now.col;
+                T* dvalue = (T*)a.dvalue.data + now.s * a.dvalue.batch + t0 * a.dvalue.step + now.col;
+#pragma unroll
+                for (int l = kSteps - 1; l >= 0; --l) {
+                    Two dh[P], dg[P], dv[P];
+                    unpack<T, false>(other[l], dh);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const Two D = dh[p] + x[p];
+                        x[p] = decay(n[l][p], D);
+                        dg[p] = slope[l][p] * D;
+                        dv[p] = n[l][p] * D;      // the sign is changed below
+                    }
+                    uint2 g = pack<T>(dg), v = pack<T>(dv);
+                    constexpr uint32_t sign = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+                    v.x ^= sign;
+                    v.y ^= sign;
+                    if (t0 + l >= now.length) g = v = make_uint2(0, 0);
+                    if (t0 + l < a.T) {
+                        store_raw<T, C>(dgate + l * a.dgate.step, g, now.left);
+                        store_raw<T, C>(dvalue + l * a.dvalue.step, v, now.left);
+                    }
+                }
             }
-            store_columns<C>(dgate + (t0 + l) * a.dgate.step, dg, left);
-            store_columns<C>(dvalue + (t0 + l) * a.dvalue.step, dv, left);
         }
-    }
-    if (a.last && mine && rank == 0 && stretch == 0)
+        // after a group's last turn: joint.carry is written again behind the next barrier
+        if (done == 0 && a.last && now.mine && rank == 0 && stretch == 0)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (!C::kRagged || e < (int)left) a.last[row + e] = joint.carry[u * E + e];
+            for (int e = 0; e < E; ++e)
+                if (!C::kRagged || e < (int)now.left) a.last[(uint64_t)now.s * a.d + now.col + e] = joint.carry[u * E + e];
+    }
 }
 
 // One step, for serving: a thread per piece of channels.
@@ -288,14 +454,13 @@ k_recurrence_step(const __grid_constant__ RecurrenceArgs a, const __grid_constan
     const Pack<T, E> g = load_columns<C>((const T*)a.gate.data + s * a.gate.batch + col, left);
     const Pack<T, E> v = load_columns<C>((const T*)a.value.data + s * a.value.batch + col, left);
     const uint64_t row = (uint64_t)s * a.d + col;
-    Pack<float, E> old = {};
-    if (a.state) old = load_columns<C>(a.state + row, left);
+    const Pack<float, E> old = load_columns<C>(a.state + row, left);
     float h[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        float exp_gate;
-        const float rest = complement(to_float(g.v[e]), exp_gate);
-        h[e] = fmaf(rest, to_float(v.v[e]), decay(rest, old.v[e]));
+    for (int e = 0; e < E; e += 2) {
+        const float2 n = complement(exp_of<T>(Two(to_float(g.v[e]), to_float(g.v[e + 1])))).floats();
+        h[e] = fmaf(n.x, -to_float(v.v[e]), decay(n.x, old.v[e]));
+        h[e + 1] = fmaf(n.y, -to_float(v.v[e + 1]), decay(n.y, old.v[e + 1]));
     }
     store_columns<C>(a.last + row, h, left);
     store_columns<C>((T*)a.out.data + s * a.out.batch + col, h, left);
@@ -314,7 +479,7 @@ uint32_t piece_of(const float* p, uint32_t e) {
 }
 
 // Calls f(columns): pieces of 8 bytes, or of as many columns one by one.
-template <typename T, int E, typename F>
+template <int E, typename F>
 cudaError_t with_pieces(const RecurrenceArgs& a, bool back, F&& f) {
     uint32_t e = a.d % E ? 1 : E;
     e = piece_of(a.gate, a.type, a.T, a.B, e);
@@ -330,6 +495,8 @@ cudaError_t with_pieces(const RecurrenceArgs& a, bool back, F&& f) {
     return e == E ? f(Columns<E, false>()) : f(Columns<E, true>());
 }
 
+// Cuts the work so that the blocks that the device holds at once, two to a multiprocessor, come out even: the fewest turns of the busiest one,
+// where a turn of a cluster counts an eighth more for its barrier.
 Cut cut_of(const RecurrenceArgs& a, uint32_t e, int sms) {
     Cut c;
     c.vecs = FastDiv((a.d + e - 1) / e);
@@ -338,32 +505,45 @@ Cut cut_of(const RecurrenceArgs& a, uint32_t e, int sms) {
     uint32_t stretches = 1;
     while (stretches < 32 && stretches * kSteps < a.T) stretches *= 2;
     c.units = kThreads / stretches;
+    c.groups = (c.total + c.units - 1) / c.units;
     c.cluster = 1;
-    const uint64_t blocks = (c.total + c.units - 1) / c.units;
-    while (c.cluster < kMostCluster && blocks * c.cluster < (uint64_t)sms * 2 && (uint64_t)c.cluster * stretches * kSteps < a.T && c.units * e <= 64) c.cluster *= 2;
-    const uint64_t span = (uint64_t)c.cluster * stretches * kSteps;
-    c.turns = (uint32_t)((a.T + span - 1) / span);
+    uint64_t least = ~0ull;
+    for (uint32_t cluster = 1; cluster <= kMostCluster; cluster *= 2) {
+        const uint64_t span = (uint64_t)cluster * stretches * kSteps, turns = (a.T + span - 1) / span;
+        const uint64_t room = (uint64_t)sms * 2 / cluster, rounds = (c.groups + room - 1) / room;
+        const uint64_t cost = turns * rounds * (cluster > 1 ? 9 : 8);
+        if (cost < least) {
+            least = cost;
+            c.cluster = cluster;
+            c.turns = (uint32_t)turns;
+        }
+        if (turns == 1 || c.units * e > kClusterChannels) break;
+    }
     return c;
 }
 
-template <typename K>
-cudaError_t launch_cut(cudaStream_t stream, K kernel, const RecurrenceArgs& a, const Cut& c) {
-    const uint64_t blocks = (uint64_t)((c.total + c.units - 1) / c.units) * c.cluster;
+template <typename T, typename C, bool kBack>
+cudaError_t launch_cut(cudaStream_t stream, const RecurrenceArgs& a, int sms) {
+    const Cut c = cut_of(a, C::E, sms);
+    auto* kernel = k_recurrence<T, C, kBack>;
+    constexpr size_t shared = (sizeof(Joint<C::E>) + 15) / 16 * 16 + (kBack ? 3 : 2) * kSteps * kThreads * 8 + (kBack ? kThreads * C::E * 4 : 0);
+    static_assert(2 * (shared + 1024) <= 227 * 1024, "two blocks to a multiprocessor");
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e == cudaSuccess && c.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    uint32_t clusters = (uint32_t)sms * 2 / c.cluster;
+    if (clusters > c.groups) clusters = c.groups;
+    if (!clusters) clusters = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((uint32_t)blocks);
+    cfg.gridDim = dim3(clusters * c.cluster);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {c.cluster, 1, 1};
-    if (c.cluster > 1) {
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        if (c.cluster > 8) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-            if (e != cudaSuccess) return e;
-        }
-    }
+    cfg.attrs = attr;
+    cfg.numAttrs = c.cluster > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a, c);
 }
 
@@ -372,19 +552,14 @@ cudaError_t launch_cut(cudaStream_t stream, K kernel, const RecurrenceArgs& a, c
 cudaError_t launch_recurrence(cudaStream_t stream, const RecurrenceArgs& a, int sms) {
     return with_type(a.type, [&](auto t) {
         using T = decltype(t);
-        constexpr int E = 8 / sizeof(T);
-        return with_pieces<T, E>(a, false, [&](auto c) {
-            return launch_cut(stream, k_recurrence<T, decltype(c)>, a, cut_of(a, E, sms));
-        });
+        return with_pieces<8 / sizeof(T)>(a, false, [&](auto c) { return launch_cut<T, decltype(c), false>(stream, a, sms); });
     });
 }
 
 cudaError_t launch_recurrence_gradient(cudaStream_t stream, const RecurrenceArgs& a, int sms) {
     return with_type(a.type, [&](auto t) {
         using T = decltype(t);
-        return with_pieces<T, 2>(a, true, [&](auto c) {
-            return launch_cut(stream, k_recurrence_gradient<T, decltype(c)>, a, cut_of(a, 2, sms));
-        });
+        return with_pieces<8 / sizeof(T)>(a, true, [&](auto c) { return launch_cut<T, decltype(c), true>(stream, a, sms); });
     });
 }
 
@@ -392,7 +567,7 @@ cudaError_t launch_recurrence_step(cudaStream_t stream, const RecurrenceArgs& a)
     return with_type(a.type, [&](auto t) {
         using T = decltype(t);
         constexpr int E = 8 / sizeof(T);
-        return with_pieces<T, E>(a, false, [&](auto c) {
+        return with_pieces<E>(a, false, [&](auto c) {
             using C = decltype(c);
             const FastDiv vecs((a.d + E - 1) / E);
             const uint32_t total = a.B * vecs.divisor;

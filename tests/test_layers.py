@@ -270,6 +270,10 @@ def _run(gate, value, state, lengths, grad=None, grad_last=None):
     B_, T, d = value.shape
     g, v = gate.double(), value.double()
     f, rest = torch.sigmoid(g), torch.sigmoid(-g)
+    # 1 - f is off by 8 u of it.  Gates of 16 bits: exp(g) = 2^t with t the rounded product of g and the rounded log2(e), off by 1.5 u |t|
+    # and so 2^t by 1.5 u |t| ln 2 <= 1.5 u |g| of it, which 1 / (1 + exp(g)) passes on at most whole: 1.5 |g| u more
+    size = 8 + (1.5 * g.abs().clamp(max=90) if gate.dtype != torch.float32 else 0 * g)
+    size = torch.where(torch.isfinite(g), size, 8.0)
     live = torch.ones(B_, T, 1, dtype=torch.bool, device=value.device)
     if lengths is not None:
         live = (torch.arange(T, device=value.device)[None] < lengths[:, None])[:, :, None]
@@ -281,7 +285,7 @@ def _run(gate, value, state, lengths, grad=None, grad_last=None):
         before.append(h)
         off.append(e)
         # per step: 1 - f is off by 8 u, two fused steps round, and the compositions that join stretches round as often again
-        e = f[:, t] * e + U * (8 * rest[:, t] * (v[:, t].abs() + h.abs()) + 5 * (f[:, t] * h.abs() + rest[:, t] * v[:, t].abs()) * live[:, t])
+        e = f[:, t] * e + U * (size[:, t] * rest[:, t] * (v[:, t].abs() + h.abs()) + 5 * (f[:, t] * h.abs() + rest[:, t] * v[:, t].abs()) * live[:, t])
         h = f[:, t] * h + rest[:, t] * v[:, t]
         out.append(h * live[:, t])
         err.append(e * live[:, t])
@@ -298,20 +302,20 @@ def _run(gate, value, state, lengths, grad=None, grad_last=None):
     dh = torch.where(live, grad.double(), 0.0)
     c = torch.zeros(B_, d, dtype=torch.float64, device=value.device) if grad_last is None else grad_last.double()
     ec = U * 8 * c.abs()
-    size = c.abs()
+    bulk = c.abs()
     dg, dv, eg, ev = [], [], [], []
     for t in range(T - 1, -1, -1):
         D = dh[:, t] + c
-        big = dh[:, t].abs() + size
+        big = dh[:, t].abs() + bulk
         eD = ec + 2 * U * big * live[:, t]
         dv.append(rest[:, t] * D)
-        ev.append(rest[:, t] * (eD + 10 * U * D.abs()))
+        ev.append(rest[:, t] * (eD + (2 + size[:, t]) * U * D.abs()))
         gap = before[:, t] - v[:, t]
         slope = f[:, t] * rest[:, t] * live[:, t]
         dg.append(slope * gap * D)
-        eg.append(slope * (gap.abs() * eD + (off[:, t] + 24 * U * (before[:, t].abs() + v[:, t].abs())) * big) + 24 * U * dg[-1].abs())
-        ec = f[:, t] * eD + U * (8 * rest[:, t] + 5 * f[:, t]) * big * live[:, t]
-        c, size = f[:, t] * D, f[:, t] * big
+        eg.append(slope * (gap.abs() * eD + (off[:, t] + (8 + 2 * size[:, t]) * U * (before[:, t].abs() + v[:, t].abs())) * big) + (8 + 2 * size[:, t]) * U * dg[-1].abs())
+        ec = f[:, t] * eD + U * (size[:, t] * rest[:, t] + 5 * f[:, t]) * big * live[:, t]
+        c, bulk = f[:, t] * D, f[:, t] * big
     back = [rows(x[::-1]) for x in (dg, dv, eg, ev)]
     return back[0], back[1], c, back[2] * 1.01, back[3] * 1.01, ec * 1.01
 
