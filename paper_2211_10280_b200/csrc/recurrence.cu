@@ -18,14 +18,17 @@
 // Kept of a gate is n = f - 1 = -sigmoid(-gate), not f: x + n x in one fused step has the relative accuracy of n, so a gate near 1
 // remembers for as long as it should (1 - 6e-8 would be the f next to 1) and a gate of minus infinity forgets all.  Compositions keep
 // f - 1 of their product for the same reason (the product itself, rounded near 1 step after step, drifts: 20,000 steps of 1 - 8e-7
-// were off by 6e-5).  Two channels go through each instruction (packed fp32).
+// were off by 6e-5).
 //
 // The next stretch's inputs are on their way into shared memory (asynchronous copies, each thread its own) while this one's are worked on.
 #include <cooperative_groups.h>
 
+#include <atomic>
+#include <type_traits>
+
 #include "columns.cuh"
+#include "kernels.h"
 #include "layers.h"
-#include "packed.cuh"
 
 namespace tensair {
 
@@ -53,67 +56,54 @@ __device__ __forceinline__ float least_or_nan(float x, float y) {
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
     return z;
 }
-// exp(gate), at most 2^127.9 (whose 1 - f is zero all the same).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by
-// (1.5 |gate| + 2) 2^-24 of it; half a unit of the gate's own last place is 10^4 times as much.  Gates of 32 bits: expf.
-template <typename T>
-__device__ __forceinline__ Two exp_of(Two gate) {
+// e = exp(gate).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by (1.5 |gate| + 2) 2^-24 of it; half a unit of the
+// gate's own last place is 10^4 times as much.  Gates of 32 bits: expf.
+// kFinite: at most 2^127.9, for what is multiplied with it (1 - f is zero all the same).
+template <typename T, bool kFinite>
+__device__ __forceinline__ float exp_of(float gate) {
     if constexpr (sizeof(T) == 2) {
-        const float2 x = (gate * Two(1.44269504f)).floats();
-        return Two(exp2_approx(least_or_nan(x.x, 127.9f)), exp2_approx(least_or_nan(x.y, 127.9f)));
-    } else {
-        const float2 x = gate.floats();
-        return Two(expf(least_or_nan(x.x, 88.6f)), expf(least_or_nan(x.y, 88.6f)));
-    }
+        const float x = gate * 1.44269504f;
+        return exp2_approx(kFinite ? least_or_nan(x, 127.9f) : x);
+    } else return expf(kFinite ? least_or_nan(gate, 88.6f) : gate);
 }
 // n = f - 1 from e = exp(gate): -1 / (1 + e)
-__device__ __forceinline__ Two complement(Two e) {
-    const float2 x = fma2(e, Two(-1.0f), Two(-1.0f)).floats();
-    return Two(reciprocal_approx(x.x), reciprocal_approx(x.y));
-}
-__device__ __forceinline__ Two decay(Two n, Two x) { return fma2(n, x, x); }
+__device__ __forceinline__ float complement(float e) { return reciprocal_approx(-1.0f - e); }
 __device__ __forceinline__ float decay(float n, float x) { return fmaf(n, x, x); }
 // f - 1 of the product of two factors, from theirs.
-__device__ __forceinline__ Two join_rest(Two a, Two b) { return fma2(b, a + Two(1.0f), a); }
 __device__ __forceinline__ float join_rest(float a, float b) { return fmaf(b, a + 1.0f, a); }
 
-// 8 bytes of raw elements as pairs of floats, and back.  kNegative: with their signs changed.
-template <typename T, bool kNegative>
-__device__ __forceinline__ void unpack(uint2 raw, Two (&x)[8 / sizeof(T) / 2]) {
-    if constexpr (sizeof(T) == 4) {
-        const uint32_t sign = kNegative ? 0x80000000u : 0;
-        x[0] = Two(__uint_as_float(raw.x ^ sign), __uint_as_float(raw.y ^ sign));
-    } else {
-        const uint32_t sign = kNegative ? 0x80008000u : 0, words[2] = {raw.x ^ sign, raw.y ^ sign};
+// 8 bytes of raw elements as floats, and back.
+template <typename T>
+__device__ __forceinline__ void unpack(uint2 raw, float (&x)[8 / sizeof(T)]) {
+    const uint32_t words[2] = {raw.x, raw.y};
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            if constexpr (std::is_same_v<T, __nv_bfloat16>) x[p] = Two(__uint_as_float(words[p] << 16), __uint_as_float(words[p] & 0xFFFF0000u));
-            else {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&words[p]));
-                x[p] = Two(f.x, f.y);
-            }
+    for (int p = 0; p < 2; ++p) {
+        if constexpr (sizeof(T) == 4) x[p] = __uint_as_float(words[p]);
+        else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            x[2 * p] = __uint_as_float(words[p] << 16);
+            x[2 * p + 1] = __uint_as_float(words[p] & 0xFFFF0000u);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&words[p]));
+            x[2 * p] = f.x;
+            x[2 * p + 1] = f.y;
         }
     }
 }
 template <typename T>
-__device__ __forceinline__ uint2 pack(const Two (&x)[8 / sizeof(T) / 2]) {
-    if constexpr (sizeof(T) == 4) {
-        const float2 f = x[0].floats();
-        return make_uint2(__float_as_uint(f.x), __float_as_uint(f.y));
-    } else {
-        uint32_t words[2];
+__device__ __forceinline__ uint2 pack(const float (&x)[8 / sizeof(T)]) {
+    uint32_t words[2];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            const float2 f = x[p].floats();
-            if constexpr (std::is_same_v<T, __nv_bfloat16>) {
-                const __nv_bfloat162 y = __floats2bfloat162_rn(f.x, f.y);
-                words[p] = *reinterpret_cast<const uint32_t*>(&y);
-            } else {
-                const __half2 y = __floats2half2_rn(f.x, f.y);
-                words[p] = *reinterpret_cast<const uint32_t*>(&y);
-            }
+    for (int p = 0; p < 2; ++p) {
+        if constexpr (sizeof(T) == 4) words[p] = __float_as_uint(x[p]);
+        else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            const __nv_bfloat162 y = __floats2bfloat162_rn(x[2 * p], x[2 * p + 1]);
+            words[p] = *reinterpret_cast<const uint32_t*>(&y);
+        } else {
+            const __half2 y = __floats2half2_rn(x[2 * p], x[2 * p + 1]);
+            words[p] = *reinterpret_cast<const uint32_t*>(&y);
         }
-        return make_uint2(words[0], words[1]);
     }
+    return make_uint2(words[0], words[1]);
 }
 template <typename T, typename C>
 __device__ __forceinline__ void store_raw(T* to, uint2 raw, uint32_t left) {
@@ -140,8 +130,9 @@ __device__ __forceinline__ uint2 infinite() {      // gates that keep everything
     else return make_uint2(0x7F807F80u, 0x7F807F80u);
 }
 
-// Between the blocks of a cluster: values are sent straight into another block's memory, where a barrier counts their bytes.  (With the
-// cluster's own barrier, which also waits for every store of the turn before, a turn of 16 blocks took 8.7 us instead of 3.)
+// Between the blocks of a cluster: compositions are stored straight from registers into the others' shared memory, where a barrier counts
+// their bytes.  (us of a turn of 16 blocks, two to a multiprocessor: 3.5; with the cluster's own barrier, which also waits for every store of the turn
+// before, 4.4; by one copy to a block out of shared memory, behind the fence that needs, 4.1.)
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void start_barrier(uint64_t* barrier) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(barrier)) : "memory");
@@ -149,11 +140,12 @@ __device__ __forceinline__ void start_barrier(uint64_t* barrier) {
 __device__ __forceinline__ void expect_bytes(uint64_t* barrier, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(barrier)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void send(const float2* to, const uint64_t* barrier, uint32_t rank, float2 x) {
+__device__ __forceinline__ void send(const float2* to, const uint64_t* barrier, uint32_t rank, float4 x) {
     uint32_t there, bar;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(shared_address(to)), "r"(rank));
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(shared_address(barrier)), "r"(rank));
-    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there), "f"(x.x), "f"(x.y), "r"(bar) : "memory");
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(there), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w), "r"(bar) : "memory");
 }
 // False: they did not come, after some 50 ms.
 __device__ __forceinline__ bool wait_bytes(uint64_t* barrier, uint32_t parity) {
@@ -173,7 +165,7 @@ struct Joint {
     alignas(16) float b[kThreads * E];
     float carry[kThreads * E], start[kThreads * E];
     float2 parts[kThreads];
-    float2 ranks[2][kMostCluster][kClusterChannels];       // the cluster's compositions, of two turns
+    alignas(16) float2 ranks[2][kMostCluster][kClusterChannels];       // the cluster's compositions, of two turns
     uint64_t arrived[2];                                   // barriers that count the bytes of those
 };
 
@@ -231,12 +223,17 @@ __device__ __forceinline__ void join_block(Joint<E>& joint, const Cut& cut, uint
             joint.start[c] = carry;
             joint.carry[c] = decay(n, carry) + b;
         } else {
+            // Two neighbours send both their channels, each to half of the blocks.  What is written over has been read: who sends this turn's
+            // compositions has those of the turn before, and they were sent by who had read the ones before them.
+            const float other_n = __shfl_xor_sync(__activemask(), n, 1), other_b = __shfl_xor_sync(__activemask(), b, 1);
+            const bool second = c & 1;
+            const float4 both = second ? make_float4(other_n, other_b, n, b) : make_float4(n, b, other_n, other_b);
 #pragma unroll 4
-            for (uint32_t r = 0; r < cut.cluster; ++r) send(&joint.ranks[odd][place][c], &joint.arrived[odd], r, make_float2(n, b));
+            for (uint32_t r = second ? cut.cluster / 2 : 0; r < (second ? cut.cluster : cut.cluster / 2); ++r)
+                send(&joint.ranks[odd][place][c & ~1u], &joint.arrived[odd], r, both);
         }
     }
     if (cut.cluster > 1) {
-        // What is written over has been read: who sent for the turn before had read this turn's predecessor but one.
         if (threadIdx.x == 0) expect_bytes(&joint.arrived[odd], cut.cluster * channels * 8);
         if (threadIdx.x < channels) {
             const uint32_t c = threadIdx.x;
@@ -285,7 +282,7 @@ __device__ __forceinline__ uint32_t first_step(const RecurrenceArgs& a, const Cu
 template <typename T, typename C, bool kBack>
 __global__ void __launch_bounds__(kThreads, 2)
 k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ Cut cut) {
-    constexpr int E = C::E, P = E / 2, kRows = (kBack ? 3 : 2) * kSteps;
+    constexpr int E = C::E, kRows = (kBack ? 3 : 2) * kSteps;
     extern __shared__ __align__(16) unsigned char memory[];
     Joint<E>& joint = *reinterpret_cast<Joint<E>*>(memory);
     uint2* rows = reinterpret_cast<uint2*>(memory + (sizeof(Joint<E>) + 15) / 16 * 16) + threadIdx.x;
@@ -358,50 +355,50 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
             for (int e = 0; e < E; ++e) joint.carry[u * E + e] = first.v[e];
         }
         fetched();
-        Two n[kSteps][P], slope[kBack ? kSteps : 1][P], all_n[P], all_b[P];
+        float n[kSteps][E], slope[kBack ? kSteps : 1][E], all_n[E], all_b[E];
         uint2 other[kSteps];      // values; backward: gradients
 #pragma unroll
-        for (int p = 0; p < P; ++p) all_n[p] = all_b[p] = Two(0.0f);
+        for (int e = 0; e < E; ++e) all_n[e] = all_b[e] = 0.0f;
         if constexpr (!kBack) {
 #pragma unroll
             for (int l = 0; l < kSteps; ++l) {
-                Two gate[P], v[P];
-                unpack<T, false>(rows[l * kThreads], gate);
+                float gate[E], v[E];
+                unpack<T>(rows[l * kThreads], gate);
                 other[l] = rows[(kSteps + l) * kThreads];
-                unpack<T, true>(other[l], v);
+                unpack<T>(other[l], v);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    n[l][p] = complement(exp_of<T>(gate[p]));
-                    all_n[p] = join_rest(all_n[p], n[l][p]);
-                    all_b[p] = fma2(n[l][p], v[p], decay(n[l][p], all_b[p]));
+                for (int e = 0; e < E; ++e) {
+                    n[l][e] = complement(exp_of<T, false>(gate[e]));
+                    all_n[e] = join_rest(all_n[e], n[l][e]);
+                    all_b[e] = fmaf(-n[l][e], v[e], decay(n[l][e], all_b[e]));
                 }
             }
         } else {
-            Two h[P];
+            float h[E];
 #pragma unroll
-            for (int p = 0; p < P; ++p) h[p] = Two(mark[2 * p], mark[2 * p + 1]);
+            for (int e = 0; e < E; ++e) h[e] = mark[e];
 #pragma unroll
             for (int l = 0; l < kSteps; ++l) {
-                Two gate[P], v[P];
-                unpack<T, false>(rows[l * kThreads], gate);
-                unpack<T, true>(rows[(kSteps + l) * kThreads], v);
+                float gate[E], v[E];
+                unpack<T>(rows[l * kThreads], gate);
+                unpack<T>(rows[(kSteps + l) * kThreads], v);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const Two e = exp_of<T>(gate[p]);
-                    n[l][p] = complement(e);
-                    slope[l][p] = (e * n[l][p]) * n[l][p] * (h[p] + v[p]);      // (-f) (-(1 - f)) (h - v)
-                    h[p] = fma2(n[l][p], v[p], decay(n[l][p], h[p]));
+                for (int e = 0; e < E; ++e) {
+                    const float exp_gate = exp_of<T, true>(gate[e]);
+                    n[l][e] = complement(exp_gate);
+                    slope[l][e] = (exp_gate * n[l][e]) * n[l][e] * (h[e] - v[e]);      // (-f) (-(1 - f)) (h - v)
+                    h[e] = fmaf(-n[l][e], v[e], decay(n[l][e], h[e]));
                 }
                 other[l] = rows[(2 * kSteps + l) * kThreads];
             }
 #pragma unroll
             for (int l = kSteps - 1; l >= 0; --l) {
-                Two dh[P];
-                unpack<T, false>(other[l], dh);
+                float dh[E];
+                unpack<T>(other[l], dh);
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    all_n[p] = join_rest(all_n[p], n[l][p]);
-                    all_b[p] = decay(n[l][p], all_b[p] + dh[p]);      // padding: the gradient passes, none is added
+                for (int e = 0; e < E; ++e) {
+                    all_n[e] = join_rest(all_n[e], n[l][e]);
+                    all_b[e] = decay(n[l][e], all_b[e] + dh[e]);      // padding: the gradient passes, none is added
                 }
             }
         }
@@ -413,40 +410,28 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
             first = first_state(piece);
         }
         if (group < cut.groups) ask(piece, kBack ? cut.turns - 1 - done : done);
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            *reinterpret_cast<float2*>(&joint.n[at + 2 * p]) = all_n[p].floats();
-            *reinterpret_cast<float2*>(&joint.b[at + 2 * p]) = all_b[p].floats();
-        }
+        store_pack<float, E>(&joint.n[at], all_n);
+        store_pack<float, E>(&joint.b[at], all_b);
         join_block<E>(joint, cut, stretches, kBack ? cut.cluster - 1 - rank : rank, count);
-        Two x[P];      // the state before the thread's steps; backward: its gradient behind them
+        float x[E];      // the state before the thread's steps; backward: its gradient behind them
+        {
+            const Pack<float, E> then_n = load_pack<float, E>(&joint.n[at]), then_b = load_pack<float, E>(&joint.b[at]);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const float2 then_n = *reinterpret_cast<const float2*>(&joint.n[at + 2 * p]), then_b = *reinterpret_cast<const float2*>(&joint.b[at + 2 * p]);
-            x[p] = decay(Two(then_n.x, then_n.y), Two(joint.start[u * E + 2 * p], joint.start[u * E + 2 * p + 1])) + Two(then_b.x, then_b.y);
+            for (int e = 0; e < E; ++e) x[e] = decay(then_n.v[e], joint.start[u * E + e]) + then_b.v[e];
         }
         __syncthreads();
         const uint32_t t0 = first_step(a, cut, turn, rank);
         if (now.mine && t0 < a.T) {
             if constexpr (!kBack) {
                 T* out = (T*)a.out.data + now.s * a.out.batch + t0 * a.out.step + now.col;
-                if (a.marks) {
-                    float y[E];
-#pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        const float2 f = x[p].floats();
-                        y[2 * p] = f.x;
-                        y[2 * p + 1] = f.y;
-                    }
-                    store_columns<C>(a.marks + ((uint64_t)now.s * marks + t0 / kMark) * a.d + now.col, y, now.left);
-                }
+                if (a.marks) store_columns<C>(a.marks + ((uint64_t)now.s * marks + t0 / kMark) * a.d + now.col, x, now.left);
                 const bool whole = t0 + kSteps <= now.length;
 #pragma unroll
                 for (int l = 0; l < kSteps; ++l, out += a.out.step) {
-                    Two v[P];
-                    unpack<T, true>(other[l], v);
+                    float v[E];
+                    unpack<T>(other[l], v);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) x[p] = fma2(n[l][p], v[p], decay(n[l][p], x[p]));
+                    for (int e = 0; e < E; ++e) x[e] = fmaf(-n[l][e], v[e], decay(n[l][e], x[e]));
                     uint2 raw = pack<T>(x);
                     if (!whole) {
                         if (t0 + l >= a.T) break;
@@ -460,19 +445,16 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
                 const bool whole = t0 + kSteps <= now.length;
 #pragma unroll
                 for (int l = kSteps - 1; l >= 0; --l) {
-                    Two dh[P], dg[P], dv[P];
-                    unpack<T, false>(other[l], dh);
+                    float dh[E], dg[E], dv[E];
+                    unpack<T>(other[l], dh);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        const Two D = dh[p] + x[p];
-                        x[p] = decay(n[l][p], D);
-                        dg[p] = slope[l][p] * D;
-                        dv[p] = n[l][p] * D;      // the sign is changed below
+                    for (int e = 0; e < E; ++e) {
+                        const float D = dh[e] + x[e];
+                        x[e] = decay(n[l][e], D);
+                        dg[e] = slope[l][e] * D;
+                        dv[e] = -n[l][e] * D;
                     }
                     uint2 g = pack<T>(dg), v = pack<T>(dv);
-                    constexpr uint32_t sign = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
-                    v.x ^= sign;
-                    v.y ^= sign;
                     if (!whole) {
                         if (t0 + l >= a.T) continue;
                         if (t0 + l >= now.length) g = v = make_uint2(0, 0);
@@ -504,10 +486,9 @@ k_recurrence_step(const __grid_constant__ RecurrenceArgs a, const __grid_constan
     const Pack<float, E> old = load_columns<C>(a.state + row, left);
     float h[E];
 #pragma unroll
-    for (int e = 0; e < E; e += 2) {
-        const float2 n = complement(exp_of<T>(Two(to_float(g.v[e]), to_float(g.v[e + 1])))).floats();
-        h[e] = fmaf(n.x, -to_float(v.v[e]), decay(n.x, old.v[e]));
-        h[e + 1] = fmaf(n.y, -to_float(v.v[e + 1]), decay(n.y, old.v[e + 1]));
+    for (int e = 0; e < E; ++e) {
+        const float n = complement(exp_of<T, false>(to_float(g.v[e])));
+        h[e] = fmaf(-n, to_float(v.v[e]), decay(n, old.v[e]));
     }
     store_columns<C>(a.last + row, h, left);
     store_columns<C>((T*)a.out.data + s * a.out.batch + col, h, left);
@@ -542,47 +523,84 @@ cudaError_t with_pieces(const RecurrenceArgs& a, bool back, F&& f) {
     return e == E ? f(Columns<E, false>()) : f(Columns<E, true>());
 }
 
-// Cuts the work so that the blocks that the device holds at once, two to a multiprocessor, come out even: the fewest turns of the busiest one,
-// where a turn of a cluster counts an eighth more for its barrier.
-Cut cut_of(const RecurrenceArgs& a, uint32_t e, int sms) {
-    Cut c;
-    c.vecs = FastDiv((a.d + e - 1) / e);
-    c.total = a.B * c.vecs.divisor;
-    // stretches enough for the sequence, 32 at most
-    uint32_t stretches = 1;
-    while (stretches < 32 && stretches * kSteps < a.T) stretches *= 2;
-    c.units = kThreads / stretches;
-    c.groups = (c.total + c.units - 1) / c.units;
-    c.cluster = 1;
-    uint64_t least = ~0ull;
-    for (uint32_t cluster = 1; cluster <= kMostCluster; cluster *= 2) {
-        const uint64_t span = (uint64_t)cluster * stretches * kSteps, turns = (a.T + span - 1) / span;
-        const uint64_t room = (uint64_t)sms * 2 / cluster, rounds = (c.groups + room - 1) / room;
-        const uint64_t cost = turns * rounds * (cluster > 1 ? 9 : 8);
-        if (cost < least) {
-            least = cost;
-            c.cluster = cluster;
-            c.turns = (uint32_t)turns;
+constexpr uint32_t kClusters[] = {1, 2, 4, 8, 12, 16};
+constexpr int kSizes = sizeof(kClusters) / sizeof(kClusters[0]);
+// How many clusters of each size the device holds at once, two blocks to a multiprocessor: asked for once.  (148 multiprocessors hold 71 of 4, 33 of 8,
+// 14 of 16; one more than that waits until another has ended.)
+template <typename T, typename C, bool kBack>
+cudaError_t rooms(size_t shared, int sms, uint32_t (&room)[kSizes]) {
+    auto* kernel = k_recurrence<T, C, kBack>;
+    static std::atomic<int> known[kMaxDevices][kSizes];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    for (int i = 0; i < kSizes; ++i) {
+        int n = device < kMaxDevices ? known[device][i].load(std::memory_order_relaxed) : 0;
+        if (!n) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e != cudaSuccess) return e;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(kClusters[i] * sms);
+            cfg.blockDim = dim3(kThreads);
+            cfg.dynamicSmemBytes = shared;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim = {kClusters[i], 1, 1};
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            if (n < 1) n = 1;
+            if (device < kMaxDevices) known[device][i].store(n, std::memory_order_relaxed);
         }
-        if (turns == 1 || c.units * e > kClusterChannels) break;
+        room[i] = n;
     }
-    return c;
+    return cudaSuccess;
+}
+
+// Cuts the work so that the blocks that the device holds at once come out even: the fewest turns of the busiest one, a group of channels
+// counting half a turn more, and turns in clusters by what their exchange takes.
+Cut cut_of(const RecurrenceArgs& a, uint32_t e, const uint32_t (&room)[kSizes], uint32_t* grid) {
+    Cut best;
+    uint64_t least = ~0ull;
+    uint32_t most = 1;      // stretches enough for the sequence, 32 at most
+    while (most < 32 && most * kSteps < a.T) most *= 2;
+    for (uint32_t stretches = most; stretches && stretches >= most / 2; stretches /= 2) {
+        Cut c = best;
+        c.vecs = FastDiv((a.d + e - 1) / e);
+        c.total = a.B * c.vecs.divisor;
+        c.units = kThreads / stretches;
+        c.groups = (c.total + c.units - 1) / c.units;
+        static constexpr uint32_t kTurn[kSizes] = {8, 9, 10, 11, 11, 12};
+        for (int i = 0; i < kSizes; ++i) {
+            c.cluster = kClusters[i];
+            const uint64_t span = (uint64_t)c.cluster * stretches * kSteps, turns = (a.T + span - 1) / span;
+            const uint64_t rounds = (c.groups + room[i] - 1) / room[i];
+            const uint64_t cost = rounds * (2 * turns + 1) * kTurn[i];
+            if (cost < least) {
+                least = cost;
+                c.turns = (uint32_t)turns;
+                *grid = (c.groups < room[i] ? c.groups : room[i]) * c.cluster;
+                best = c;
+            }
+            if (turns == 1 || c.units * e > kClusterChannels) break;
+        }
+    }
+    return best;
 }
 
 template <typename T, typename C, bool kBack>
 cudaError_t launch_cut(cudaStream_t stream, const RecurrenceArgs& a, int sms) {
-    const Cut c = cut_of(a, C::E, sms);
     auto* kernel = k_recurrence<T, C, kBack>;
     constexpr size_t shared = (sizeof(Joint<C::E>) + 15) / 16 * 16 + (kBack ? 3 : 2) * kSteps * kThreads * 8 + (kBack ? kThreads * C::E * 4 : 0);
     static_assert(2 * (shared + 1024) <= 227 * 1024, "two blocks to a multiprocessor");
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
-    if (e == cudaSuccess && c.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    uint32_t room[kSizes], grid = 0;
+    const cudaError_t e = rooms<T, C, kBack>(shared, sms, room);
     if (e != cudaSuccess) return e;
-    uint32_t clusters = (uint32_t)sms * 2 / c.cluster;
-    if (clusters > c.groups) clusters = c.groups;
-    if (!clusters) clusters = 1;
+    const Cut c = cut_of(a, C::E, room, &grid);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(clusters * c.cluster);
+    cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
