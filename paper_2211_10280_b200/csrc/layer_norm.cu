@@ -15,7 +15,8 @@ namespace tensair {
 namespace {
 
 constexpr int kThreads = 256;            // of blocks whose rows belong to warps or parts of them
-constexpr int kMostThreads = 1024;       // of a block that shares a row
+constexpr int kMostThreads = 512;        // of a block that shares a row
+constexpr int kWideThreads = 1024;       // of blocks for rows that do not fit into one
 
 // `E` values of a parameter vector from column `col` on.
 template <typename C>
@@ -90,7 +91,7 @@ struct Place {
 // ------------------------------------------------------------------ forward
 // K vectors of a row to a thread.
 template <typename TX, typename TY, typename C, int kGroup, int K>
-__global__ void __launch_bounds__(kGroup ? kThreads : kMostThreads)
+__global__ void __launch_bounds__(kGroup ? kThreads : kMostThreads, K < 4 ? kGroup ? 5 : 3 : kGroup ? 3 : 1)
 k_norm(const __grid_constant__ NormArgs a, uint32_t vecs) {
     constexpr int E = C::E;
     __shared__ float2 shared[kGroup ? 1 : 64];
@@ -151,7 +152,7 @@ k_norm(const __grid_constant__ NormArgs a, uint32_t vecs) {
 
 // Rows that do not fit into a block's registers: three passes, the later ones out of the level-2 cache.
 template <typename TX, typename TY, typename C>
-__global__ void __launch_bounds__(kMostThreads)
+__global__ void __launch_bounds__(kWideThreads)
 k_norm_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
     constexpr int E = C::E;
     __shared__ float2 shared[64];
@@ -159,13 +160,13 @@ k_norm_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
     const uint32_t row = blockIdx.x;
     const TX* x = (const TX*)a.x.data + (uint64_t)row * a.x.stride;
     float sum = 0.0f, square = 0.0f;
-    for (uint32_t v = threadIdx.x; v < vecs; v += kMostThreads) {
+    for (uint32_t v = threadIdx.x; v < vecs; v += kWideThreads) {
         const Pack<TX, E> raw = load_columns<C>(x + v * E, a.d - v * E);
 #pragma unroll
         for (int e = 0; e < E; ++e) sum += to_float(raw.v[e]);
     }
     const float mean = row_sum(sum) / (float)a.d;
-    for (uint32_t v = threadIdx.x; v < vecs; v += kMostThreads) {
+    for (uint32_t v = threadIdx.x; v < vecs; v += kWideThreads) {
         const Pack<TX, E> raw = load_columns<C>(x + v * E, a.d - v * E);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -179,7 +180,7 @@ k_norm_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
         a.rstd[row] = rstd;
     }
     TY* y = (TY*)a.y.data + (uint64_t)row * a.y.stride;
-    for (uint32_t v = threadIdx.x; v < vecs; v += kMostThreads) {
+    for (uint32_t v = threadIdx.x; v < vecs; v += kWideThreads) {
         const uint32_t col = v * E;
         const Pack<TX, E> raw = load_columns<C>(x + col, a.d - col);
         float w[E], b[E];
@@ -231,6 +232,18 @@ k_norm_gradient(const __grid_constant__ NormArgs a, uint32_t vecs) {
             }
         }
         const float mean = in ? a.mean[row] : 0.0f, rstd = in ? a.rstd[row] : 0.0f;
+        if (row + step < a.n) {      // the next row, into the level-2 cache
+            const TX* next_x = x + (uint64_t)step * a.x.stride;
+            const TY* next_dy = dy + (uint64_t)step * a.y.stride;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const uint32_t v = at.lane + k * at.width;
+                if (v < vecs) {
+                    prefetch(next_x + v * E);
+                    prefetch(next_dy + v * E);
+                }
+            }
+        }
         float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -291,7 +304,7 @@ k_norm_gradient(const __grid_constant__ NormArgs a, uint32_t vecs) {
 }
 
 template <typename TX, typename TY, typename C>
-__global__ void __launch_bounds__(kMostThreads)
+__global__ void __launch_bounds__(kWideThreads)
 k_norm_gradient_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
     constexpr int E = C::E;
     __shared__ float2 shared[64];
@@ -302,7 +315,7 @@ k_norm_gradient_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
     TX* dx = (TX*)a.dx.data + (uint64_t)row * a.dx.stride;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float2 sum = make_float2(0.0f, 0.0f);
-    for (uint32_t v = threadIdx.x; v < vecs; v += kMostThreads) {
+    for (uint32_t v = threadIdx.x; v < vecs; v += kWideThreads) {
         const uint32_t col = v * E;
         const Pack<TX, E> rx = load_columns<C>(x + col, a.d - col);
         const Pack<TY, E> rg = load_columns<C>(dy + col, a.d - col);
@@ -320,7 +333,7 @@ k_norm_gradient_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
     sum = row_sum(sum);
     sum.x /= (float)a.d;
     sum.y /= (float)a.d;
-    for (uint32_t v = threadIdx.x; v < vecs; v += kMostThreads) {
+    for (uint32_t v = threadIdx.x; v < vecs; v += kWideThreads) {
         const uint32_t col = v * E;
         const Pack<TX, E> rx = load_columns<C>(x + col, a.d - col);
         const Pack<TY, E> rg = load_columns<C>(dy + col, a.d - col);
@@ -334,7 +347,7 @@ k_norm_gradient_wide(const __grid_constant__ NormArgs a, uint32_t vecs) {
 
 // The sums over rows for wide rows: a thread takes a column, a block 32 of them and every gridDim.y-th row.
 template <typename TX, typename TY>
-__global__ void __launch_bounds__(kMostThreads)
+__global__ void __launch_bounds__(kWideThreads)
 k_norm_columns(const __grid_constant__ NormArgs a) {
     __shared__ float join[2][32][33];
     const uint32_t lane = threadIdx.x % 32, part = threadIdx.x / 32, col = blockIdx.x * 32 + lane;
@@ -356,7 +369,7 @@ k_norm_columns(const __grid_constant__ NormArgs a) {
 }
 
 // Adds up the blocks' partial rows: 32 columns to a block, every 32nd partial row to a warp.
-__global__ void __launch_bounds__(kMostThreads)
+__global__ void __launch_bounds__(kWideThreads)
 k_norm_join(const __grid_constant__ NormArgs a, uint32_t count) {
     __shared__ float join[32][33];
     after_previous_launch();
@@ -381,8 +394,6 @@ k_norm_join(const __grid_constant__ NormArgs a, uint32_t count) {
 template <int kGroup, int kVectors> struct Shape2 {
     static constexpr int group = kGroup, k = kVectors;
 };
-constexpr uint32_t kBlockVectors = 2;      // of a row to a thread, where a block shares it
-
 // Calls f(shape) for rows of `vecs` vectors; false: they do not fit.
 template <typename F>
 bool with_shape(uint32_t vecs, F&& f) {
@@ -390,13 +401,14 @@ bool with_shape(uint32_t vecs, F&& f) {
     else if (vecs <= 32) f(Shape2<32, 1>());
     else if (vecs <= 64) f(Shape2<32, 2>());
     else if (vecs <= 128) f(Shape2<32, 4>());
-    else if (vecs <= kMostThreads * kBlockVectors) f(Shape2<0, kBlockVectors>());
+    else if (vecs <= kMostThreads * 2) f(Shape2<0, 2>());
+    else if (vecs <= kMostThreads * 4) f(Shape2<0, 4>());
     else return false;
     return true;
 }
-uint32_t threads_of(int group, uint32_t vecs) {
+uint32_t threads_of(int group, int k, uint32_t vecs) {
     if (group) return kThreads;
-    const uint32_t t = (vecs + kBlockVectors - 1) / kBlockVectors;
+    const uint32_t t = (vecs + k - 1) / k;
     return (t + 31) / 32 * 32;
 }
 
@@ -438,10 +450,10 @@ cudaError_t launch_norm(cudaStream_t stream, const NormArgs& a) {
             const uint32_t vecs = (a.d + C::E - 1) / C::E;
             const bool fits = with_shape(vecs, [&](auto shape) {
                 using S = decltype(shape);
-                const uint32_t threads = threads_of(S::group, vecs), rows = S::group ? kThreads / S::group : 1;
+                const uint32_t threads = threads_of(S::group, S::k, vecs), rows = S::group ? kThreads / S::group : 1;
                 k_norm<TX, TY, C, S::group, S::k><<<(a.n + rows - 1) / rows, threads, 0, stream>>>(a, vecs);
             });
-            if (!fits) k_norm_wide<TX, TY, C><<<a.n, kMostThreads, 0, stream>>>(a, vecs);
+            if (!fits) k_norm_wide<TX, TY, C><<<a.n, kWideThreads, 0, stream>>>(a, vecs);
             return cudaGetLastError();
         });
     });
@@ -451,7 +463,7 @@ cudaError_t launch_norm(cudaStream_t stream, const NormArgs& a) {
 static constexpr uint32_t kNormBlocks = 148 * 2, kWideParts = 32;
 uint32_t norm_partials(uint32_t n, uint32_t d) {
     // the widest any of the ways takes for rows of d columns
-    const uint32_t most = d <= kMostThreads * kBlockVectors * 8 ? kNormBlocks : kWideParts;
+    const uint32_t most = d <= kMostThreads * 4 * 8 ? kNormBlocks : kWideParts;
     return n < most ? n : most;
 }
 
@@ -465,23 +477,23 @@ cudaError_t launch_norm_gradient(cudaStream_t stream, const NormArgs& a) {
             const uint32_t vecs = (a.d + C::E - 1) / C::E;
             const bool fits = with_shape(vecs, [&](auto shape) {
                 using S = decltype(shape);
-                const uint32_t threads = threads_of(S::group, vecs), rows = S::group ? kThreads / S::group : 1;
+                const uint32_t threads = threads_of(S::group, S::k, vecs), rows = S::group ? kThreads / S::group : 1;
                 parts = (a.n + rows - 1) / rows;
                 if (parts > kNormBlocks) parts = kNormBlocks;
                 k_norm_gradient<TX, TY, C, S::group, S::k><<<parts, threads, 0, stream>>>(a, vecs);
             });
             if (!fits) {
-                k_norm_gradient_wide<TX, TY, C><<<a.n, kMostThreads, 0, stream>>>(a, vecs);
+                k_norm_gradient_wide<TX, TY, C><<<a.n, kWideThreads, 0, stream>>>(a, vecs);
                 if (a.partials) {
                     parts = a.n < kWideParts ? a.n : kWideParts;
-                    k_norm_columns<TX, TY><<<dim3((a.d + 31) / 32, parts), kMostThreads, 0, stream>>>(a);
+                    k_norm_columns<TX, TY><<<dim3((a.d + 31) / 32, parts), kWideThreads, 0, stream>>>(a);
                 }
             }
             return cudaGetLastError();
         });
     });
     if (err != cudaSuccess || !a.partials) return err;
-    return launch_early(k_norm_join, dim3((a.d + 31) / 32, 2), kMostThreads, 0, stream, a, parts);
+    return launch_early(k_norm_join, dim3((a.d + 31) / 32, 2), kWideThreads, 0, stream, a, parts);
 }
 
 }  // namespace tensair
