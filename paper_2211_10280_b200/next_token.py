@@ -1,6 +1,6 @@
 """A small next-token model trained on from streamed word embeddings: the language-model operators used together.
 
-    python -m paper_2211_10280_b200.next_token [--steps 200] [--state-bits 8] [--dense]
+    python -m paper_2211_10280_b200.next_token [--steps 200] [--state-bits 8] [--dense | --recurrent [--generate 40]]
 
 1. A stream of token batches trains the SGNS tables (`binding.Context`), as a streaming job does.
 2. Their input rows become the embedding table of a next-token model: scaled lookup of a window of tokens, mean over the
@@ -10,6 +10,9 @@
    batch's gradient rows and touches only the rows of its tokens; the table's share of the norm is that of its touched rows
    (`Embedding.gradient_rows`, the form that a message has).  With --dense the table's whole gradient is made
    (autograd through `Embedding.__call__`) and the table is one more tensor of the AdamW step.
+With --recurrent the window is a sequence, and the model carries a state along it (`RecurrentModel`: norm, gates, recurrence, dropout and
+residual, norm); every position predicts its next token.  --generate N then draws N tokens for each of a few streams, one recurrence step at a
+time, the states updated in place.
 Nothing in a step waits for the device; the loss is read every `report` steps.
 """
 from __future__ import annotations
@@ -20,7 +23,7 @@ import math
 import numpy as np
 import torch
 
-from . import binding, operators
+from . import binding, layers, operators, sampling
 
 
 def token_stream(V: int, length: int, seed: int) -> np.ndarray:
@@ -112,13 +115,118 @@ def train(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows:
     return dict(before=before, after=table, seen=seen, losses=losses, optimizer=optimizer)
 
 
+class RecurrentModel:
+    """A recurrent block between an embedding table (V, d) and the logits of the next token:
+
+        n = norm(x),  h = recurrence(n Wg, n Wv),  y = n + dropout(h Wo),  logits = norm(y) Wl + bl
+
+    `params`: name -> float32 tensor, the weights that an optimizer updates; `half`: copies of the matrices in `dtype`, in which the
+    forward pass runs."""
+
+    MATRICES = ("gates", "out", "logits")
+
+    def __init__(self, V: int, d: int, hidden: int, dtype=torch.bfloat16, drop: float = 0.1, seed: int = 0):
+        gen = torch.Generator("cuda").manual_seed(seed)
+
+        def normal(*shape):
+            return torch.randn(shape, device="cuda", generator=gen).mul_(shape[-1] ** -0.5)
+
+        self.V, self.d, self.hidden, self.dtype, self.drop, self.seed = V, d, hidden, dtype, drop, seed
+        self.params = dict(norm=torch.ones(d, device="cuda"), shift=torch.zeros(d, device="cuda"), gates=normal(2 * hidden, d),
+                           out=normal(d, hidden), last_norm=torch.ones(d, device="cuda"), last_shift=torch.zeros(d, device="cuda"),
+                           logits=normal(V, d), bias=torch.zeros(V, device="cuda"))
+        # gates that remember for some ten steps to begin with
+        self.params["gate_bias"] = torch.cat([torch.full((hidden,), 2.0, device="cuda"), torch.zeros(hidden, device="cuda")])
+        self.half = {k: self.params[k].to(dtype) for k in self.MATRICES}
+
+    def weights(self):
+        """What the forward pass takes: the copies of the matrices, and the rest as it is, each wanting a gradient."""
+        return {k: self.half.get(k, p).detach().requires_grad_() for k, p in self.params.items()}
+
+    def block(self, x, w, call: int, state=None, lengths=None, drop=None):
+        """(y, last state) for x (B, T, d); call numbers the dropout's mask."""
+        n = layers.layer_norm(x, w["norm"], w["shift"], dtype=self.dtype)
+        gate, value = (n @ w["gates"].t() + w["gate_bias"].to(self.dtype)).chunk(2, -1)
+        h, last = layers.recurrence(gate, value, state, lengths)
+        return layers.dropout(h @ w["out"].t(), self.drop if drop is None else drop, self.seed, call, residual=n), last
+
+    def read(self, y, w):
+        """Logits of y (..., d)."""
+        return layers.layer_norm(y, w["last_norm"], w["last_shift"]) @ w["logits"].t() + w["bias"].to(self.dtype)
+
+    @torch.no_grad()
+    def step(self, x, state):
+        """Logits of the next token of B streams from their rows x (B, d); state (B, hidden) is updated in place."""
+        w = {k: self.half.get(k, p) for k, p in self.params.items()}
+        n = layers.layer_norm(x, w["norm"], w["shift"], dtype=self.dtype)
+        gate, value = (n @ w["gates"].t() + w["gate_bias"].to(self.dtype)).chunk(2, -1)
+        h = layers.recurrence_step(gate, value, state)
+        return self.read(n + h @ w["out"].t(), w)
+
+
+def train_recurrent(steps: int = 200, V: int = 5000, d: int = 64, hidden: int = 128, rows: int = 64, window: int = 32, state_bits: int = 8,
+                    lr: float = 3e-3, max_norm: float = 1.0, drop: float = 0.1, report: int = 50, quiet: bool = True):
+    """Trains a RecurrentModel on from streamed embeddings; returns the model, its table and embedding, and the reported losses."""
+    table = streamed_table(V, d)
+    model = RecurrentModel(V, d, hidden, drop=drop)
+    embedding = operators.Embedding(V, d, max_tokens=rows * window, scale=math.sqrt(d))
+    m, v, slot = torch.zeros_like(table), torch.zeros_like(table), rows_slot(min(V, rows * window), d)
+    names = list(model.params)
+    optimizer = operators.AdamW([model.params[k] for k in names], lr=lr, weight_decay=0.01, state_bits=state_bits,
+                                copies=[model.half.get(k) for k in names], decay_factors=[float(k in model.MATRICES) for k in names])
+    length = rows * window
+    stream = torch.from_numpy(token_stream(V, steps * length + 1, seed=2)).cuda()
+    losses = []
+    for step in range(1, steps + 1):
+        at = (step - 1) * length
+        ids, target = stream[at:at + length].view(rows, window), stream[at + 1:at + length + 1]
+        x = embedding.lookup(table, ids).requires_grad_()
+        w = model.weights()
+        y, _ = model.block(x, w, call=step)
+        loss = torch.nn.functional.cross_entropy(model.read(y, w).float().view(-1, V), target)
+        grads = list(torch.autograd.grad(loss, [w[k] for k in names] + [x]))
+        clip = clip_factor(grads[:-1] + [touched_rows(embedding, grads[-1], ids, slot)], max_norm)
+        optimizer.step(grads[:-1], grad_scale=clip)
+        embedding.adamw(grads[-1], ids, table, m, v, step=step, lr=lr, weight_decay=0.0, grad_scale=clip)
+        if step % report == 0 or step == 1:
+            losses.append(loss.item())
+            embedding.check()
+            if not quiet:
+                print(f"step {step:5d}  loss {losses[-1]:.4f}")
+    return dict(model=model, table=table, embedding=embedding, losses=losses)
+
+
+@torch.no_grad()
+def generate(model: RecurrentModel, table, embedding, first, count: int, temperature=0.8, top_k=50, top_p=0.95, min_p=0.0, seed: int = 0):
+    """`count` tokens for each of the streams that begin with the tokens `first` (int64), drawn one after the other: (B, count)."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    uniform = torch.rand(count, first.numel(), device="cuda", generator=gen)
+    state = torch.zeros(first.numel(), model.hidden, device="cuda")
+    tokens = torch.empty(count, first.numel(), dtype=torch.int64, device="cuda")
+    ids = first
+    for i in range(count):
+        logits = model.step(embedding.lookup(table, ids), state)
+        ids = sampling.sample(logits, uniform[i], temperature, top_k, top_p, min_p, out=tokens[i])
+    return tokens.t()
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=8)
     ap.add_argument("--dense", action="store_true")
+    ap.add_argument("--recurrent", action="store_true")
+    ap.add_argument("--generate", type=int, default=0, metavar="N")
     a = ap.parse_args()
-    train(a.steps, state_bits=a.state_bits, dense=a.dense, quiet=False)
+    if a.generate and not a.recurrent:
+        ap.error("--generate goes with --recurrent")
+    if not a.recurrent:
+        train(a.steps, state_bits=a.state_bits, dense=a.dense, quiet=False)
+        return
+    r = train_recurrent(a.steps, state_bits=a.state_bits, quiet=False)
+    if a.generate:
+        for row in generate(r["model"], r["table"], r["embedding"], torch.arange(4, device="cuda"), a.generate).tolist():
+            print(*row)
 
 
 if __name__ == "__main__":

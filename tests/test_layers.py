@@ -547,6 +547,84 @@ def test_a_backward_pass_is_captured():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+# ---------------------------------------------------------------- together
+def _plain_block(model, x, w, kept, lengths):
+    """The model's block and logits in 64 bits, elementary operations alone."""
+    def norm(x, weight, bias):
+        c = x - x.mean(-1, keepdim=True)
+        return c / ((c * c).mean(-1, keepdim=True) + 1e-5) ** 0.5 * weight + bias
+
+    n = norm(x, w["norm"], w["shift"])
+    gate, value = (n @ w["gates"].t() + w["gate_bias"]).chunk(2, -1)
+    f, h, out = torch.sigmoid(gate), torch.zeros_like(gate[:, 0]), []
+    live = (torch.arange(x.shape[1], device="cuda")[None] < lengths[:, None])[:, :, None].double()
+    for t in range(x.shape[1]):
+        h = torch.where(live[:, t] > 0, f[:, t] * h + (1 - f[:, t]) * value[:, t], h)
+        out.append(h * live[:, t])
+    y = n + torch.where(kept, (torch.stack(out, 1) @ w["out"].t()) / (1 - model.drop), 0.0)
+    return norm(y, w["last_norm"], w["last_shift"]) @ w["logits"].t() + w["bias"]
+
+
+@gpu
+def test_the_recurrent_model_has_the_gradients_of_its_formula():
+    from paper_2211_10280_b200.next_token import RecurrentModel
+
+    B_, T, V, d, hidden = 3, 41, 50, 24, 20
+    model = RecurrentModel(V, d, hidden, dtype=F32, drop=0.25, seed=5)
+    lengths = torch.tensor([41, 7, 30], dtype=torch.int32, device="cuda")
+    x, weigh = _rand((B_, T, d), seed=1).requires_grad_(), _rand((B_, T, V), seed=2)
+    w = model.weights()
+    y, _ = model.block(x, w, call=3, lengths=lengths)
+    logits = model.read(y, w)
+    got = torch.autograd.grad((logits * weigh).sum(), [x] + list(w.values()))
+    kept = _kept(B_ * T * d, 0.25, 3, 5).view(B_, T, d)
+    x64, w64 = x.detach().double().requires_grad_(), {k: p.detach().double().requires_grad_() for k, p in w.items()}
+    plain = _plain_block(model, x64, w64, kept, lengths)
+    want = torch.autograd.grad((plain * weigh.double()).sum(), [x64] + list(w64.values()))
+    # chains of some 300 roundings (T steps, products of 50 terms) of sums whose parts do not cancel by more than ten: 300 * 10 u
+    assert (logits.double() - plain).norm() <= 3e3 * U * plain.norm()
+    for a, b in zip(got, want):
+        assert (a.double() - b).norm() <= 3e3 * U * b.norm(), (a.shape, ((a.double() - b).norm() / b.norm()).item())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_generation_goes_the_way_of_the_sequence(dtype):
+    from paper_2211_10280_b200 import next_token, operators
+
+    V, d, hidden, count = 300, 32, 24, 12
+    model = next_token.RecurrentModel(V, d, hidden, dtype=dtype)
+    table = _rand((V, d), seed=1)
+    e = operators.Embedding(V, d, max_tokens=64, scale=d ** 0.5)
+    first = torch.tensor([5, 17, 299], device="cuda")
+    for temperature, top_k in ((0.0, 0), (0.8, 20)):
+        got = next_token.generate(model, table, e, first, count, temperature=temperature, top_k=top_k, seed=4)
+        assert got.shape == (3, count) and ((got >= 0) & (got < V)).all()
+        assert torch.equal(got, next_token.generate(model, table, e, first, count, temperature=temperature, top_k=top_k, seed=4))
+    # greedy: each token is the largest logit of the whole sequence's pass, or one that rounding (of 16 bits: a few 2^-8 of the logits) cannot tell from it
+    got = next_token.generate(model, table, e, first, count, temperature=0.0)
+    ids = torch.cat([first[:, None], got[:, :-1]], 1)
+    with torch.no_grad():
+        w = {k: model.half.get(k, p) for k, p in model.params.items()}
+        y, _ = model.block(e.lookup(table, ids), w, call=0, drop=0.0)
+        logits = model.read(y, w).float()
+    chosen = logits.gather(2, got[:, :, None])[..., 0]
+    size = logits.abs().amax()
+    assert (logits.amax(2) - chosen <= (1e-5 if dtype == F32 else 0.05) * size).all()
+
+
+@gpu
+@pytest.mark.parametrize("state_bits", [8, 32])
+def test_the_recurrent_example_runs(state_bits):
+    from paper_2211_10280_b200 import next_token
+
+    r = next_token.train_recurrent(steps=6, V=500, d=32, hidden=48, rows=16, window=20, state_bits=state_bits, report=3)
+    assert len(r["losses"]) == 3 and all(np.isfinite(r["losses"]))
+    assert all(torch.isfinite(p).all() for p in r["model"].params.values()) and torch.isfinite(r["table"]).all()
+    out = next_token.generate(r["model"], r["table"], r["embedding"], torch.arange(4, device="cuda"), 5)
+    assert out.shape == (4, 5) and ((out >= 0) & (out < 500)).all()
+
+
 # ---------------------------------------------------------------- refusals
 def _norm_call(gradient=False, **change):
     h = B.Norm(weight=4096, bias=4096, mean=4096, rstd=4096, n=10, param_type=B.FLOAT32, eps=1e-5)
