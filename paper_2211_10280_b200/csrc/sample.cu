@@ -14,9 +14,11 @@
 // asked for.  (Slices that do not fit are read again, out of the level-2 cache.)
 #include <cooperative_groups.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "columns.cuh"
+#include "kernels.h"
 #include "layers.h"
 
 namespace tensair {
@@ -467,6 +469,7 @@ __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
             // few lanes have any, and few of them more than one: read again rather than picked from registers
             for (uint32_t to = at + upto - own; mine; mine &= mine - 1, ++to) {
                 const uint32_t id = place + __ffs(mine) - 1;
+                if (!in_bounds(nullptr, to, kList)) break;
                 logits[to] = slice.logits[id];
                 ids[to] = slice.begin + id;
             }
@@ -505,6 +508,7 @@ __device__ Border find_border(Shared& sh, const Slice<T>& slice, const Team& tea
         const uint32_t which = turn & 1;
         ++turn;
         auto add = [&](float x, uint32_t b, uint32_t times) {
+            if (!in_bounds(nullptr, b, kBuckets)) return;
             if (kByMass) {
                 const mass_t m = weights.of(x) * times;
                 if (!m) return;
@@ -874,10 +878,16 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
         const bool staged = bytes <= kStage;
         const bool whole = (uintptr_t)a.logits.data % 16 == 0 && (a.n < 2 || a.logits.stride % E == 0);
         auto* kernel = k_sample<T>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-        if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        static std::atomic<bool> prepared[kMaxDevices];      // the kernel's attributes, once for each device
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
         if (e != cudaSuccess) return e;
+        if (device >= kMaxDevices || !prepared[device].load(std::memory_order_relaxed)) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e != cudaSuccess) return e;
+            if (device < kMaxDevices) prepared[device].store(true, std::memory_order_relaxed);
+        }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(a.n * cluster);
         cfg.blockDim = dim3(kThreads);

@@ -57,13 +57,14 @@ def _rows(x, n, d):
     return B.Rows(x.data_ptr(), x.stride(0) if n > 1 else d, d, _FLOATS[x.dtype])
 
 
-def _norm_of(weight, bias, mean, rstd, n, eps, index):
-    d = weight.shape[0] if weight.dim() == 1 else 0
+def _norm_of(weight, bias, mean, rstd, n, d, eps, index):
     kind = _FLOATS.get(weight.dtype)
-    for x in (weight,) if bias is None else (weight, bias):
-        if x.shape != (d,) or kind is None or x.dtype != weight.dtype or x.get_device() != index or not x.is_contiguous():
-            raise ValueError(f"weight and bias: contiguous (d,) of one type, float32, bfloat16 or float16, on the rows' device; "
-                             f"got {tuple(x.shape)} of {x.dtype} on {x.device}")
+    if (kind is None or weight.dim() != 1 or weight.get_device() != index or not weight.is_contiguous()
+            or bias is not None and (bias.shape != weight.shape or bias.dtype != weight.dtype or bias.get_device() != index
+                                     or not bias.is_contiguous())):
+        raise ValueError(f"weight and bias: contiguous ({d},) of one type, float32, bfloat16 or float16, on the rows' device; "
+                         f"got {tuple(weight.shape)} of {weight.dtype} on {weight.device}"
+                         + ("" if bias is None else f" and {tuple(bias.shape)} of {bias.dtype} on {bias.device}"))
     return B.Norm(weight.data_ptr(), None if bias is None else bias.data_ptr(), None if mean is None else mean.data_ptr(),
                   None if rstd is None else rstd.data_ptr(), n, kind, eps)
 
@@ -81,26 +82,33 @@ def layer_norm(x, weight, bias=None, eps: float = 1e-5, out=None, dtype=None, st
 
 def _layer_norm(x, weight, bias, eps, out, dtype, stats):
     index = _device_of(x, "x")
-    d = weight.shape[-1] if weight.dim() else 0
+    d = weight.numel()
     rows = _flat(x, d, "x")
-    n = rows.shape[0]
+    n, kind = rows.shape[0], _FLOATS[rows.dtype]
     mean = rstd = None
     if stats:
         mean, rstd = torch.empty((2, n), dtype=torch.float32, device=x.device)
-    norm = _norm_of(weight, bias, mean, rstd, n, eps, index)
+    norm = _norm_of(weight, bias, mean, rstd, n, d, eps, index)
     given = out
     if out is None:
-        shaped = out = torch.empty(x.shape, dtype=dtype or x.dtype, device=x.device)
-        if out.dtype not in _FLOATS:
-            raise ValueError("dtype: float32, bfloat16 or float16")
-        ro = B.Rows(out.data_ptr(), d, d, _FLOATS[out.dtype])
+        # (of the rows, whose layout is that of a matrix whatever x's is)
+        if dtype is None or dtype is x.dtype:
+            out, to = torch.empty_like(rows, memory_format=torch.contiguous_format), kind
+        else:
+            to = _FLOATS.get(dtype)
+            if to is None:
+                raise ValueError("dtype: float32, bfloat16 or float16")
+            out = torch.empty_like(rows, dtype=dtype, memory_format=torch.contiguous_format)
+        ro = B.Rows(out.data_ptr(), d, d, to)
+        shaped = out if x.dim() == 2 else out.view(x.shape)
     else:
         _need(out.shape == x.shape and out.dtype in _FLOATS and out.get_device() == index, "out: of x's shape, on its device")
         shaped = out
         out = out.view(n, d)
         _need((out.stride(1) == 1 or d == 1) and (out.stride(0) >= d or n < 2), "out: rows of columns next to each other, apart")
         ro = _rows(out, n, d)
-    rc = B.lib().tensair_layer_norm(_at(norm), _at(_rows(rows, n, d)), _at(ro), _current_stream(index))
+    rc = B.lib().tensair_layer_norm(_at(norm), _at(B.Rows(rows.data_ptr(), rows.stride(0) if n > 1 else d, d, kind)), _at(ro),
+                                    _current_stream(index))
     if rc:
         B._check(rc, "tensair_layer_norm")
     if given is not None:
@@ -113,7 +121,7 @@ def layer_norm_gradient(grad, x, weight, mean, rstd, bias: bool = True, params: 
 
     bias False: no dbias; params False: neither dweight nor dbias (None in their places)."""
     index = _device_of(x, "x")
-    d = weight.shape[-1] if weight.dim() else 0
+    d = weight.numel()
     rows = _flat(x, d, "x")
     n = rows.shape[0]
     _need(grad.shape == x.shape and grad.get_device() == index, "grad: of x's shape, on its device")
@@ -121,8 +129,10 @@ def layer_norm_gradient(grad, x, weight, mean, rstd, bias: bool = True, params: 
         if s.shape != (n,) or s.dtype != torch.float32 or s.get_device() != index or not s.is_contiguous():
             raise ValueError(f"mean and rstd: contiguous float32 of ({n},) on the rows' device")
     grad = _flat(grad, d, "grad")
-    norm = _norm_of(weight, None, mean, rstd, n, 0.0, index)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    norm = _norm_of(weight, None, mean, rstd, n, d, 0.0, index)
+    dx = torch.empty_like(rows, memory_format=torch.contiguous_format)
+    if x.dim() != 2:
+        dx = dx.view(x.shape)
     dw = torch.empty_like(weight) if params else None
     db = torch.empty_like(weight) if params and bias else None
     workspace, size = None, 0
@@ -340,24 +350,31 @@ def recurrence_step(gate, value, state, out=None):
     """The next step of B streams: gate and value (B, d); state (B, d) float32 is updated in place.  Returns h, of value's type."""
     _need(not _wants_gradient(gate, value, state), "recurrence_step has no gradient: `recurrence` over one step has")
     index = _device_of(value, "value")
-    shape, kind = value.shape, _FLOATS.get(value.dtype)
-    given = out
-    if out is None:
-        out = torch.empty(shape, dtype=value.dtype, device=value.device)
-    places = []
-    for x, name in ((gate, "gate"), (value, "value"), (out, "out")):
-        if kind is None or len(shape) != 2 or x.shape != shape or x.dtype != value.dtype or x.get_device() != index:
-            raise ValueError(f"{name}: {tuple(x.shape)} of {x.dtype} on {x.device}; (B, d) of one type, float32, bfloat16 or float16, on one device goes")
-        row, column = x.stride()
-        if column != 1 and shape[1] > 1:
-            _need(name != "out", "out: channels next to each other")
-            x = x.contiguous()
-            row = x.stride(0)
-        places.append((x, B.Steps(x.data_ptr(), row, 0)))
+    shape, dtype = value.shape, value.dtype
+    kind = _FLOATS.get(dtype)
+    if kind is None or len(shape) != 2 or gate.shape != shape or gate.dtype is not dtype or gate.get_device() != index:
+        raise ValueError(f"gate and value: (B, d) of one type, float32, bfloat16 or float16, on one device; got {tuple(gate.shape)} of {gate.dtype} "
+                         f"on {gate.device} and {tuple(shape)} of {dtype} on {value.device}")
     h = _states(state, shape, index, "state")
     _need(h is not None, "state: None")
-    seq = B.Sequences(places[0][1], places[1][1], None, shape[0], 1, shape[1], kind)
-    rc = B.lib().tensair_recurrence_step(_at(seq), h, _at(places[2][1]), _current_stream(index))
+    streams, d = shape
+    gate_row, column = gate.stride()
+    if column != 1 and d > 1:
+        gate = gate.contiguous()
+        gate_row = d
+    value_row, column = value.stride()
+    if column != 1 and d > 1:
+        value = value.contiguous()
+        value_row = d
+    given = out
+    if out is None:
+        out, out_row = torch.empty_like(value, memory_format=torch.contiguous_format), d
+    else:
+        out_row, column = out.stride() if out.dim() == 2 else (0, 0)
+        if out.shape != shape or out.dtype is not dtype or out.get_device() != index or (column != 1 and d > 1):
+            raise ValueError("out: of value's shape and type, on its device, channels next to each other")
+    seq = B.Sequences((gate.data_ptr(), gate_row, 0), (value.data_ptr(), value_row, 0), None, streams, 1, d, kind)
+    rc = B.lib().tensair_recurrence_step(_at(seq), h, _at(B.Steps(out.data_ptr(), out_row, 0)), _current_stream(index))
     if rc:
         B._check(rc, "tensair_recurrence_step")
     _written(state if given is None else (state, given))

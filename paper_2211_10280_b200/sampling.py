@@ -12,6 +12,17 @@ from .operators import _FLOATS, _current_stream, _need, _written
 _at = C.byref
 
 
+_INFINITY = float("inf")
+
+
+def _setting(name, x, dtype, n, index):
+    if not isinstance(x, torch.Tensor):
+        return None, x
+    if x.shape != (n,) or x.dtype != dtype or x.get_device() != index or not x.is_contiguous():
+        raise ValueError(f"{name}: a number, or contiguous {dtype} of ({n},) on the logits' device")
+    return x.data_ptr(), 0
+
+
 def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, logprobs: bool = False):
     """Draws a token for each row of logits (n, V), with the random numbers `uniform` (float32 (n,), in [0, 1)).
 
@@ -34,27 +45,20 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=
         row = V
     if uniform.shape != (n,) or uniform.dtype != torch.float32 or uniform.get_device() != index or not uniform.is_contiguous():
         raise ValueError(f"uniform: contiguous float32 of ({n},) on the logits' device")
-    h = B.Draw(uniform=uniform.data_ptr(), n=n)
-    for name, x, dtype, low, high in (("temperature", temperature, torch.float32, 0, float("inf")), ("top_k", top_k, torch.int32, 0, 1 << 31),
-                                      ("top_p", top_p, torch.float32, 0, 2), ("min_p", min_p, torch.float32, 0, 1.0000001)):
-        if isinstance(x, torch.Tensor):
-            if x.shape != (n,) or x.dtype != dtype or x.get_device() != index or not x.is_contiguous():
-                raise ValueError(f"{name}: a number, or contiguous {dtype} of ({n},) on the logits' device")
-            setattr(h, name + "s", x.data_ptr())
-        else:
-            if not low <= x < high:
-                raise ValueError(f"{name}: {x} is out of range")
-            setattr(h, name, x)
+    # each setting: (address of one for each row, or None; the one for all)
+    ts, t = (None, temperature) if temperature.__class__ is float else _setting("temperature", temperature, torch.float32, n, index)
+    ks, k = (None, top_k) if top_k.__class__ is int else _setting("top_k", top_k, torch.int32, n, index)
+    ps, p = (None, top_p) if top_p.__class__ is float else _setting("top_p", top_p, torch.float32, n, index)
+    ms, m = (None, min_p) if min_p.__class__ is float else _setting("min_p", min_p, torch.float32, n, index)
+    if not (0 <= t < _INFINITY and 0 <= k < 1 << 31 and p >= 0 and 0 <= m <= 1):
+        raise ValueError(f"temperature {t}, top_k {k}, top_p {p} or min_p {m} is out of range")
     given = out
     if out is None:
         out = torch.empty(n, dtype=torch.int64, device=logits.device)
     elif out.shape != (n,) or out.dtype != torch.int64 or out.get_device() != index or not out.is_contiguous():
         raise ValueError(f"out: contiguous int64 of ({n},) on the logits' device")
-    h.token = out.data_ptr()
-    logprob = None
-    if logprobs:
-        logprob = torch.empty(n, dtype=torch.float32, device=logits.device)
-        h.logprob = logprob.data_ptr()
+    logprob = torch.empty_like(uniform) if logprobs else None
+    h = B.Draw(uniform.data_ptr(), out.data_ptr(), None if logprob is None else logprob.data_ptr(), ts, ps, ms, ks, t, p, m, k, n)
     rc = B.lib().tensair_sample(_at(h), _at(B.Rows(logits.data_ptr(), row if n > 1 else V, V, kind)), _current_stream(index))
     if rc:
         B._check(rc, "tensair_sample")
