@@ -130,7 +130,9 @@ struct Border {
     __device__ __forceinline__ bool operator<(const Border& o) const { return key > o.key || (key == o.key && ties < o.ties); }   // keeps less
 };
 
-constexpr uint32_t kList = 4096;             // tokens that are taken out of the row, at most
+// Tokens that are taken out of a row, at most.  0.9 of the mass of 100,000 logits (normal, 3.1 wide): 3,100 tokens, in one row of twelve more
+// than 4,096, for which the search through the whole row would take three times as long and the others wait.
+constexpr uint32_t kList = 8192;
 struct Shared {
     // logits (of any type) and ids of tokens that are taken out
     alignas(16) unsigned char listed[kList * 4];
@@ -150,7 +152,7 @@ struct Shared {
     uint32_t bucket, count_before, count_in;
     uint32_t edge[2];
 };
-constexpr uint32_t kShort = kList;           // rows whose border is looked for among all their tokens
+constexpr uint32_t kShort = 4096;            // rows whose border is looked for among all their tokens
 constexpr uint32_t kSharedBytes = (sizeof(Shared) + 15) / 16 * 16;
 
 // A row's slice, cut into kWarps runs of `steps` accesses of a warp.
@@ -860,7 +862,9 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
     }
 }
 
-constexpr uint32_t kStage = 160 * 1024;      // of shared memory for a slice, at most
+// Shared memory for a slice, at most: of a block that has a multiprocessor to itself, and of one that shares it with another.  (Large batches read
+// their rows again out of the level-2 cache: as fast.)
+constexpr uint32_t kStage = 226 * 1024 - kSharedBytes, kStageShared = 112 * 1024 - kSharedBytes;
 
 }  // namespace
 
@@ -875,7 +879,7 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
         while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 5000) cluster *= 2;
         const uint32_t steps = (uint32_t)(((uint64_t)a.V + (uint64_t)cluster * unit - 1) / ((uint64_t)cluster * unit));
         const uint64_t bytes = (uint64_t)steps * unit * sizeof(T);
-        const bool staged = bytes <= kStage;
+        const bool staged = bytes <= ((uint64_t)a.n * cluster <= (uint64_t)sms ? kStage : kStageShared);
         const bool whole = (uintptr_t)a.logits.data % 16 == 0 && (a.n < 2 || a.logits.stride % E == 0);
         auto* kernel = k_sample<T>;
         static std::atomic<bool> prepared[kMaxDevices];      // the kernel's attributes, once for each device
