@@ -10,8 +10,13 @@
 // A weight is exp((logit - largest) / temperature), in 64 bits, rounded to a multiple of 2^-bits: sums of weights are whole numbers, exact in
 // any order, so the draw does not depend on how a row is cut or on timing, and shared-memory atomics may add them up.
 //
-// A cluster of blocks shares a row, each with a slice of it in its shared memory: the logits are read from memory once, whatever is
-// asked for.  (Slices that do not fit are read again, out of the level-2 cache.)
+// Few of a row's tokens are near the border, though.  One pass counts all logits (and adds up their weights, where a share of the mass is
+// asked for); the counts bound the masses, and say from which logit on the border must lie.  Those tokens, in order of their ids, are
+// taken out into the shared memory of one block, which finds border and token among them.
+//
+// A block has a row to itself in large batches; in small ones a cluster of blocks shares it.  Bound by instructions (256 rows of 100,000 bf16
+// logits, 0.9 of the mass: 98 us, of which the pass with the weights takes a third, 34 instructions a logit; reading is 8) and, for single
+// rows, by the latency of a dozen steps with a barrier each (one row of 100,000: 22 us).
 #include <cooperative_groups.h>
 
 #include <atomic>

@@ -8,7 +8,8 @@
 layer_norm, dropout and recurrence take part in autograd where an input needs a gradient.  Every call enqueues its kernels on the
 current stream of the tensors' device and returns without waiting; tensors that another stream is still writing are ordered by the
 caller, as for torch's own operators.  Nothing is kept from one call for the next, so calls may be made from several threads
-and on several streams, and captured.  There is no fallback: a missing library, a CPU tensor or a refused argument is an error.
+and on several streams, and captured (a captured `backward()`, as one through torch's own operators, wants leaves that no eager graph
+still holds; torch.autograd.grad does not mind).  There is no fallback: a missing library, a CPU tensor or a refused argument is an error.
 """
 from __future__ import annotations
 
@@ -43,7 +44,7 @@ def _wants_gradient(*tensors):
 def _flat(x, d, name):
     """x as rows of d elements that lie next to each other, (n, d)."""
     shape = x.shape
-    if len(shape) == 0 or shape[-1] != d or x.dtype not in _FLOATS:
+    if len(shape) == 0 or shape[-1] != d or d == 0 or x.dtype not in _FLOATS:
         raise ValueError(f"{name}: {tuple(shape)} of {x.dtype}; (..., {d}) of float32, bfloat16 or float16 goes")
     if len(shape) != 2:
         x = x.reshape(x.numel() // d, d)
