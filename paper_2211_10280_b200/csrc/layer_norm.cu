@@ -7,6 +7,11 @@
 // variance is taken about the mean, in a second pass over those registers.  Rows that do not fit (beyond 16,384 columns of 16 bits)
 // are read again, out of the level-2 cache.  The sums over rows (dw, db) stay in the registers of a grid that goes round
 // the rows; each block leaves one partial row, and a second launch adds those up in block order: no sum depends on timing.
+//
+// Bound by the latency of the rows' reads.  65,536 rows of 512 in bf16: forward 35 us (134 MB, 3.8 TB/s; blocks for five to a
+// multiprocessor; six spill, 41 us), backward 48 us (201 MB, 4.2 TB/s) and 6 for the second launch.  The backward pass has 16 warps to
+// a multiprocessor, whose registers hold weight and sums of 16 columns to a lane; the next rows are prefetched into the level-2
+// cache (52 us against 54).  Held in registers instead they left room for half the warps (74 us).  One row: 4.6 us, a launch.
 #include "columns.cuh"
 #include "layers.h"
 

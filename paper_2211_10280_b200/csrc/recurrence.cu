@@ -21,6 +21,10 @@
 // were off by 6e-5).
 //
 // The next stretch's inputs are on their way into shared memory (asynchronous copies, each thread its own) while this one's are worked on.
+//
+// Bound by instructions and the barriers of a turn: 64 sequences of 1,024 of 512 in bf16 take 66 us forward (201 MB, 35 instructions an
+// element, issue slots 0.55 busy) and 91 to 95 us backward (336 MB, 52 instructions, 0.61); from 128 sequences on 0.73 us a sequence forward, 4.3 TB/s.
+// One stream of 65,536 steps: 95 to 102 us, a chain of 22 turns of 12 blocks.  One step of 64 streams: 4.2 us, a launch.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -567,7 +571,9 @@ cudaError_t rooms(size_t shared, int sms, uint32_t (&room)[kSizes]) {
 }
 
 // Cuts the work so that the blocks that the device holds at once come out even: the fewest turns of the busiest one, a group of channels
-// counting half a turn more, and turns in clusters by what their exchange takes.
+// counting half a turn more, and turns in clusters by what their exchange takes.  us, stretches x cluster: gradient of 64 sequences of 1,024 of
+// 512, bf16: 16 x 1 97, 16 x 2 89, 16 x 4 92, 32 x 1 110, 32 x 2 107, 32 x 8 206; forward, 64 padded of 1,021 of 300, fp32: 72, 68, 67, 68, 69, 151; one
+// of 65,536 of 512, bf16: 32 x 4 198, 32 x 8 137, 32 x 12 103, 32 x 16 121.
 Cut cut_of(const RecurrenceArgs& a, uint32_t e, const uint32_t (&room)[kSizes], uint32_t* grid) {
     Cut best;
     uint64_t least = ~0ull;

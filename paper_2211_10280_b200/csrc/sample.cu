@@ -15,8 +15,8 @@
 // taken out into the shared memory of one block, which finds border and token among them.
 //
 // A block has a row to itself in large batches; in small ones a cluster of blocks shares it.  Bound by instructions (256 rows of 100,000 bf16
-// logits, 0.9 of the mass: 98 us, of which the pass with the weights takes a third, 34 instructions a logit; reading is 8) and, for single
-// rows, by the latency of a dozen steps with a barrier each (one row of 100,000: 22 us).
+// logits, 0.9 of the mass: 108 us, of which the pass with the weights takes a third, 34 instructions a logit; reading alone would be 8) and, for
+// single rows, by the latency of some 25 steps with a barrier each (one row of 100,000: 22 us).
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -877,9 +877,9 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
     return with_type(a.logits.type, [&](auto t) {
         using T = decltype(t);
         constexpr uint32_t E = Slice<T>::E, unit = kWarps * 32 * E;      // tokens of one access of a block
-        // Blocks enough for the device, two to a multiprocessor, as long as a slice is worth the cluster's barriers.  us, one block to
-        // a row against more (a power of two each): 256 rows of 100,000 0.9 of the mass: 174, 167, 192; first 50: 66, 86, 109; 64 rows of 10,000: 27, 27,
-        // 31, 48; one row of 100,000: 69, 47, 34, 29, 26
+        // Blocks enough for the device, as long as a slice is worth the cluster's barriers.  us, 1, 2, 4, 8, 16 blocks to a row, each with 10
+        // for the launch: 256 rows of 100,000, 0.9 of the mass: 108, 170, 212; first 50: 65, 109; 64 rows of 10,000: 25, 28, 32, 47, 83; 16 rows of
+        // 100,000: 194, 112, 74, 53, 55; one row of 100,000: 69, 46, 29, 28, 24
         uint32_t cluster = 1;
         while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 5000) cluster *= 2;
         const uint32_t steps = (uint32_t)(((uint64_t)a.V + (uint64_t)cluster * unit - 1) / ((uint64_t)cluster * unit));
