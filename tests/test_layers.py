@@ -547,6 +547,54 @@ def test_a_backward_pass_is_captured():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@gpu
+def test_calls_from_two_threads_at_once():
+    import threading
+
+    from paper_2211_10280_b200 import sampling
+
+    L = _ops()
+
+    def work(seed, out):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            x, w, u = _rand((700, 96), BF16, seed=seed), _rand((96,), F32, 0.1, 1.0, seed=seed), torch.rand(5, generator=torch.Generator().manual_seed(seed)).cuda()
+            logits, state = _rand((5, 4000), seed=seed), _rand((7, 96), seed=seed + 1)
+            for _ in range(60):
+                y, mean, rstd = L.layer_norm(x, w, stats=True)
+                h, last = L.recurrence(y.view(7, 100, 96), y.view(7, 100, 96), state)
+                out[seed] = [y, h, last, *L.layer_norm_gradient(y, x, w, mean, rstd), L.dropout(y, 0.3, seed, 4), sampling.sample(logits, u, 0.9, 30, 0.9)]
+            torch.cuda.current_stream().synchronize()
+
+    alone, together = {}, {}
+    for seed in range(4):
+        work(seed, alone)
+    threads = [threading.Thread(target=work, args=(seed, together)) for seed in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for seed in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(alone[seed], together[seed]))
+
+
+@gpu
+def test_gradients_of_broadcast_inputs():
+    L = _ops()
+    gate, value, bias = _rand((1, 1, 24), seed=1).requires_grad_(), _rand((3, 50, 24), seed=2), _rand((24,), seed=3)
+    full = gate.detach().expand(3, 50, 24).contiguous().requires_grad_()
+    a, = torch.autograd.grad(L.recurrence(gate.expand(3, 50, 24), value)[0].square().sum(), gate)
+    b, = torch.autograd.grad(L.recurrence(full, value)[0].square().sum(), full)
+    assert torch.allclose(a, b.sum((0, 1), keepdim=True), rtol=1e-5, atol=1e-6)
+    row = _rand((1, 24), seed=4).requires_grad_()
+    many = row.detach().expand(70, 24).contiguous().requires_grad_()
+    weigh = _rand((70, 24), seed=5)
+    a, = torch.autograd.grad((L.layer_norm(row.expand(70, 24), bias) * weigh).sum(), row)
+    b, = torch.autograd.grad((L.layer_norm(many, bias) * weigh).sum(), many)
+    assert torch.allclose(a, b.sum(0, keepdim=True), rtol=1e-4, atol=1e-5)
+    x = _rand((40, 30), seed=6)          # transposed: the mask goes by the element's place in the tensor, not in memory
+    assert torch.equal(L.dropout(x.t(), 0.4, 1, 2), L.dropout(x.t().contiguous(), 0.4, 1, 2))
+
+
 # ---------------------------------------------------------------- together
 def _plain_block(model, x, w, kept, lengths):
     """The model's block and logits in 64 bits, elementary operations alone."""

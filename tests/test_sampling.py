@@ -209,6 +209,25 @@ def test_the_largest_vocabularies(V, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("n,V,dtype", [(3, 60_000, F32), (2, 40_000, BF16), (160, 20_000, F32), (150, 30_000, F16)])
+def test_fronts_that_do_not_fit_into_one_block(n, V, dtype):
+    """Flat rows, of which tens of thousands of tokens are kept: the border is looked for in the whole row, by a cluster or by a block."""
+    x = _logits(n, V, dtype, std=0.4, seed=V)
+    x[0, ::3] = -INF
+    for s in (dict(p=0.93), dict(k=15_000), dict(k=15_000, p=0.8), dict(T=20.0, p=0.5, min_p=0.97), dict(k=9000, min_p=0.2)):
+        _check(x, _uniform(n, 3), **s)
+
+
+@gpu
+@pytest.mark.parametrize("V", [8190, 8192, 8194, 4096, 4097, 16_400])
+def test_sizes_at_which_the_search_changes_its_way(V):
+    for dtype in (F32, BF16):
+        x = _logits(3, V, dtype, std=0.3, seed=V)
+        for s in (dict(p=0.999), dict(k=V - 1), dict(k=V), dict(k=V + 1, p=0.99), dict(k=4096), dict(k=8192, p=0.9999)):
+            _check(x, _uniform(3, 5), **s)
+
+
+@gpu
 def test_rows_beyond_32_bits():
     V, n = 2 ** 20, 2100                    # 2.2 G logits
     logits = torch.full((n, V), -30.0, dtype=F16, device="cuda")
