@@ -20,6 +20,7 @@
 #include <cooperative_groups.h>
 
 #include <atomic>
+#include <cstddef>
 #include <type_traits>
 
 #include "columns.cuh"
@@ -439,8 +440,24 @@ template <typename T>
 __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
     constexpr int E = Slice<T>::E;
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+    // What goes of an access is kept as a byte for the second pass, as long as there is room: where the sums of masses are otherwise, which are not
+    // in use yet (and are set to zero again below).
+    unsigned char* bytes = reinterpret_cast<unsigned char*>(sh.low);
+    static_assert(offsetof(Shared, high) == offsetof(Shared, low) + sizeof(Shared::low), "one behind the other");
+    const bool kept = slice.steps * kThreads <= sizeof(sh.low) + sizeof(sh.high);
+    auto clear = [&] {
+        if (kept)
+            for (uint32_t b = tid; b < kBuckets; b += kThreads) sh.low[0][b] = sh.low[1][b] = sh.high[0][b] = sh.high[1][b] = 0;
+        __syncthreads();
+    };
     uint32_t here = 0;
-    slice.accesses([&](uint32_t, const Pack<T, E>& x) { here += __popc(slice.from_on(x, from)); });
+    for (uint32_t s = 0; s < slice.steps; ++s) {
+        const uint32_t place = slice.place(s);
+        if (place - lane * E >= slice.length) break;
+        const uint32_t mine = slice.from_on(slice.load(place), from);
+        if (kept) bytes[s * kThreads + tid] = (unsigned char)mine;
+        here += __popc(mine);
+    }
     here = __reduce_add_sync(0xFFFFFFFFu, here);
     __syncthreads();
     if (lane == 0) sh.warp_count[warp] = here;
@@ -459,13 +476,18 @@ __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
         if (r < team.rank) at += n;
         count += n;
     }
-    if (count > kList) return kTooMany;
+    if (count > kList) {
+        clear();
+        return kTooMany;
+    }
     T* logits = team.of((T*)sh.listed, 0);
     uint32_t* ids = team.of(&sh.ids[0], 0);
     if (here)
-        slice.accesses([&](uint32_t place, const Pack<T, E>& x) {
-            uint32_t mine = slice.from_on(x, from);
-            if (!__any_sync(0xFFFFFFFFu, mine)) return;
+        for (uint32_t s = 0; s < slice.steps; ++s) {
+            const uint32_t place = slice.place(s);
+            if (place - lane * E >= slice.length) break;
+            uint32_t mine = kept ? bytes[s * kThreads + tid] : slice.from_on(slice.load(place), from);
+            if (!__any_sync(0xFFFFFFFFu, mine)) continue;
             const uint32_t own = __popc(mine);
             uint32_t upto = own;
 #pragma unroll
@@ -473,7 +495,7 @@ __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
                 const uint32_t c = __shfl_up_sync(0xFFFFFFFFu, upto, o);
                 if (lane >= (uint32_t)o) upto += c;
             }
-            // few lanes have any, and few of them more than one: read again rather than picked from registers
+            // few lanes have any, and few of them more than one
             for (uint32_t to = at + upto - own; mine; mine &= mine - 1, ++to) {
                 const uint32_t id = place + __ffs(mine) - 1;
                 if (!in_bounds(nullptr, to, kList)) break;
@@ -481,9 +503,10 @@ __device__ Taken take_out(Shared& sh, Slice<T>& slice, Team& team, T from) {
                 ids[to] = slice.begin + id;
             }
             at += __shfl_sync(0xFFFFFFFFu, upto, 31);
-        });
+        }
     team.sync();      // all is there
     if (team.rank != 0) return kByOther;
+    clear();
     team = Team{1, 0};
     slice.logits = (const T*)sh.listed;
     slice.begin = 0;
@@ -881,7 +904,7 @@ cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
         // for the launch: 256 rows of 100,000, 0.9 of the mass: 108, 170, 212; first 50: 65, 109; 64 rows of 10,000: 25, 28, 32, 47, 83; 16 rows of
         // 100,000: 194, 112, 74, 53, 55; one row of 100,000: 69, 46, 29, 28, 24
         uint32_t cluster = 1;
-        while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 5000) cluster *= 2;
+        while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 8000) cluster *= 2;
         const uint32_t steps = (uint32_t)(((uint64_t)a.V + (uint64_t)cluster * unit - 1) / ((uint64_t)cluster * unit));
         const uint64_t bytes = (uint64_t)steps * unit * sizeof(T);
         const bool staged = bytes <= ((uint64_t)a.n * cluster <= (uint64_t)sms ? kStage : kStageShared);
