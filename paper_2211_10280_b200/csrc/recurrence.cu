@@ -151,7 +151,7 @@ __device__ __forceinline__ void send(const float2* to, const uint64_t* barrier, 
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
                  ::"r"(there), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w), "r"(bar) : "memory");
 }
-// False: they did not come, after some 50 ms.
+// False: they did not come, however often it was asked.
 __device__ __forceinline__ bool wait_bytes(uint64_t* barrier, uint32_t parity) {
     for (int i = 0; i < 1 << 20; ++i) {
         uint32_t done;
