@@ -26,10 +26,5 @@ __device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
     return r;
 }
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-    Two r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
-    return r;
-}
 
 }  // namespace tensair
