@@ -488,11 +488,11 @@ cudaError_t launch_norm_gradient(cudaStream_t stream, const NormArgs& a) {
                 k_norm_gradient<TX, TY, C, S::group, S::k><<<parts, threads, 0, stream>>>(a, vecs);
             });
             if (!fits) {
-                k_norm_gradient_wide<TX, TY, C><<<a.n, kWideThreads, 0, stream>>>(a, vecs);
-                if (a.partials) {
+                if (a.partials) {      // first: dx may be written over the incoming gradient
                     parts = a.n < kWideParts ? a.n : kWideParts;
                     k_norm_columns<TX, TY><<<dim3((a.d + 31) / 32, parts), kWideThreads, 0, stream>>>(a);
                 }
+                k_norm_gradient_wide<TX, TY, C><<<a.n, kWideThreads, 0, stream>>>(a, vecs);
             }
             return cudaGetLastError();
         });
