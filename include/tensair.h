@@ -649,6 +649,8 @@ TENSAIR_API int tensair_dropout(const tensair_dropout_call* dropout, void* strea
  * A tensair_steps holds rows of d elements: `step` elements between the steps of a sequence, `batch` between sequences.
  * lengths: steps of each sequence, clamped to 0 .. T; the steps from there on are padding: what is there is not
  * used, out is zero there and the state stays.  state: what h begins with (NULL = 0); last: h after the last step.
+ * f and 1 - f, and products of f, keep
+ * their relative accuracy: what is left of a state (or gradient) that is being forgotten is as right as the rest.
  * marks: h before every eighth step, float[B][ceil(T / 8)][d], for the gradient.  state and last may be one (not in the gradient).
  * A value, gate or state that is not finite makes its channel NaN or infinite from that step of its sequence on.
  */

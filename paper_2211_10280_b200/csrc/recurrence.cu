@@ -6,7 +6,7 @@
 //
 //     D_t = dh_t + e_{t+1},  e_t = f_t D_t,  dv_t = (1 - f_t) D_t,  dgate_t = f_t (1 - f_t) (h_{t-1} - v_t) D_t
 //
-// Both are first-order linear recurrences x <- (1 - r) x + b.  Steps compose: (r, b) then (r', b') is (r + r' - r r', (1 - r') b + b').  A thread takes
+// Both are first-order linear recurrences x <- f x + b.  Steps compose: (f, b) then (f', b') is (f f', f' b + b').  A thread takes
 // 8 steps of a few channels and holds them in registers; the threads of a block cover more steps one after the other, the blocks of
 // a cluster still more, and a block goes on with its cluster's next stretch until the sequence ends, and then with other channels.  Every
 // level passes on the composition of what it holds, gets the state that it begins with, and only then makes its outputs: the inputs are
@@ -15,10 +15,11 @@
 // The gradient needs h_{t-1} again: the forward call leaves the state before every eighth step in fp32 (half a byte per element),
 // and a thread of the backward call replays its own 8 steps from there.
 //
-// Kept of a gate is n = f - 1 = -sigmoid(-gate), not f: x + n x in one fused step has the relative accuracy of n, so a gate near 1
-// remembers for as long as it should (1 - 6e-8 would be the f next to 1) and a gate of minus infinity forgets all.  Compositions keep
-// f - 1 of their product for the same reason (the product itself, rounded near 1 step after step, drifts: 20,000 steps of 1 - 8e-7
-// were off by 6e-5).
+// A factor f, of a step or of many, is kept as q: f - 1 (never positive) from f = 1/2 on, f itself below; the sign bit tells which.  So it keeps
+// its relative accuracy at both ends.  A gate near 1 remembers for as long as it should (1 - 6e-8 would be the f next to 1; products of such an f, rounded
+// step after step, drift: 20,000 steps of 1 - 8e-7 were off by 6e-5).  And what is left of a state that has been forgotten is right: with
+// f - 1 alone a step of gate -17 was off by 44 %, 128 steps of gate 2 by 32 %.  (Three instructions an element forward, five
+// backward: 64 sequences of 1,024 of 512 in bf16 63 us as before, their gradient 98 us for 93.)
 //
 // The next stretch's inputs are on their way into shared memory (asynchronous copies, each thread its own) while this one's are worked on.
 //
@@ -55,26 +56,44 @@ __device__ __forceinline__ float reciprocal_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float least_or_nan(float x, float y) {
-    float z;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
-    return z;
-}
 // e = exp(gate).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by (1.5 |gate| + 2) 2^-24 of it; half a unit of the
 // gate's own last place is 10^4 times as much.  Gates of 32 bits: expf.
-// kFinite: at most 2^127.9, for what is multiplied with it (1 - f is zero all the same).
-template <typename T, bool kFinite>
+template <typename T>
 __device__ __forceinline__ float exp_of(float gate) {
-    if constexpr (sizeof(T) == 2) {
-        const float x = gate * 1.44269504f;
-        return exp2_approx(kFinite ? least_or_nan(x, 127.9f) : x);
-    } else return expf(kFinite ? least_or_nan(gate, 88.6f) : gate);
+    if constexpr (sizeof(T) == 2) return exp2_approx(gate * 1.44269504f);
+    else return expf(gate);
 }
-// n = f - 1 from e = exp(gate): -1 / (1 + e)
+// f - 1 from e = exp(gate): -1 / (1 + e).  The quotient is off by a unit in the last place of 32 bits at most, and zero below 2^-126.
 __device__ __forceinline__ float complement(float e) { return reciprocal_approx(-1.0f - e); }
-__device__ __forceinline__ float decay(float n, float x) { return fmaf(n, x, x); }
-// f - 1 of the product of two factors, from theirs.
-__device__ __forceinline__ float join_rest(float a, float b) { return fmaf(b, a + 1.0f, a); }
+// q of a factor: f - 1 or, where the sign bit is not set, f.
+__device__ __forceinline__ bool near_one(float q) { return __float_as_int(q) < 0; }
+constexpr float kOne = -0.0f;      // the factor 1
+// f x
+__device__ __forceinline__ float decay(float q, float x) { return fmaf(q, x, near_one(q) ? x : 0.0f); }
+// (1 - f) x
+__device__ __forceinline__ float share(float q, float x) { return fmaf(-q, x, near_one(q) ? 0.0f : x); }
+// f x + (1 - f) v: x + n (x - v), or v + f (x - v)
+__device__ __forceinline__ float advance(float q, float x, float v) { return fmaf(q, x, fmaf(-q, v, near_one(q) ? x : v)); }
+// Factors one after the other: their product p, and that less one, n = sum of (f - 1) * (the product before), whose terms have one sign.  p's
+// rounding errors are few (a stretch's, a block's), and n goes on where p is near 1: nothing drifts.
+struct Product {
+    float p = 1.0f, n = kOne;
+    __device__ __forceinline__ void join(float f, float rest) {
+        n = fmaf(rest, p, n);
+        p *= f;
+    }
+    __device__ __forceinline__ float q() const { return p <= 0.5f ? p : n; }
+};
+// A composition: what is there already comes before what is joined to it.
+struct Joined {
+    Product product;
+    float b = 0.0f;
+    __device__ __forceinline__ void join(float q, float add) {
+        const float f = near_one(q) ? q + 1.0f : q;
+        product.join(f, q);      // (n is not used behind a factor of 1/2 or less)
+        b = fmaf(f, b, add);
+    }
+};
 
 // 8 bytes of raw elements as floats, and back.
 template <typename T>
@@ -194,33 +213,28 @@ __device__ __forceinline__ void join_block(Joint<E>& joint, const Cut& cut, uint
     // a channel's stretches are cut into parts of E (or are one part, where there are few)
     for (uint32_t i = threadIdx.x; i < channels * parts; i += kThreads) {
         const uint32_t c = i & (channels - 1), from = i / channels * each;
-        float n = 0.0f, b = 0.0f;
+        Joined all;
 #pragma unroll 4
-        for (uint32_t s = from; s < from + each; ++s) {
-            const float then = joint.n[odd][s * channels + c];
-            b = decay(then, b) + joint.b[odd][s * channels + c];
-            n = join_rest(n, then);
-        }
-        if (parts > 1) joint.parts[i] = make_float2(n, b);
+        for (uint32_t s = from; s < from + each; ++s) all.join(joint.n[odd][s * channels + c], joint.b[odd][s * channels + c]);
+        if (parts > 1) joint.parts[i] = make_float2(all.product.q(), all.b);
     }
     if (parts > 1) __syncthreads();
     for (uint32_t i = threadIdx.x; i < channels * parts; i += kThreads) {
         const uint32_t c = i & (channels - 1), part = i / channels;
-        float n = 0.0f, b = 0.0f;
+        Joined all;
 #pragma unroll 4
         for (uint32_t q = 0; q < part; ++q) {
             const float2 x = joint.parts[q * channels + c];
-            b = decay(x.x, b) + x.y;
-            n = join_rest(n, x.x);
+            all.join(x.x, x.y);
         }
 #pragma unroll 4
         for (uint32_t s = part * each; s < (part + 1) * each; ++s) {
             const float then = joint.n[odd][s * channels + c], add = joint.b[odd][s * channels + c];
-            joint.n[odd][s * channels + c] = n;
-            joint.b[odd][s * channels + c] = b;
-            b = decay(then, b) + add;
-            n = join_rest(n, then);
+            joint.n[odd][s * channels + c] = all.product.q();
+            joint.b[odd][s * channels + c] = all.b;
+            all.join(then, add);
         }
+        const float n = all.product.q(), b = all.b;
         if (part + 1 < parts) continue;
         if (cut.cluster == 1) {
             const float carry = joint.carry[c];
@@ -359,62 +373,60 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
             for (int e = 0; e < E; ++e) joint.carry[u * E + e] = first.v[e];
         }
         fetched();
-        float n[kSteps][E], slope[kBack ? kSteps : 1][E], all_n[E], all_b[E];
-        uint2 other[kSteps];      // values; backward: gradients
+        // forward: the product of the factors up to a step, and what the steps up to it add; backward: a step's factor, and f (h - v)
+        float by[kSteps][E], with[kSteps][E], all_b[E];
+        uint2 grads[kBack ? kSteps : 1];
+        Product all[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) all_n[e] = all_b[e] = 0.0f;
+        for (int e = 0; e < E; ++e) all_b[e] = 0.0f;
         const uint32_t t0 = first_step(a, cut, turn, rank);
         // nothing but padding: the state stays  (forwards 65 us become 56, a padded batch; backwards the same made unpadded ones 8 us slower)
         if (!kBack && t0 >= now.length) {
 #pragma unroll
             for (int l = 0; l < kSteps; ++l) {
-                other[l] = make_uint2(0, 0);
-#pragma unroll
-                for (int e = 0; e < E; ++e) n[l][e] = 0.0f;
-            }
-        } else if constexpr (!kBack) {
-#pragma unroll
-            for (int l = 0; l < kSteps; ++l) {
-                float gate[E], v[E];
-                unpack<T>(rows[l * kThreads], gate);
-                other[l] = rows[(kSteps + l) * kThreads];
-                unpack<T>(other[l], v);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    n[l][e] = complement(exp_of<T, false>(gate[e]));
-                    all_n[e] = join_rest(all_n[e], n[l][e]);
-                    all_b[e] = fmaf(-n[l][e], v[e], decay(n[l][e], all_b[e]));
+                    by[l][e] = 1.0f;
+                    with[l][e] = 0.0f;
                 }
             }
         } else {
             float h[E];
+            if constexpr (kBack) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) h[e] = mark[e];
-#pragma unroll
-            for (int l = 0; l < kSteps; ++l) {
-                float gate[E], v[E];
-                unpack<T>(rows[l * kThreads], gate);
-                unpack<T>(rows[(kSteps + l) * kThreads], v);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float exp_gate = exp_of<T, true>(gate[e]);
-                    n[l][e] = complement(exp_gate);
-                    slope[l][e] = (exp_gate * n[l][e]) * n[l][e] * (h[e] - v[e]);      // (-f) (-(1 - f)) (h - v)
-                    h[e] = fmaf(-n[l][e], v[e], decay(n[l][e], h[e]));
-                }
-                other[l] = rows[(2 * kSteps + l) * kThreads];
+                for (int e = 0; e < E; ++e) h[e] = mark[e];
             }
 #pragma unroll
-            for (int l = kSteps - 1; l >= 0; --l) {
-                float dh[E];
-                unpack<T>(other[l], dh);
+            for (int l = 0; l < kSteps; ++l) {
+                float gate[E], v[E], dh[E];
+                unpack<T>(rows[l * kThreads], gate);
+                unpack<T>(rows[(kSteps + l) * kThreads], v);
+                if constexpr (kBack) {
+                    grads[l] = rows[(2 * kSteps + l) * kThreads];
+                    unpack<T>(grads[l], dh);
+                }
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    all_n[e] = join_rest(all_n[e], n[l][e]);
-                    all_b[e] = decay(n[l][e], all_b[e] + dh[e]);      // padding: the gradient passes, none is added
+                    const float exp_gate = exp_of<T>(gate[e]), rest = complement(exp_gate), small = exp_gate * -rest;
+                    const bool near = !(gate[e] < 0.0f);
+                    const float f = near ? 1.0f + rest : small;
+                    all[e].join(f, rest);
+                    if constexpr (!kBack) {
+                        all_b[e] = fmaf(f, all_b[e], -rest * v[e]);
+                        by[l][e] = all[e].p;
+                        with[l][e] = all_b[e];
+                    } else {
+                        all_b[e] = fmaf(all[e].p, dh[e], all_b[e]);      // padding: the gradient passes, none is added
+                        by[l][e] = near ? rest : small;
+                        with[l][e] = f * (h[e] - v[e]);
+                        h[e] = fmaf(f, h[e], -rest * v[e]);
+                    }
                 }
             }
         }
+        float all_n[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) all_n[e] = all[e].q();
         // the next turn's data, of this group or of the next
         if (++done == cut.turns) {
             done = 0;
@@ -439,11 +451,10 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
                 const bool whole = t0 + kSteps <= now.length;
 #pragma unroll
                 for (int l = 0; l < kSteps; ++l, out += a.out.step) {
-                    float v[E];
-                    unpack<T>(other[l], v);
+                    float h[E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = fmaf(-n[l][e], v[e], decay(n[l][e], x[e]));
-                    uint2 raw = pack<T>(x);
+                    for (int e = 0; e < E; ++e) h[e] = fmaf(by[l][e], x[e], with[l][e]);
+                    uint2 raw = pack<T>(h);
                     if (!whole) {
                         if (t0 + l >= a.T) break;
                         if (t0 + l >= now.length) raw = make_uint2(0, 0);
@@ -451,27 +462,27 @@ k_recurrence(const __grid_constant__ RecurrenceArgs a, const __grid_constant__ C
                     store_raw<T, C>(out, raw, now.left);
                 }
             } else {
-                T* dgate = (T*)a.dgate.data + now.s * a.dgate.batch + t0 * a.dgate.step + now.col;
-                T* dvalue = (T*)a.dvalue.data + now.s * a.dvalue.batch + t0 * a.dvalue.step + now.col;
+                T* dgate = (T*)a.dgate.data + now.s * a.dgate.batch + (t0 + kSteps - 1) * a.dgate.step + now.col;
+                T* dvalue = (T*)a.dvalue.data + now.s * a.dvalue.batch + (t0 + kSteps - 1) * a.dvalue.step + now.col;
                 const bool whole = t0 + kSteps <= now.length;
 #pragma unroll
-                for (int l = kSteps - 1; l >= 0; --l) {
+                for (int l = kSteps - 1; l >= 0; --l, dgate -= a.dgate.step, dvalue -= a.dvalue.step) {
                     float dh[E], dg[E], dv[E];
-                    unpack<T>(other[l], dh);
+                    unpack<T>(grads[l], dh);
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         const float D = dh[e] + x[e];
-                        x[e] = decay(n[l][e], D);
-                        dg[e] = slope[l][e] * D;
-                        dv[e] = -n[l][e] * D;
+                        x[e] = decay(by[l][e], D);
+                        dv[e] = share(by[l][e], D);
+                        dg[e] = with[l][e] * dv[e];
                     }
                     uint2 g = pack<T>(dg), v = pack<T>(dv);
                     if (!whole) {
                         if (t0 + l >= a.T) continue;
                         if (t0 + l >= now.length) g = v = make_uint2(0, 0);
                     }
-                    store_raw<T, C>(dgate + l * a.dgate.step, g, now.left);
-                    store_raw<T, C>(dvalue + l * a.dvalue.step, v, now.left);
+                    store_raw<T, C>(dgate, g, now.left);
+                    store_raw<T, C>(dvalue, v, now.left);
                 }
             }
         }
@@ -498,8 +509,8 @@ k_recurrence_step(const __grid_constant__ RecurrenceArgs a, const __grid_constan
     float h[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float n = complement(exp_of<T, false>(to_float(g.v[e])));
-        h[e] = fmaf(-n, to_float(v.v[e]), decay(n, old.v[e]));
+        const float gate = to_float(g.v[e]), exp_gate = exp_of<T>(gate), rest = complement(exp_gate);
+        h[e] = advance(gate < 0.0f ? exp_gate * -rest : rest, old.v[e], to_float(v.v[e]));
     }
     store_columns<C>(a.last + row, h, left);
     store_columns<C>((T*)a.out.data + s * a.out.batch + col, h, left);

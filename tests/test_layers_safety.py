@@ -1,7 +1,15 @@
-"""Calls of the recurrent model's operators that their documentation allows and that go wrong easily: results written over their inputs.
+"""Calls of the recurrent model's operators that their documentation allows and that go wrong easily: results written over their inputs, states
+that fall by many orders of magnitude.
+
+Bounds of the recurrence, u = 2^-24: 1 - f is off by S u of itself, and so is f where it is below 1/2 (S = 8: expf 2 u, the fast quotient 4 u and a
+rounding each of 1 + e and the product; with gates of 16 bits 1.5 |gate| more for the rounded product with log2(e)).  Where f is 1/2 or
+more it is taken from 1 - f and is off by S u (1 - f).  So f is off by S u min(f, 1 - f).  On top of that a step has two roundings, and the joining of
+stretches of eight steps as often again or less; 8 u of the terms' sizes are allowed for all of these.  All of it is relative to
+f |h| + (1 - f) |v|: nothing is left of a state that has been forgotten.
 """
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
@@ -9,6 +17,8 @@ from paper_2211_10280_b200 import binding as B
 from paper_2211_10280_b200 import build as libbuild
 
 gpu = pytest.mark.gpu
+U = 2.0 ** -24
+LAST = {torch.float32: (2.0 ** -24, 2.0 ** -150), torch.bfloat16: (2.0 ** -8, 2.0 ** -134), torch.float16: (2.0 ** -11, 2.0 ** -25)}
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
@@ -26,6 +36,14 @@ def _ops():
 def _rand(shape, dtype=F32, std=1.0, mean=0.0, seed=0):
     g = torch.Generator().manual_seed(seed)
     return (torch.randn(shape, generator=g) * std + mean).to(dtype).cuda()
+
+
+def _close(got, want, slack):
+    rel, least = LAST[got.dtype]
+    assert got.shape == want.shape and not torch.isnan(got).any()
+    excess = (got.double() - want).abs() - (slack + (want.abs() + slack) * rel + least)
+    worst = excess.argmax()
+    assert excess.max().item() <= 0, (got.flatten()[worst].item(), want.flatten()[worst].item(), slack.flatten()[worst].item())
 
 
 def _ok(rc):
@@ -78,3 +96,98 @@ def test_last_states_in_the_place_of_the_first(B_, T, d):
     q = B.Sequences(rows[0], rows[1], None, B_, T, d, B.BFLOAT16)
     _ok(B.lib().tensair_recurrence(q, state.data_ptr(), rows[2], state.data_ptr(), None, torch.cuda.current_stream().cuda_stream))
     assert torch.equal(again, out) and torch.equal(state, last)
+
+
+# ---------------------------------------------------------------- states that fall by orders of magnitude
+def _run(gate, value, state, grad, end):
+    """Everything in 64 bits, step by step, with the bounds of the head of this file: pairs (value, bound) of out, last, dgate, dvalue, dstate."""
+    g, v = gate.double(), value.double()
+    f, rest = torch.sigmoid(g), torch.sigmoid(-g)
+    size = 8 + (1.5 * g.abs() if gate.dtype != F32 else 0 * g)
+    off_f, off_rest = size * torch.minimum(f, rest) * U, size * rest * U
+    h, H, e = state.double(), state.double().abs(), 0 * state.double()
+    before, off, out, err = [], [], [], []
+    for t in range(gate.shape[1]):
+        before.append(h), off.append(e)
+        new = f[:, t] * H + rest[:, t] * v[:, t].abs()
+        e = f[:, t] * e + off_f[:, t] * H + off_rest[:, t] * v[:, t].abs() + 8 * U * new
+        h, H = f[:, t] * h + rest[:, t] * v[:, t], new
+        out.append(h), err.append(e)
+    last = h, e * 1.001
+    c, Z, e = end.double(), end.double().abs(), 0 * end.double()
+    back = []
+    for t in range(gate.shape[1] - 1, -1, -1):
+        D, big = grad[:, t].double() + c, grad[:, t].double().abs() + Z
+        e = e + 2 * U * big
+        gap, e_gap = before[t] - v[:, t], off[t] + U * (before[t] - v[:, t]).abs()
+        slope = f[:, t] * rest[:, t]
+        dv, e_v = rest[:, t] * D, rest[:, t] * e + (off_rest[:, t] + 2 * U * rest[:, t]) * big
+        dg, e_g = slope * gap * D, slope * (gap.abs() * e + e_gap * big + (2 * size[:, t] + 4) * U * gap.abs() * big)
+        back.append((dg, e_g * 1.001, dv, e_v * 1.001))
+        e = f[:, t] * e + off_f[:, t] * big + 8 * U * f[:, t] * big
+        c, Z = f[:, t] * D, f[:, t] * big
+    dg, eg, dv, ev = (torch.stack(x[::-1], 1) for x in zip(*back))
+    return (torch.stack(out, 1), torch.stack(err, 1) * 1.001), last, (dg, eg), (dv, ev), (c, e * 1.001)
+
+
+def _gates(kind, shape, seed):
+    r = np.random.default_rng(seed)
+    if kind == "two":                # each step keeps 0.88
+        x = np.full(shape, 2.0)
+    elif kind == "resets":           # two steps that keep next to nothing
+        x = r.choice([0.0, 3.0, 8.0, 14.0], shape)
+        x[:, 100:] = r.choice([8.0, 14.0], shape)[:, 100:]
+        for t in (20, 70):
+            x[:, t] = r.choice([-20.0, -17.0, -10.0, -5.0], (shape[0], shape[2]))
+    elif kind == "slow":             # a stretch keeps nearly all, the sequence little: products cross 1/2 between stretches, blocks and turns
+        x = r.uniform(5.5, 9.0, shape)
+    else:                            # about 1/2
+        x = r.uniform(-0.3, 0.3, shape)
+    return torch.from_numpy(x)
+
+
+@gpu
+@pytest.mark.parametrize("kind,shape", [("two", (2, 7, 8)), ("two", (1, 128, 4)), ("two", (2, 192, 24)), ("two", (3, 300, 7)), ("half", (2, 90, 64)), ("half", (40, 33, 30)),
+                                        ("resets", (2, 130, 24)), ("resets", (1, 1500, 5)), ("resets", (70, 200, 64)), ("slow", (1, 4000, 24)), ("slow", (2, 6000, 16)),
+                                        ("slow", (60, 1100, 40))])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("small", [0.0, 1.0])
+def test_a_state_and_a_gradient_that_are_forgotten_step_by_step(kind, shape, dtype, small):
+    """A first state of 10^6 (16 bits' outputs: what they hold of it) over values of 0 or 1, and the gradient of the last states alone."""
+    L = _ops()
+    B_, T, d = shape
+    gate, value = _gates(kind, shape, T).to(dtype).cuda(), (_rand(shape, F32, seed=T) * small).to(dtype)
+    state = _rand((B_, d), seed=3) * (3e3 if dtype == F16 else 1e6)
+    end, grad = _rand((B_, d), seed=5), torch.zeros(shape, dtype=dtype, device="cuda")
+    out, last, marks = L.recurrence(gate, value, state, marks=True)
+    dgate, dvalue, dstate = L.recurrence_gradient(grad, gate, value, marks, grad_state=end)
+    want = _run(gate, value, state, grad, end)
+    for got, (x, slack) in zip((out, last, dgate, dvalue, dstate), want):
+        _close(got, x, slack)
+    # and step by step, as it is served
+    now = state.clone()
+    for t in range(min(T, 100)):
+        h = L.recurrence_step(gate[:, t], value[:, t], now)
+        _close(h, want[0][0][:, t], want[0][1][:, t])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("T", [1, 5, 100, 5000])
+def test_infinite_gates_keep_everything_or_nothing(dtype, T):
+    L = _ops()
+    B_, d = 2, 20
+    value, state, grad, end = _rand((B_, T, d), dtype, 100.0), _rand((B_, d), seed=1), _rand((B_, T, d), dtype, seed=2), _rand((B_, d), seed=3)
+    gate = torch.full((B_, T, d), float("inf"), dtype=dtype, device="cuda")
+    out, last, marks = L.recurrence(gate, value, state, marks=True)
+    assert torch.equal(last, state) and torch.equal(out, state.to(dtype)[:, None].expand_as(out))
+    dgate, dvalue, dstate = L.recurrence_gradient(torch.zeros_like(grad), gate, value, marks, grad_state=end)
+    assert torch.equal(dstate, end) and not dgate.any() and not dvalue.any()
+    gate = -gate
+    out, last, marks = L.recurrence(gate, value, state, marks=True)
+    assert torch.equal(out, value) and torch.equal(last, value[:, -1].float())
+    dgate, dvalue, dstate = L.recurrence_gradient(grad, gate, value, marks, grad_state=end)
+    grad[:, -1] = (grad[:, -1].float() + end).to(dtype)
+    assert torch.equal(dvalue, grad) and not dgate.any() and not dstate.any()
+    step = state.clone()
+    assert torch.equal(L.recurrence_step(gate[:, 0], value[:, 0], step), value[:, 0]) and torch.equal(step, value[:, 0].float())
