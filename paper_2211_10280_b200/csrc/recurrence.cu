@@ -34,6 +34,7 @@
 #include "columns.cuh"
 #include "kernels.h"
 #include "layers.h"
+#include "recurrence_cut.h"
 
 namespace tensair {
 
@@ -41,10 +42,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256;
-constexpr int kSteps = kMark;            // of a thread
-constexpr uint32_t kMostCluster = 16;
-constexpr uint32_t kClusterChannels = 64;      // of a block that is part of a cluster, at most
+using namespace recurrence;
+static_assert(kSteps == kMark, "a thread's steps begin with a mark");
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -192,14 +191,9 @@ struct Joint {
     uint64_t arrived[2];                                   // barriers that count the bytes of those
 };
 
-// How a launch cuts its work: a block covers `units` pieces of channels (of all sequences, one after the other) and kThreads /
-// units stretches of kSteps steps at a time.
-struct Cut {
+struct Cut : Plan {
     FastDiv vecs;          // pieces of channels of a sequence
     uint32_t total;        // of all sequences
-    uint32_t units;        // power of two
-    uint32_t cluster, turns;
-    uint32_t groups;       // of `units` pieces
 };
 
 // The state that every stretch of the block begins with, from the stretches' compositions.  `place`: of the block in its cluster, in the order
@@ -545,22 +539,19 @@ cudaError_t with_pieces(const RecurrenceArgs& a, bool back, F&& f) {
     return e == E ? f(Columns<E, false>()) : f(Columns<E, true>());
 }
 
-constexpr uint32_t kClusters[] = {1, 2, 4, 8, 12, 16};
-constexpr int kSizes = sizeof(kClusters) / sizeof(kClusters[0]);
 // How many clusters of each size the device holds at once, two blocks to a multiprocessor: asked for once.  (148 multiprocessors hold 71 of 4, 33 of 8,
-// 14 of 16; one more than that waits until another has ended.)
+// 14 of 16; one more than that waits until another has ended.  A part of a device may hold none of the large ones.)
 template <typename T, typename C, bool kBack>
 cudaError_t rooms(size_t shared, int sms, uint32_t (&room)[kSizes]) {
     auto* kernel = k_recurrence<T, C, kBack>;
-    static std::atomic<int> known[kMaxDevices][kSizes];
+    static std::atomic<int> known[kMaxDevices][kSizes];      // one more than the answer; 0: not asked for yet
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     for (int i = 0; i < kSizes; ++i) {
-        int n = device < kMaxDevices ? known[device][i].load(std::memory_order_relaxed) : 0;
-        if (!n) {
+        int n = device < kMaxDevices ? known[device][i].load(std::memory_order_relaxed) - 1 : -1;
+        if (n < 0) {
             e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
             if (e != cudaSuccess) return e;
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = dim3(kClusters[i] * sms);
@@ -571,47 +562,18 @@ cudaError_t rooms(size_t shared, int sms, uint32_t (&room)[kSizes]) {
             attr[0].val.clusterDim = {kClusters[i], 1, 1};
             cfg.attrs = attr;
             cfg.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-            if (e != cudaSuccess) return e;
-            if (n < 1) n = 1;
-            if (device < kMaxDevices) known[device][i].store(n, std::memory_order_relaxed);
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e == cudaSuccess || kClusters[i] <= 8) e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+            if (e != cudaSuccess) {
+                if (i == 0) return e;
+                cudaGetLastError();      // a refusal of a cluster is no error
+                n = 0;
+            }
+            if (device < kMaxDevices) known[device][i].store(n + 1, std::memory_order_relaxed);
         }
         room[i] = n;
     }
     return cudaSuccess;
-}
-
-// Cuts the work so that the blocks that the device holds at once come out even: the fewest turns of the busiest one, a group of channels
-// counting half a turn more, and turns in clusters by what their exchange takes.  us, stretches x cluster: gradient of 64 sequences of 1,024 of
-// 512, bf16: 16 x 1 97, 16 x 2 89, 16 x 4 92, 32 x 1 110, 32 x 2 107, 32 x 8 206; forward, 64 padded of 1,021 of 300, fp32: 72, 68, 67, 68, 69, 151; one
-// of 65,536 of 512, bf16: 32 x 4 198, 32 x 8 137, 32 x 12 103, 32 x 16 121.
-Cut cut_of(const RecurrenceArgs& a, uint32_t e, const uint32_t (&room)[kSizes], uint32_t* grid) {
-    Cut best;
-    uint64_t least = ~0ull;
-    uint32_t most = 1;      // stretches enough for the sequence, 32 at most
-    while (most < 32 && most * kSteps < a.T) most *= 2;
-    for (uint32_t stretches = most; stretches && stretches >= most / 2; stretches /= 2) {
-        Cut c = best;
-        c.vecs = FastDiv((a.d + e - 1) / e);
-        c.total = a.B * c.vecs.divisor;
-        c.units = kThreads / stretches;
-        c.groups = (c.total + c.units - 1) / c.units;
-        static constexpr uint32_t kTurn[kSizes] = {8, 9, 10, 11, 11, 12};
-        for (int i = 0; i < kSizes; ++i) {
-            c.cluster = kClusters[i];
-            const uint64_t span = (uint64_t)c.cluster * stretches * kSteps, turns = (a.T + span - 1) / span;
-            const uint64_t rounds = (c.groups + room[i] - 1) / room[i];
-            const uint64_t cost = rounds * (2 * turns + 1) * kTurn[i];
-            if (cost < least) {
-                least = cost;
-                c.turns = (uint32_t)turns;
-                *grid = (c.groups < room[i] ? c.groups : room[i]) * c.cluster;
-                best = c;
-            }
-            if (turns == 1 || c.units * e > kClusterChannels) break;
-        }
-    }
-    return best;
 }
 
 template <typename T, typename C, bool kBack>
@@ -619,12 +581,15 @@ cudaError_t launch_cut(cudaStream_t stream, const RecurrenceArgs& a, int sms) {
     auto* kernel = k_recurrence<T, C, kBack>;
     constexpr size_t shared = (sizeof(Joint<C::E>) + 15) / 16 * 16 + (kBack ? 3 : 2) * kSteps * kThreads * 8 + (kBack ? kThreads * C::E * 4 : 0);
     static_assert(2 * (shared + 1024) <= 227 * 1024, "two blocks to a multiprocessor");
-    uint32_t room[kSizes], grid = 0;
+    uint32_t room[kSizes];
     const cudaError_t e = rooms<T, C, kBack>(shared, sms, room);
     if (e != cudaSuccess) return e;
-    const Cut c = cut_of(a, C::E, room, &grid);
+    Cut c;
+    c.vecs = FastDiv((a.d + C::E - 1) / C::E);
+    c.total = a.B * c.vecs.divisor;
+    static_cast<Plan&>(c) = cut(a.T, c.total, C::E, room);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = dim3(c.grid);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;

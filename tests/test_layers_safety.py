@@ -1,5 +1,5 @@
 """Calls of the recurrent model's operators that their documentation allows and that go wrong easily: results written over their inputs, states
-that fall by many orders of magnitude.
+that fall by many orders of magnitude, devices that hold no large clusters.
 
 Bounds of the recurrence, u = 2^-24: 1 - f is off by S u of itself, and so is f where it is below 1/2 (S = 8: expf 2 u, the fast quotient 4 u and a
 rounding each of 1 + e and the product; with gates of 16 bits 1.5 |gate| more for the rounded product with log2(e)).  Where f is 1/2 or
@@ -8,6 +8,7 @@ stretches of eight steps as often again or less; 8 u of the terms' sizes are all
 f |h| + (1 - f) |v|: nothing is left of a state that has been forgotten.
 """
 import ctypes as C
+import subprocess
 
 import numpy as np
 import pytest
@@ -191,3 +192,39 @@ def test_infinite_gates_keep_everything_or_nothing(dtype, T):
     assert torch.equal(dvalue, grad) and not dgate.any() and not dstate.any()
     step = state.clone()
     assert torch.equal(L.recurrence_step(gate[:, 0], value[:, 0], step), value[:, 0]) and torch.equal(step, value[:, 0].float())
+
+
+# ---------------------------------------------------------------- devices that hold no large clusters
+SIZES = [1, 2, 4, 8, 12, 16]
+FULL = [296, 140, 71, 33, 20, 14]
+WORK = [(T, total, e) for T in (1, 5, 8, 9, 300, 1021, 1024, 65_536, 2 ** 30) for total in (1, 75, 128, 4800, 8192, 2 ** 20, 2 ** 30) for e in (2, 4)]
+
+
+def _compiled(tmp_path, header, body, lines):
+    """What a program that includes `header` prints for each line of numbers."""
+    src, exe = tmp_path / "cut.cpp", tmp_path / "cut"
+    src.write_text(f'#include <cstdio>\n#include "{header}"\nusing namespace tensair;\nint main() {{ unsigned long long x[9]; {body} }}')
+    subprocess.check_call(["g++", "-std=c++17", "-I", str(libbuild.CSRC), str(src), "-o", str(exe)])
+    text = "\n".join(" ".join(map(str, line)) for line in lines)
+    return [list(map(int, line.split())) for line in subprocess.check_output([str(exe)], input=text, text=True).splitlines()]
+
+
+def test_the_recurrence_is_cut_for_the_clusters_that_there_are(tmp_path):
+    rooms = [FULL, [296, 140, 71, 33, 0, 0], [296, 140, 71, 0, 0, 0], [296, 0, 0, 0, 0, 0], [20, 9, 0, 0, 1, 1], [2, 1, 1, 1, 1, 1], [0] * 6]
+    body = """while (scanf("%llu %llu %llu %llu %llu %llu %llu %llu %llu", x, x + 1, x + 2, x + 3, x + 4, x + 5, x + 6, x + 7, x + 8) == 9) {
+        const uint32_t room[recurrence::kSizes] = {(uint32_t)x[3], (uint32_t)x[4], (uint32_t)x[5], (uint32_t)x[6], (uint32_t)x[7], (uint32_t)x[8]};
+        const recurrence::Plan p = recurrence::cut((uint32_t)x[0], (uint32_t)x[1], (uint32_t)x[2], room);
+        printf("%u %u %u %u %u\\n", p.units, p.cluster, p.turns, p.groups, p.grid); }"""
+    lines = [(*w, *room) for room in rooms for w in WORK]
+    got = _compiled(tmp_path, "recurrence_cut.h", body, lines)
+    assert len(got) == len(lines)
+    for (T, total, e, *room), (units, cluster, turns, groups, grid) in zip(lines, got):
+        held = room[SIZES.index(cluster)]
+        assert held or cluster == 1                                              # none of a size that is not held
+        assert units in (8, 16, 32, 64, 128, 256) and (cluster == 1 or units * e <= 64)
+        span = cluster * (256 // units) * 8
+        assert (turns - 1) * span < T <= turns * span and (groups - 1) * units < total <= groups * units
+        assert grid == min(groups, max(held, 1)) * cluster
+    # one long stream: the largest clusters of a whole device, or what there is
+    long = WORK.index((65_536, 128, 4))
+    assert [got[i * len(WORK) + long][1] for i in range(4)] == [12, 8, 4, 1]
