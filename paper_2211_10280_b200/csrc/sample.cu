@@ -26,6 +26,7 @@
 #include "columns.cuh"
 #include "kernels.h"
 #include "layers.h"
+#include "sample_cut.h"
 
 namespace tensair {
 
@@ -35,7 +36,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr uint32_t kMostCluster = 16;
+constexpr uint32_t kMostCluster = kMostRowBlocks;
 constexpr uint32_t kBuckets = 1024;          // two to a thread
 constexpr float kPerLogit = 48.0f;           // buckets of the first turn
 typedef unsigned long long mass_t;
@@ -894,42 +895,59 @@ k_sample(const __grid_constant__ SampleArgs a, uint32_t cluster, uint32_t steps,
 // their rows again out of the level-2 cache: as fast.)
 constexpr uint32_t kStage = 226 * 1024 - kSharedBytes, kStageShared = 112 * 1024 - kSharedBytes;
 
+cudaLaunchConfig_t launch_of(uint32_t rows, uint32_t cluster, uint32_t shared, cudaStream_t stream, cudaLaunchAttribute* attr) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(rows * cluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    return cfg;
+}
+
+// The kernel's attributes, and the largest cluster that the device holds (with the most shared memory that a block takes): once for each device.
+template <typename T>
+cudaError_t prepare(void (*kernel)(SampleArgs, uint32_t, uint32_t, bool, bool), int sms, uint32_t* most) {
+    static std::atomic<uint32_t> known[kMaxDevices];      // 0: not asked for yet
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    *most = device < kMaxDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (*most) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
+    if (e != cudaSuccess) return e;
+    *most = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess ? kMostCluster : 8;
+    for (; *most > 1; *most /= 2) {
+        cudaLaunchAttribute attr[1];
+        const cudaLaunchConfig_t cfg = launch_of((uint32_t)sms, *most, kSharedBytes + kStage, nullptr, attr);
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0) break;
+    }
+    cudaGetLastError();      // a refusal of a larger cluster is no error
+    if (device < kMaxDevices) known[device].store(*most, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
 }  // namespace
 
 cudaError_t launch_sample(cudaStream_t stream, const SampleArgs& a, int sms) {
     return with_type(a.logits.type, [&](auto t) {
         using T = decltype(t);
         constexpr uint32_t E = Slice<T>::E, unit = kWarps * 32 * E;      // tokens of one access of a block
-        // Blocks enough for the device, as long as a slice is worth the cluster's barriers.  us, 1, 2, 4, 8, 16 blocks to a row, each with 10
-        // for the launch: 256 rows of 100,000, 0.9 of the mass: 108, 170, 212; first 50: 65, 109; 64 rows of 10,000: 25, 28, 32, 47, 83; 16 rows of
-        // 100,000: 194, 112, 74, 53, 55; one row of 100,000: 69, 46, 29, 28, 24
-        uint32_t cluster = 1;
-        while (cluster < kMostCluster && (uint64_t)a.n * cluster < (uint64_t)sms && a.V > cluster * 8000) cluster *= 2;
+        auto* kernel = k_sample<T>;
+        uint32_t most = 0;
+        const cudaError_t e = prepare<T>(kernel, sms, &most);
+        if (e != cudaSuccess) return e;
+        const uint32_t cluster = row_blocks(a.n, a.V, sms, most);
         const uint32_t steps = (uint32_t)(((uint64_t)a.V + (uint64_t)cluster * unit - 1) / ((uint64_t)cluster * unit));
         const uint64_t bytes = (uint64_t)steps * unit * sizeof(T);
         const bool staged = bytes <= ((uint64_t)a.n * cluster <= (uint64_t)sms ? kStage : kStageShared);
         const bool whole = (uintptr_t)a.logits.data % 16 == 0 && (a.n < 2 || a.logits.stride % E == 0);
-        auto* kernel = k_sample<T>;
-        static std::atomic<bool> prepared[kMaxDevices];      // the kernel's attributes, once for each device
-        int device = 0;
-        cudaError_t e = cudaGetDevice(&device);
-        if (e != cudaSuccess) return e;
-        if (device >= kMaxDevices || !prepared[device].load(std::memory_order_relaxed)) {
-            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes + kStage);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-            if (e != cudaSuccess) return e;
-            if (device < kMaxDevices) prepared[device].store(true, std::memory_order_relaxed);
-        }
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(a.n * cluster);
-        cfg.blockDim = dim3(kThreads);
-        cfg.dynamicSmemBytes = kSharedBytes + (staged ? bytes : 0);
-        cfg.stream = stream;
         cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim = {cluster, 1, 1};
-        cfg.attrs = attr;
-        cfg.numAttrs = cluster > 1 ? 1 : 0;
+        const cudaLaunchConfig_t cfg = launch_of(a.n, cluster, kSharedBytes + (staged ? (uint32_t)bytes : 0), stream, attr);
         return cudaLaunchKernelEx(&cfg, kernel, a, cluster, steps, staged, whole);
     });
 }

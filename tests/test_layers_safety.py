@@ -228,3 +228,13 @@ def test_the_recurrence_is_cut_for_the_clusters_that_there_are(tmp_path):
     # one long stream: the largest clusters of a whole device, or what there is
     long = WORK.index((65_536, 128, 4))
     assert [got[i * len(WORK) + long][1] for i in range(4)] == [12, 8, 4, 1]
+
+
+def test_a_row_of_the_draw_is_shared_by_clusters_that_there_are(tmp_path):
+    body = """while (scanf("%llu %llu %llu %llu", x, x + 1, x + 2, x + 3) == 4) printf("%u\\n", row_blocks((uint32_t)x[0], (uint32_t)x[1], (uint32_t)x[2], (uint32_t)x[3]));"""
+    lines = [(n, V, sms, most) for n in (1, 2, 5, 9, 37, 74, 75, 148, 256, 2 ** 24) for V in (1, 8000, 8001, 16_001, 100_000, 2 ** 20) for sms in (18, 72, 148)
+             for most in (1, 2, 4, 8, 16)]
+    for (n, V, sms, most), (blocks,) in zip(lines, _compiled(tmp_path, "sample_cut.h", body, lines)):
+        assert blocks in (1, 2, 4, 8, 16) and blocks <= most
+        assert blocks == 1 or (n * blocks // 2 < sms and V > blocks // 2 * 8000)          # a half would not do
+        assert blocks == most or n * blocks >= sms or V <= blocks * 8000                  # a double is not worth it
