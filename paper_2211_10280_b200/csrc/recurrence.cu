@@ -237,7 +237,8 @@ __device__ __forceinline__ void join_block(Joint<E>& joint, const Cut& cut, uint
         } else {
             // Two neighbours send both their channels, each to half of the blocks.  What is written over has been read: who sends this turn's
             // compositions has those of the turn before, and they were sent by who had read the ones before them.
-            const float other_n = __shfl_xor_sync(__activemask(), n, 1), other_b = __shfl_xor_sync(__activemask(), b, 1);
+            const uint32_t lanes = last_lanes(channels, threadIdx.x);      // at most 64 channels: their last parts are those of the last threads
+            const float other_n = __shfl_xor_sync(lanes, n, 1), other_b = __shfl_xor_sync(lanes, b, 1);
             const bool second = c & 1;
             const float4 both = second ? make_float4(other_n, other_b, n, b) : make_float4(n, b, other_n, other_b);
 #pragma unroll 4

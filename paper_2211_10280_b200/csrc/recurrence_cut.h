@@ -55,5 +55,11 @@ inline Plan cut(uint32_t T, uint32_t total, uint32_t e, const uint32_t (&room)[k
     return best;
 }
 
+// The lanes of a thread's warp that belong to the last `channels` (a power of two from 16 on) threads of a block, as that thread does.
+#ifdef __CUDACC__
+__device__
+#endif
+inline uint32_t last_lanes(uint32_t channels, uint32_t thread) { return channels >= 32 ? 0xFFFFFFFFu : 0xFFFFu << (thread & 16); }
+
 }  // namespace recurrence
 }  // namespace tensair

@@ -238,3 +238,13 @@ def test_a_row_of_the_draw_is_shared_by_clusters_that_there_are(tmp_path):
         assert blocks in (1, 2, 4, 8, 16) and blocks <= most
         assert blocks == 1 or (n * blocks // 2 < sms and V > blocks // 2 * 8000)          # a half would not do
         assert blocks == most or n * blocks >= sms or V <= blocks * 8000                  # a double is not worth it
+
+
+def test_the_lanes_that_exchange_compositions_are_those_that_are_there(tmp_path):
+    """Blocks of a cluster have 16, 32 or 64 channels; the last part of each is a thread's, of the last ones of the block."""
+    body = 'while (scanf("%llu %llu", x, x + 1) == 2) printf("%u\\n", recurrence::last_lanes((uint32_t)x[0], (uint32_t)x[1]));'
+    lines = [(channels, thread) for channels in (16, 32, 64) for thread in range(256 - channels, 256)]
+    for (channels, thread), (mask,) in zip(lines, _compiled(tmp_path, "recurrence_cut.h", body, lines)):
+        first = thread // 32 * 32
+        assert mask == sum(1 << lane for lane in range(32) if first + lane >= 256 - channels)
+    assert "__activemask" not in (libbuild.CSRC / "recurrence.cu").read_text()
