@@ -5,11 +5,12 @@
     recurrence        h_t = f_t h_{t-1} + (1 - f_t) value_t with f = sigmoid(gate), over padded batches of sequences, and its gradient
     recurrence_step   one step of it for serving, the states updated in place
 
-layer_norm, dropout and recurrence take part in autograd where an input needs a gradient.  Every call enqueues its kernels on the
-current stream of the tensors' device and returns without waiting; tensors that another stream is still writing are ordered by the
-caller, as for torch's own operators.  Nothing is kept from one call for the next, so calls may be made from several threads
-and on several streams, and captured (a captured `backward()`, as one through torch's own operators, wants leaves that no eager graph
-still holds; torch.autograd.grad does not mind).  There is no fallback: a missing library, a CPU tensor or a refused argument is an error.
+layer_norm, dropout and recurrence take part in autograd where an input needs a gradient (backwards; forward mode is an error).
+Every call enqueues its kernels on the current stream of the tensors' device and returns without waiting; tensors that another
+stream is still writing are ordered by the caller, as for torch's own operators.  Nothing is kept from one call for the next, so calls
+may be made from several threads and on several streams, and captured (a captured `backward()`, as one through torch's own
+operators, wants leaves that no eager graph still holds; torch.autograd.grad does not mind).  There is no fallback: a missing
+library, a CPU tensor or a refused argument is an error.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ import ctypes as C
 from typing import Optional, Union
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import binding as B
 from .operators import _FLOATS, _current_stream, _need, _written
@@ -33,9 +35,14 @@ def _device_of(x, name):
 
 
 def _wants_gradient(*tensors):
+    """Whether autograd has to know of the call: backwards, or forwards (which it then refuses: a tangent would be lost silently)."""
     if torch.is_grad_enabled():
         for x in tensors:
             if x is not None and x.requires_grad:
+                return True
+    if _forward._current_level >= 0 and not torch.is_inference_mode_enabled():
+        for x in tensors:
+            if x is not None and _forward.unpack_dual(x).tangent is not None:
                 return True
     return False
 

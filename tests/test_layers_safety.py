@@ -1,5 +1,5 @@
 """Calls of the recurrent model's operators that their documentation allows and that go wrong easily: results written over their inputs, states
-that fall by many orders of magnitude, devices that hold no large clusters.
+that fall by many orders of magnitude, forward-mode derivatives, devices that hold no large clusters.
 
 Bounds of the recurrence, u = 2^-24: 1 - f is off by S u of itself, and so is f where it is below 1/2 (S = 8: expf 2 u, the fast quotient 4 u and a
 rounding each of 1 + e and the product; with gates of 16 bits 1.5 |gate| more for the rounded product with log2(e)).  Where f is 1/2 or
@@ -192,6 +192,40 @@ def test_infinite_gates_keep_everything_or_nothing(dtype, T):
     assert torch.equal(dvalue, grad) and not dgate.any() and not dstate.any()
     step = state.clone()
     assert torch.equal(L.recurrence_step(gate[:, 0], value[:, 0], step), value[:, 0]) and torch.equal(step, value[:, 0].float())
+
+
+# ---------------------------------------------------------------- derivatives that are not there
+def test_a_tangent_is_seen():
+    import torch.autograd.forward_ad as fwd
+
+    L, x = _ops(), torch.ones(3)
+    assert not L._wants_gradient(x, None)
+    with fwd.dual_level():
+        dual = fwd.make_dual(x, torch.ones(3))
+        assert L._wants_gradient(None, dual) and not L._wants_gradient(x, None)
+        with torch.no_grad():              # which leaves forward mode on
+            assert L._wants_gradient(dual)
+        with torch.inference_mode():       # which does not
+            assert not L._wants_gradient(x)
+    assert not L._wants_gradient(x)
+
+
+@gpu
+def test_forward_mode_is_refused():
+    import torch.autograd.forward_ad as fwd
+
+    L = _ops()
+    x, w, s = _rand((2, 16, 8)), _rand((8,)), _rand((2, 8))
+    with fwd.dual_level():
+        dx, dw, ds = (fwd.make_dual(t, torch.ones_like(t)) for t in (x, w, s))
+        for i, call in enumerate([lambda: L.layer_norm(dx, w), lambda: L.layer_norm(x, dw), lambda: L.layer_norm(x, w, dw), lambda: L.dropout(dx, 0.1, 1, 1),
+                                  lambda: L.dropout(x, 0.1, 1, 1, residual=dx), lambda: L.recurrence(dx, x), lambda: L.recurrence(x, dx), lambda: L.recurrence(x, x, ds),
+                                  lambda: L.recurrence_step(ds, s, s.clone()), lambda: L.recurrence_step(s, s, ds), lambda: L.layer_norm(dx, w, stats=True)]):
+            for mode in (torch.enable_grad, torch.no_grad):
+                with pytest.raises((NotImplementedError, ValueError)), mode():
+                    call()
+                    pytest.fail(f"call {i} lost a tangent")
+        assert L.layer_norm(x, w).shape == x.shape
 
 
 # ---------------------------------------------------------------- devices that hold no large clusters
