@@ -214,8 +214,9 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=8)
-    ap.add_argument("--dense", action="store_true")
-    ap.add_argument("--recurrent", action="store_true")
+    way = ap.add_mutually_exclusive_group()
+    way.add_argument("--dense", action="store_true")
+    way.add_argument("--recurrent", action="store_true")
     ap.add_argument("--generate", type=int, default=0, metavar="N")
     a = ap.parse_args()
     if a.generate and not a.recurrent:

@@ -282,3 +282,16 @@ def test_the_lanes_that_exchange_compositions_are_those_that_are_there(tmp_path)
         first = thread // 32 * 32
         assert mask == sum(1 << lane for lane in range(32) if first + lane >= 256 - channels)
     assert "__activemask" not in (libbuild.CSRC / "recurrence.cu").read_text()
+
+
+# ---------------------------------------------------------------- the example's command line
+@pytest.mark.parametrize("args", [["--dense", "--recurrent"], ["--generate", "3"]])
+def test_the_example_refuses_what_it_would_not_do(args, monkeypatch, capsys):
+    from paper_2211_10280_b200 import next_token
+
+    monkeypatch.setattr("sys.argv", ["next_token", *args])
+    for name in ("train", "train_recurrent"):
+        monkeypatch.setattr(next_token, name, lambda *a, **k: pytest.fail("it went on"))
+    with pytest.raises(SystemExit):
+        next_token.main()
+    assert args[0] in capsys.readouterr().err
