@@ -194,6 +194,28 @@ def test_infinite_gates_keep_everything_or_nothing(dtype, T):
     assert torch.equal(L.recurrence_step(gate[:, 0], value[:, 0], step), value[:, 0]) and torch.equal(step, value[:, 0].float())
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_every_gate_has_the_factor_of_its_formula(dtype):
+    """One step from 1 to 0 is f, one from 0 to 1 is 1 - f: all gates of 16 bits, a million of 32."""
+    L = _ops()
+    if dtype == F32:
+        g = torch.cat([_rand((500_000,), std=30.0), _rand((500_000,), std=2.0, seed=1), _rand((50_000,), std=1e-3, seed=2)])
+    else:
+        g = torch.arange(-2 ** 15, 2 ** 15, dtype=torch.int32).to(torch.int16).view(dtype).cuda()
+        g = g[~torch.isnan(g)]
+    g = g.view(-1, 50) if dtype == F32 else g[None]
+    one, zero = torch.ones(g.shape, device="cuda"), torch.zeros(g.shape, device="cuda")
+    keep, take = one.clone(), zero.clone()
+    L.recurrence_step(g, zero.to(dtype), keep)
+    L.recurrence_step(g, one.to(dtype), take)
+    wide = g.double()
+    f, rest = torch.sigmoid(wide), torch.sigmoid(-wide)
+    size = (8 + (0 if dtype == F32 else 1.5 * wide.abs().clamp(max=100))) * torch.minimum(f, rest) * U
+    for got, want in ((keep, f), (take, rest)):      # below 2^-126: zero, or what fp32 has of it
+        assert ((got.double() - want).abs() <= size + want * U + 2.0 ** -126).all()
+
+
 # ---------------------------------------------------------------- derivatives that are not there
 def test_a_tangent_is_seen():
     import torch.autograd.forward_ad as fwd
