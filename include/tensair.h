@@ -613,7 +613,7 @@ TENSAIR_API int tensair_layer_norm(const tensair_norm* norm, const tensair_rows*
  * Its gradient.  With c = (x - mean) rstd and g = grad weight:
  *     dx = rstd (g - mean(g) - c mean(g c)),    dweight = sum over rows of grad c,    dbias = sum over rows of grad
  * grad is of the type of what the forward call wrote, dx of x's type, dweight and dbias ([d], param_type) nullable; norm->bias is not
- * looked at.  The sums over rows are taken in an order that n, d and the types fix.  dx may be grad (of the same type).
+ * looked at.  The sums over rows are taken in an order that n, d, the types and the rows' alignment fix.  dx may be grad (of the same type).
  * workspace: needed where dweight or dbias is; tensair_norm_workspace_bytes(n, d) bytes, 256-byte aligned; it
  * holds nothing between calls, and calls that share one must be ordered by their streams.
  */
@@ -687,7 +687,7 @@ TENSAIR_API int tensair_recurrence_step(const tensair_sequences* seq, float* sta
  * temperature) in 64 bits, rounded to a multiple of 2^-b, b = min(46, 62 - bits of V - 1), so that sums are exact.  Kept are
  *     the first top_k tokens (top_k <= 0 or >= V: all);
  *     of those the tokens with less than top_p * (their weight) before them, one at least (top_p >= 1: all);
- *     of those the ones with logit - largest >= temperature * ln(min_p) (min_p <= 0: all).
+ *     of those the ones with logit - largest >= temperature * ln(min_p) (min_p <= 0: all; >= 1: the largest and its ties).
  * token = the lowest id whose running kept weight, ids ascending, exceeds floor(u * kept weight), u clamped to [0, 1); logprob =
  * ln(its share of the kept weight).  A temperature above 1e30 counts as 1e30.  temperature <= 0 (or NaN): the lowest id of the largest logit, logprob 0.  A row
  * without a logit above minus infinity has token -1 and logprob minus infinity.  Where the largest logit is plus infinity only such tokens have weight.

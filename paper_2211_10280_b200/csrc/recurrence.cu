@@ -23,9 +23,10 @@
 //
 // The next stretch's inputs are on their way into shared memory (asynchronous copies, each thread its own) while this one's are worked on.
 //
-// Bound by instructions and the barriers of a turn: 64 sequences of 1,024 of 512 in bf16 take 66 us forward (201 MB, 35 instructions an
-// element, issue slots 0.55 busy) and 91 to 95 us backward (336 MB, 52 instructions, 0.61); from 128 sequences on 0.73 us a sequence forward, 4.3 TB/s.
-// One stream of 65,536 steps: 95 to 102 us, a chain of 22 turns of 12 blocks.  One step of 64 streams: 4.2 us, a launch.
+// Bound by instructions and the barriers of a turn: 64 sequences of 1,024 of 512 in bf16 take 61 us forward (201 MB), 62 with marks (218 MB, 37
+// instructions an element, issue slots 0.65 busy), and 97 us backward (352 MB, 54 instructions, 0.61); from 64 to 256 sequences 0.76 us a sequence
+// forward, 4.2 TB/s.  One stream of 65,536 steps: 98 us, a chain of 22 turns of 12 blocks.  One step of 64 streams: 3 us, a launch.  Rows that
+// begin between two pieces (301 channels of 16 bits) are read one by one and not ahead of their turn: 64 sequences of 1,021 take 105 us and 183.
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -55,8 +56,10 @@ __device__ __forceinline__ float reciprocal_approx(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// e = exp(gate).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by (1.5 |gate| + 2) 2^-24 of it; half a unit of the
-// gate's own last place is 10^4 times as much.  Gates of 32 bits: expf.
+// e = exp(gate).  Gates of 16 bits: 2^x of the rounded product with log2(e), off by (1.5 |gate| + 2) 2^-24 of it, which is a choice: it is as if the
+// gate were off by that, and half a unit of the gate's own last place is at least 9,000 (bf16) or 1,100 (fp16) times as much for gates of 1 and
+// more, 160 or 20 times for one of 0.01.  (f and 1 - f, whichever is smaller: at most 1.4 times that off, of all gates of 16 bits.)
+// Gates of 32 bits: expf; f and 1 - f at most 4.3 2^-24 off.
 template <typename T>
 __device__ __forceinline__ float exp_of(float gate) {
     if constexpr (sizeof(T) == 2) return exp2_approx(gate * 1.44269504f);

@@ -33,7 +33,7 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=
     each row (float32; top_k int32) in which a value <= 0 (top_p: >= 1) switches that setting off (temperature: draws the largest).
 
     A logit of minus infinity, or NaN, is never drawn; a row without any other has token -1.  Returns int64 (n,) (`out`, if
-    given), with logprobs also the logarithms, float32, of the tokens' probabilities among those kept."""
+    given), with logprobs also the logarithms, float32, of the tokens' probabilities among those kept.  Neither takes part in autograd."""
     index = _device_of(logits, "logits")
     kind = _FLOATS.get(logits.dtype)
     if kind is None or logits.dim() != 2:
