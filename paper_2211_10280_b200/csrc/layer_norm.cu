@@ -15,8 +15,8 @@
 // Rows that fit into no block: 1,024 of 20,000 in bf16 43 us forward; the gradient 281, of which 231 are the sums over rows, by columns of
 // 2 or 4 bytes to a thread, from a grid that reads its inputs once more.
 //
-// The sums over rows are held in 32 bits: a thread adds up n / 9,472 to n / 296 rows, by their width (n / 1,024 of the widest), and what the threads
-// have is joined block by block, 32 blocks to a sum.
+// The sums over rows are held in 32 bits: a thread adds up n / 9,472 to n / 296 rows, by their width (n / 1,024 of the widest); the blocks' partial
+// rows are joined by sums of up to 10 and of 32 of those.
 #include "columns.cuh"
 #include "layers.h"
 

@@ -9,6 +9,7 @@ f |h| + (1 - f) |v|: nothing is left of a state that has been forgotten.
 """
 import ctypes as C
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -214,6 +215,30 @@ def test_every_gate_has_the_factor_of_its_formula(dtype):
     size = (8 + (0 if dtype == F32 else 1.5 * wide.abs().clamp(max=100))) * torch.minimum(f, rest) * U
     for got, want in ((keep, f), (take, rest)):      # below 2^-126: zero, or what fp32 has of it
         assert ((got.double() - want).abs() <= size + want * U + 2.0 ** -126).all()
+
+
+# ---------------------------------------------------------------- first calls
+@gpu
+def test_the_first_calls_of_a_process_may_be_captured():
+    """What a device is asked once, and what kernels are told once, happens while the graph is being captured."""
+    code = """
+import torch
+from paper_2211_10280_b200 import layers, sampling
+x, u = torch.randn(1, 40_000, device="cuda"), torch.rand(1, device="cuda")
+a, s = torch.randn(1, 5000, 64, device="cuda"), torch.randn(1, 64, device="cuda")
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    token = sampling.sample(x, u, 0.9, 50, 0.9)
+    out, last, marks = layers.recurrence(a, a, s, marks=True)
+    back = layers.recurrence_gradient(a, a, a, marks)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(token, sampling.sample(x, u, 0.9, 50, 0.9))
+again = layers.recurrence(a, a, s, marks=True)
+assert all(torch.equal(p, q) for p, q in zip((out, last, marks), again))
+assert all(torch.equal(p, q) for p, q in zip(back, layers.recurrence_gradient(a, a, a, marks)))
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=300, cwd=libbuild.HERE.parent)
 
 
 # ---------------------------------------------------------------- derivatives that are not there
